@@ -418,6 +418,110 @@ parle_status parle_k_fc_head(void *hip_stream, int32_t dtype, int32_t n, int32_t
 parle_status parle_k_gap_head(void *hip_stream, const parle_act_desc *desc, const void *feat, const int32_t *labels,
                               float *loss_img, float *loss, void *dlogits, void *dfeat);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of token models: what a language model's replicas run beside the layers above.  n replicas per
+ * call, tensors one block per replica as above; descriptors are plain structs.  dtype 0: fp32, 1: bf16
+ * (raw 16-bit, rounded to nearest even once, on the store); sums, statistics and gradients of parameters are fp32.
+ * Device pointers are 16-byte aligned; rows need no alignment of their own, so odd widths are as good as even ones.
+ * Asynchronous on `hip_stream`; scratch belongs to one call at a time and need not be cleared; nothing is
+ * allocated, every call can be captured into a graph, and results do not depend on what ran before (no atomics
+ * on floating point).  A count of zero (tokens, rows) is allowed: pointers of empty tensors may then be NULL.
+ * Errors: EINVAL (a field or a NULL pointer), ESIZE (a size the kernels do not index, scratch too small), EALIGN,
+ * EHIP, each with a text behind parle_last_error(NULL).
+ *
+ * 8-bit tensors: e4m3 codes (1-4-3 bits, largest 448, no infinity) with E8M0 scales: byte s stands for 2^(s-127), and a code c
+ * under it for the value c * 2^(s-127).  `block` values of a tensor share a scale: 1 x 128 along the row (block = 1) or
+ * 128 x 128 (block = 128).  A matrix [rows, cols] has codes [rows][cols rounded up to 16], the padding zero, and scales
+ * [ceil(rows / block)][ceil(cols / 128) rounded up to 4], the padding zero.  Quantising takes the smallest power of two that
+ * keeps the largest finite magnitude of a block within 448 (1 for a block of zeros) and rounds to nearest even; NaN and
+ * infinities become the NaN code.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+  int32_t dtype;        /* of out, dout */
+  int32_t table_dtype;  /* of the table in the forward call */
+  int32_t n, tokens, vocab, dim;
+  int64_t table_stride; /* elements from one replica's table (and table gradient) to the next, >= vocab * dim */
+  float scale;          /* sqrt(dim), 1, ... */
+} parle_embed_desc;
+/* out [n][tokens, dim] = scale * table[a][tokens[a][i]]; a token outside 0 .. vocab-1 (padding) gives a row of zeros. */
+parle_status parle_k_embed_forward(void *hip_stream, const parle_embed_desc *desc, const void *table, const int32_t *tokens,
+                                   void *out);
+/* dtable [n][vocab, dim] fp32 (rows table_stride apart) = scale * sum of dout [n][tokens, dim] over the positions of each
+ * token, written whole: zero for tokens that do not occur.  The sum's order depends on the tokens alone. */
+parle_status parle_k_embed_backward(void *hip_stream, const parle_embed_desc *desc, const int32_t *tokens, const void *dout,
+                                    void *scratch, int64_t scratch_bytes, float *dtable);
+int64_t parle_k_embed_scratch_bytes(const parle_embed_desc *desc); /* -1 on a bad descriptor */
+
+typedef struct {
+  int32_t dtype;    /* of x, resid, h, y and their gradients */
+  int32_t w_dtype;  /* of w: fp32 parameters or their bf16 copy */
+  int32_t n, rows, dim;
+  int64_t w_stride; /* elements from one replica's w (and dw) to the next, >= dim */
+  float eps;
+} parle_norm_desc;
+/* h = x + resid (rounded to dtype; resid NULL: h = x), rstd = 1 / sqrt(mean_i h_i^2 + eps), y = w * h * rstd, row by row.
+ * h, y, rstd [n][rows] and the pair q, scales (y with a scale for 1 x 128 values, quantised from fp32) may each be
+ * NULL; y or q is wanted. */
+parle_status parle_k_rmsnorm_forward(void *hip_stream, const parle_norm_desc *desc, const void *x, const void *resid,
+                                     const void *w, void *h, void *y, uint8_t *q, uint8_t *scales, float *rstd);
+/* From h and rstd of the forward pass and dout = dy:  g = dout * w,  dx = rstd * (g - h * rstd^2 * mean_i(g_i h_i)) + dresid
+ * (the gradient of x and of resid; dresid, the gradient that h receives elsewhere, may be NULL),
+ * dw [n][dim] fp32 (rows w_stride apart) = sum over the rows of dout * h * rstd, in a fixed order. */
+parle_status parle_k_rmsnorm_backward(void *hip_stream, const parle_norm_desc *desc, const void *h, const void *w,
+                                      const float *rstd, const void *dout, const void *dresid, void *scratch,
+                                      int64_t scratch_bytes, void *dx, float *dw);
+int64_t parle_k_rmsnorm_scratch_bytes(const parle_norm_desc *desc); /* -1 on a bad descriptor */
+
+typedef struct {
+  int32_t dtype;      /* of src */
+  int32_t block;      /* 1: a scale for 1 x 128 values, 128: for 128 x 128 */
+  int32_t n, rows, cols;
+  int64_t ld, stride; /* elements of src from row to row (>= cols) and from replica to replica */
+} parle_quant_desc;
+/* src [n][rows, cols] -> q, scales; and qt, scales_t of its transpose [cols, rows] from the same pass: with block = 128 the
+ * same values, with block = 1 values of their own, as the scales then run down the columns.  Either pair may be NULL. */
+parle_status parle_k_fp8_quantize(void *hip_stream, const parle_quant_desc *desc, const void *src, uint8_t *q, uint8_t *scales,
+                                  uint8_t *qt, uint8_t *scales_t);
+
+typedef struct {
+  int32_t out_dtype;           /* of out */
+  int32_t b_block;             /* block of b: 1 or 128 (a has block 1) */
+  int32_t accumulate;          /* 1: added to what out holds */
+  int32_t n, rows, cols, depth;
+  int64_t ld_out, out_stride;  /* elements of out from row to row (>= cols) and from replica to replica */
+} parle_fp8_desc;
+/* out [n][rows, cols] (+)= a b^T + bias: a [n][rows, depth] and b [n][cols, depth] 8-bit with their scales, products and sums
+ * in fp32; bias [n][cols] fp32 or NULL.  A linear layer is y = x w^T (b = w), dx = dy w (b = the transpose of w), dw = dy^T x
+ * (a, b = the transposes of dy and x, b_block = 1). */
+parle_status parle_k_fp8_matmul(void *hip_stream, const parle_fp8_desc *desc, const uint8_t *a, const uint8_t *a_scales,
+                                const uint8_t *b, const uint8_t *b_scales, const float *bias, void *scratch,
+                                int64_t scratch_bytes, void *out);
+int64_t parle_k_fp8_scratch_bytes(const parle_fp8_desc *desc); /* -1 on a bad descriptor */
+
+#define PARLE_LOGPROB_MAX_TOP 64
+typedef struct {
+  int32_t dtype;  /* of logits, dlogits */
+  int32_t n, rows, classes;
+  int32_t top;    /* alternatives per row, 0 .. PARLE_LOGPROB_MAX_TOP */
+  int64_t ld;     /* elements from row to row of logits and dlogits, >= classes; columns from `classes` on are not touched */
+} parle_logprob_desc;
+/* Row by row of logits [n][rows, ld], p = softmax: lse = log sum exp, logp = log p[label], entropy = -sum p log p (all [n][rows]
+ * fp32), and the `top` most likely classes, top_ids [n][rows][top] with their log probabilities top_logp, the lower class
+ * first where two are equal; -1 and -inf where a row has no more classes above -inf.  logp, entropy, lse may each be NULL;
+ * top_ids and top_logp are NULL where top is 0.  A label outside 0 .. classes-1 gives logp 0.  A row of -inf only has lse = -inf,
+ * entropy 0 and logp = -inf.  A NaN or +inf in a row makes its logp, entropy and lse NaN, and its alternatives unspecified. */
+parle_status parle_k_logprob_forward(void *hip_stream, const parle_logprob_desc *desc, const void *logits, const int32_t *labels,
+                                     void *scratch, int64_t scratch_bytes, float *logp, float *entropy, float *lse,
+                                     int32_t *top_ids, float *top_logp);
+/* dlogits = dlogp * (onehot(label) - p) - dentropy * p * (log p + entropy), with lse and entropy of the forward pass; dlogp counts
+ * as 0 where the label is outside; dentropy (then also entropy) may be NULL; a row of -inf only has gradient 0.  p is e^(logit - lse):
+ * it has the digits that lse has after the point in fp32, none where a row's largest logit is beyond 2^24.  dlogits may be
+ * logits: an element is read by the thread that writes it. */
+parle_status parle_k_logprob_backward(void *hip_stream, const parle_logprob_desc *desc, const void *logits, const int32_t *labels,
+                                      const float *lse, const float *entropy, const float *dlogp, const float *dentropy,
+                                      void *dlogits);
+int64_t parle_k_logprob_scratch_bytes(const parle_logprob_desc *desc); /* -1 on a bad descriptor */
+
 #ifdef __cplusplus
 }
 #endif

@@ -60,6 +60,28 @@ class parle_act_desc(C.Structure):
     _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "batch", "h", "w", "c")]
 
 
+class parle_embed_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "table_dtype", "n", "tokens", "vocab", "dim")] + [
+        ("table_stride", C.c_int64), ("scale", C.c_float)]
+
+
+class parle_norm_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "w_dtype", "n", "rows", "dim")] + [("w_stride", C.c_int64), ("eps", C.c_float)]
+
+
+class parle_quant_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "block", "n", "rows", "cols")] + [("ld", C.c_int64), ("stride", C.c_int64)]
+
+
+class parle_fp8_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("out_dtype", "b_block", "accumulate", "n", "rows", "cols", "depth")] + [
+        ("ld_out", C.c_int64), ("out_stride", C.c_int64)]
+
+
+class parle_logprob_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "rows", "classes", "top")] + [("ld", C.c_int64)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -112,9 +134,26 @@ _SIGNATURES = {
                          C.c_void_p, C.c_void_p],
     "parle_k_fc_head": [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                         C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_embed_forward": [C.c_void_p, C.POINTER(parle_embed_desc), C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_embed_backward": [C.c_void_p, C.POINTER(parle_embed_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
+    "parle_k_rmsnorm_forward": [C.c_void_p, C.POINTER(parle_norm_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_rmsnorm_backward": [C.c_void_p, C.POINTER(parle_norm_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p],
+    "parle_k_fp8_quantize": [C.c_void_p, C.POINTER(parle_quant_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_fp8_matmul": [C.c_void_p, C.POINTER(parle_fp8_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                           C.c_void_p, C.c_int64, C.c_void_p],
+    "parle_k_logprob_forward": [C.c_void_p, C.POINTER(parle_logprob_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_logprob_backward": [C.c_void_p, C.POINTER(parle_logprob_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_void_p, C.c_void_p],
 }
-EXPORTS = sorted(list(_SIGNATURES) + ["parle_last_error", "parle_destroy", "parle_k_conv_scratch_bytes",
-                                         "parle_k_layer_scratch_bytes"])
+_SCRATCH_BYTES = {
+    "parle_k_conv_scratch_bytes": parle_conv_desc, "parle_k_layer_scratch_bytes": parle_act_desc,
+    "parle_k_embed_scratch_bytes": parle_embed_desc, "parle_k_rmsnorm_scratch_bytes": parle_norm_desc,
+    "parle_k_fp8_scratch_bytes": parle_fp8_desc, "parle_k_logprob_scratch_bytes": parle_logprob_desc,
+}
+EXPORTS = sorted(list(_SIGNATURES) + list(_SCRATCH_BYTES) + ["parle_last_error", "parle_destroy"])
 
 
 def lib():
@@ -133,10 +172,10 @@ def lib():
         L.parle_last_error.restype = C.c_char_p
         L.parle_destroy.argtypes = [C.c_void_p]
         L.parle_destroy.restype = None
-        L.parle_k_conv_scratch_bytes.argtypes = [C.POINTER(parle_conv_desc)]
-        L.parle_k_conv_scratch_bytes.restype = C.c_int64
-        L.parle_k_layer_scratch_bytes.argtypes = [C.POINTER(parle_act_desc)]
-        L.parle_k_layer_scratch_bytes.restype = C.c_int64
+        for name, desc in _SCRATCH_BYTES.items():
+            fn = getattr(L, name)
+            fn.argtypes = [C.POINTER(desc)]
+            fn.restype = C.c_int64
         _lib = L
     return _lib
 
@@ -333,6 +372,60 @@ def parle_k_fc_head(dtype, feat, w, bias, labels, relu_mask, loss_img, loss, dlo
 def parle_k_gap_head(desc, feat, labels, loss_img, loss, dlogits, dfeat, stream=None):
     _check(lib().parle_k_gap_head(_stream_handle(stream), C.byref(desc), _ptr(feat), _ptr(labels), _ptr(loss_img),
                                   _ptr(loss), _ptr(dlogits), _ptr(dfeat)))
+
+def parle_k_embed_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_embed_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_embed_forward(desc, table, tokens, out, stream=None):
+    _check(lib().parle_k_embed_forward(_stream_handle(stream), C.byref(desc), _ptr(table), _ptr(tokens), _ptr(out)))
+
+
+def parle_k_embed_backward(desc, tokens, dout, scratch, dtable, stream=None):
+    _check(lib().parle_k_embed_backward(_stream_handle(stream), C.byref(desc), _ptr(tokens), _ptr(dout), _ptr(scratch),
+                                        _nbytes(scratch), _ptr(dtable)))
+
+
+def parle_k_rmsnorm_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_rmsnorm_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_rmsnorm_forward(desc, x, resid, w, h, y, q, scales, rstd, stream=None):
+    _check(lib().parle_k_rmsnorm_forward(_stream_handle(stream), C.byref(desc), _ptr(x), _ptr(resid), _ptr(w), _ptr(h), _ptr(y),
+                                         _ptr(q), _ptr(scales), _ptr(rstd)))
+
+
+def parle_k_rmsnorm_backward(desc, h, w, rstd, dout, dresid, scratch, dx, dw, stream=None):
+    _check(lib().parle_k_rmsnorm_backward(_stream_handle(stream), C.byref(desc), _ptr(h), _ptr(w), _ptr(rstd), _ptr(dout),
+                                          _ptr(dresid), _ptr(scratch), _nbytes(scratch), _ptr(dx), _ptr(dw)))
+
+
+def parle_k_fp8_quantize(desc, src, q, scales, qt, scales_t, stream=None):
+    _check(lib().parle_k_fp8_quantize(_stream_handle(stream), C.byref(desc), _ptr(src), _ptr(q), _ptr(scales), _ptr(qt),
+                                      _ptr(scales_t)))
+
+
+def parle_k_fp8_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_fp8_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_fp8_matmul(desc, a, a_scales, b, b_scales, bias, scratch, out, stream=None):
+    _check(lib().parle_k_fp8_matmul(_stream_handle(stream), C.byref(desc), _ptr(a), _ptr(a_scales), _ptr(b), _ptr(b_scales),
+                                    _ptr(bias), _ptr(scratch), _nbytes(scratch), _ptr(out)))
+
+
+def parle_k_logprob_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_logprob_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_logprob_forward(desc, logits, labels, scratch, logp, entropy, lse, top_ids, top_logp, stream=None):
+    _check(lib().parle_k_logprob_forward(_stream_handle(stream), C.byref(desc), _ptr(logits), _ptr(labels), _ptr(scratch),
+                                         _nbytes(scratch), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logp)))
+
+
+def parle_k_logprob_backward(desc, logits, labels, lse, entropy, dlogp, dentropy, dlogits, stream=None):
+    _check(lib().parle_k_logprob_backward(_stream_handle(stream), C.byref(desc), _ptr(logits), _ptr(labels), _ptr(lse),
+                                          _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits)))
 
 
 class Parle:

@@ -1,0 +1,400 @@
+// Rows of a table by token, scaled, and the table's gradient.
+//
+// Forward: out[i] = scale * table[tokens[i]], a copy whose source rows are anywhere.  Groups of lanes walk a row in
+// steps of eight elements.
+//
+// Gradient: dtable[v] = scale * sum of dout[i] over the positions i with tokens[i] = v.  A row of the table belongs to a run of
+// equal keys of the sorted tokens, so nothing is added atomically and the order of a sum depends on the tokens alone:
+//   1. One workgroup per replica sorts (token, position) in LDS, a stable radix sort by 6 bits a pass; the other workgroups
+//      meanwhile write the table's zeros, which is most of the bytes.  More tokens than a workgroup sorts are
+//      sorted in tiles, and tiles are merged in pairs.
+//   2. The sorted positions are cut into chunks of kChunk, whatever the tokens: a frequent token spreads over many
+//      chunks.  A group of lanes sums the runs of its chunk; a run that ends inside goes to the table, one that crosses a border
+//      to scratch.
+//   3. Runs of several chunks are joined, chunk by chunk in order.
+#include <algorithm>
+
+#include "tok.h"
+
+namespace {
+
+using namespace tok;
+
+constexpr int kThreads = 256;
+
+// `lanes` = 2^lane_shift threads per row.  ROWS rows per group of lanes, their loads in flight together.
+template <typename TI, typename TO, int ROWS>
+__global__ __launch_bounds__(kThreads) void k_embed_fwd(const TI *table, long long table_rs, const int32_t *tokens, int T, int V,
+                                                        int D, float scale, int lane_shift, TO *out) {
+  const int lanes = 1 << lane_shift, per_block = kThreads >> lane_shift;
+  const int rep = blockIdx.y;
+  const long long first = ((long long)blockIdx.x * per_block + (threadIdx.x >> lane_shift)) * ROWS;
+  if (first >= T) return;
+  const TI *src[ROWS];
+  bool live[ROWS], exists[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    exists[r] = first + r < T;
+    const int t = exists[r] ? tokens[(long long)rep * T + first + r] : -1;
+    live[r] = t >= 0 && t < V;
+    src[r] = table + rep * table_rs + (long long)(live[r] ? t : 0) * D;
+  }
+  TO *dst = out + ((long long)rep * T + first) * D;
+  for (int c = (threadIdx.x & (lanes - 1)) * kVec; c < D; c += lanes * kVec) {
+    float v[ROWS][kVec];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (live[r]) {
+        load8(src[r] + c, D - c, 0.f, v[r]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[r][i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (!exists[r]) continue;
+      if (live[r]) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[r][i] *= scale;
+      }
+      store8(dst + (long long)r * D + c, D - c, v[r]);
+    }
+  }
+}
+
+// ---- gradient ----
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / PARLE_WAVE;
+constexpr int kMostItems = 16, kTile = kSortThreads * kMostItems;  // tokens that one workgroup sorts
+constexpr int kDigitBits = 6, kDigits = 1 << kDigitBits;
+constexpr int kChunk = 32;  // sorted positions of one group of lanes
+
+// A stable sort of one tile by key, in LDS: thread t of wavefront w holds items w * 64 * ITEMS + 64 j + lane.
+// The rank of an item among equal digits is its rank in the wavefront's vector (from ballots) plus what earlier vectors and
+// wavefronts hold of the digit.
+template <int ITEMS>
+__device__ void sort_tile(const int32_t *tokens, int first, int count, int V, int bits, uint32_t *keys_out, uint32_t *pos_out,
+                          uint32_t *lds) {
+  constexpr int kItems = kSortThreads * ITEMS;
+  uint32_t *skey = lds, *hist = lds + kItems;                       // hist [digit][wave]
+  unsigned short *spos = (unsigned short *)(hist + kDigits * kSortWaves + kSortWaves);
+  uint32_t *wave_tot = hist + kDigits * kSortWaves;
+  const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = threadIdx.x / PARLE_WAVE;
+  const int base = wave * PARLE_WAVE * ITEMS + lane;
+  uint32_t key[ITEMS];
+  unsigned short pos[ITEMS];
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    const int i = base + PARLE_WAVE * j;
+    const int t = i < count ? tokens[first + i] : -1;
+    key[j] = t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;  // what has no row goes to the end
+    pos[j] = (unsigned short)i;
+  }
+  for (int shift = 0; shift < bits; shift += kDigitBits) {
+    for (int i = threadIdx.x; i < kDigits * kSortWaves; i += kSortThreads) hist[i] = 0;
+    __syncthreads();
+    uint32_t rank[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const uint32_t digit = (key[j] >> shift) & (kDigits - 1);
+      uint64_t same = ~0ull;
+#pragma unroll
+      for (int b = 0; b < kDigitBits; ++b) {
+        const uint64_t set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+      }
+      const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+      // All lanes of the digit read, then its first lane writes, then the next vector reads: LDS keeps a wavefront's order,
+      // and volatile accesses keep the compiler's.
+      volatile uint32_t *h = &hist[digit * kSortWaves + wave];
+      const uint32_t held = *h;
+      rank[j] = held + before;
+      __builtin_amdgcn_wave_barrier();
+      if (before == 0) *h = held + __popcll(same);
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // exclusive sum over [digit][wave]; 1024 counts, one per thread
+    const uint32_t mine = hist[threadIdx.x];
+    uint32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < PARLE_WAVE; o <<= 1) {
+      const uint32_t up = __shfl_up(sum, o, PARLE_WAVE);
+      if (lane >= o) sum += up;
+    }
+    if (lane == PARLE_WAVE - 1) wave_tot[wave] = sum;
+    __syncthreads();
+    uint32_t ahead = 0;
+    for (int w = 0; w < wave; ++w) ahead += wave_tot[w];
+    hist[threadIdx.x] = ahead + sum - mine;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const uint32_t digit = (key[j] >> shift) & (kDigits - 1), to = hist[digit * kSortWaves + wave] + rank[j];
+      skey[to] = key[j];
+      spos[to] = pos[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      key[j] = skey[base + PARLE_WAVE * j];
+      pos[j] = spos[base + PARLE_WAVE * j];
+    }
+  }
+  // items past `count` have the largest key and came last: the sort leaves them at the end
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    const int i = base + PARLE_WAVE * j;
+    if (i < count) {
+      keys_out[first + i] = key[j];
+      pos_out[first + i] = (uint32_t)(first + pos[j]);
+    }
+  }
+}
+
+constexpr size_t sort_lds(int items) {
+  return (size_t)(kSortThreads * items + kDigits * kSortWaves + kSortWaves) * 4 + (size_t)kSortThreads * items * 2;
+}
+
+// Workgroups 0 .. sorters-1: one tile each of one replica; the others write zeros.
+template <int ITEMS>
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort_zero(const int32_t *tokens, int T, int V, int bits, int tiles, int n,
+                                                                  uint32_t *keys, uint32_t *pos, float *dtable, long long table_rs,
+                                                                  long long table_elems) {
+  extern __shared__ uint32_t lds[];
+  const int sorters = tiles * n;
+  if ((int)blockIdx.x < sorters) {
+    const int rep = blockIdx.x / tiles, first = (blockIdx.x % tiles) * (kSortThreads * ITEMS);
+    sort_tile<ITEMS>(tokens + (long long)rep * T, first, min(T - first, kSortThreads * ITEMS), V, bits, keys + (long long)rep * T,
+                     pos + (long long)rep * T, lds);
+    return;
+  }
+  const long long vecs = table_elems / 4, step = (long long)(gridDim.x - sorters) * kSortThreads;
+  const long long me = (long long)(blockIdx.x - sorters) * kSortThreads + threadIdx.x;
+  for (int rep = 0; rep < n; ++rep) {
+    float *row = dtable + rep * table_rs;
+    for (long long i = me; i < vecs; i += step) *(f4_any *)(row + 4 * i) = f4{0.f, 0.f, 0.f, 0.f};
+    if (me < (table_elems & 3)) row[vecs * 4 + me] = 0.f;
+  }
+}
+
+// Merges sorted runs of `len` in pairs: an item's place is its own index plus its rank in the partner run; equal keys
+// of the left run come first.
+__global__ __launch_bounds__(kThreads) void k_embed_merge(const uint32_t *keys, const uint32_t *pos, int T, long long len,
+                                                          uint32_t *keys_out, uint32_t *pos_out) {
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= T) return;
+  const long long off = (long long)blockIdx.y * T, run = i / len, pair = run & ~1ll;
+  const bool left = run == pair;
+  const long long a0 = pair * len, b0 = min(a0 + len, (long long)T), b1 = min(a0 + 2 * len, (long long)T);
+  const uint32_t k = keys[off + i];
+  long long lo = left ? b0 : a0, hi = left ? b1 : b0;
+  const long long from = lo;
+  while (lo < hi) {
+    const long long mid = (lo + hi) / 2;
+    const uint32_t m = keys[off + mid];
+    if (left ? m < k : m <= k)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  const long long to = a0 + (i - (left ? a0 : b0)) + (lo - from);
+  keys_out[off + to] = k;
+  pos_out[off + to] = pos[off + i];
+}
+
+struct SumArgs {
+  const uint32_t *keys, *pos;  // [n][T]
+  float *dtable;
+  float *part;                 // [n][chunks][2][Dp]: a run that began before the chunk; one that goes on after it
+  long long table_rs;
+  int T, V, D, Dp, chunks, lane_shift;
+  float scale;
+};
+
+// A group of lanes sums one chunk for its columns.  grid: (chunks / groups per block, column slices, n)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArgs a) {
+  const int lanes = 1 << a.lane_shift, rep = blockIdx.z;
+  const int chunk = blockIdx.x * (kThreads >> a.lane_shift) + (threadIdx.x >> a.lane_shift);
+  const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * kVec;
+  if (chunk >= a.chunks || col >= a.D) return;
+  const uint32_t *keys = a.keys + (long long)rep * a.T, *pos = a.pos + (long long)rep * a.T;
+  const T *src = dout + (long long)rep * a.T * a.D + col;
+  float *table = a.dtable + rep * a.table_rs + col;
+  float *part = a.part + ((long long)rep * a.chunks + chunk) * 2 * a.Dp + col;
+  const int first = chunk * kChunk, last = min(first + kChunk, a.T), left = a.D - col;
+  float acc[kVec] = {};
+  bool from_before = first > 0 && keys[first - 1] == keys[first];
+  constexpr int kAhead = 8;
+  for (int i = first; i < last; i += kAhead) {
+    uint32_t k[kAhead + 1];
+    float v[kAhead][kVec];
+#pragma unroll
+    for (int j = 0; j <= kAhead; ++j) k[j] = i + j < a.T ? keys[i + j] : 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i + j < last && k[j] < (uint32_t)a.V) load8(src + (long long)pos[i + j] * a.D, left, 0.f, v[j]);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j >= last || k[j] >= (uint32_t)a.V) continue;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) acc[e] += v[j][e];
+      const bool ends = k[j] != k[j + 1];
+      if (ends || i + j + 1 == last) {
+        if (ends && !from_before) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) acc[e] *= a.scale;
+          store8(table + (long long)k[j] * a.D, left, acc);
+        } else {
+          float *p = part + (from_before ? 0 : a.Dp);
+          *(f4 *)p = f4{acc[0], acc[1], acc[2], acc[3]};
+          *(f4 *)(p + 4) = f4{acc[4], acc[5], acc[6], acc[7]};
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) acc[e] = 0.f;
+        from_before = false;
+      }
+    }
+  }
+}
+
+// Joins the run that begins in a chunk and goes on after it: its parts of this chunk and of all that follow, by four
+// wavefronts that take a quarter of the chunks each.  grid: (chunks - 1, column slices, n)
+__global__ __launch_bounds__(kThreads) void k_embed_join(SumArgs a) {
+  constexpr int kWaves = kThreads / PARLE_WAVE;
+  const int chunk = blockIdx.x, rep = blockIdx.z;
+  const uint32_t *keys = a.keys + (long long)rep * a.T;
+  const int first = chunk * kChunk, end = first + kChunk;  // there is a chunk behind this one, so end < T
+  const uint32_t k = keys[end];
+  if (k >= (uint32_t)a.V || keys[end - 1] != k) return;                             // no run crosses the border
+  if (keys[first] == k && first > 0 && keys[first - 1] == k) return;               // it began before this chunk
+  // the last chunk that holds the key: binary search over the chunks' first keys
+  int lo = chunk + 1, hi = a.chunks;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (keys[mid * kChunk] == k)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  const int parts = lo - chunk;  // chunk .. lo-1
+  const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = threadIdx.x / PARLE_WAVE;
+  const int col = (blockIdx.y * PARLE_WAVE + lane) * 4;
+  __shared__ f4 red[kWaves][PARLE_WAVE];
+  const float *part = a.part + ((long long)rep * a.chunks + chunk) * 2 * a.Dp + col;
+  const int each = (parts + kWaves - 1) / kWaves, p1 = min((wave + 1) * each, parts);
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (col < a.D) {
+#pragma unroll 8
+    for (int p = wave * each; p < p1; ++p) acc += *(const f4 *)(part + (long long)p * 2 * a.Dp + (p == 0 ? a.Dp : 0));
+  }
+  red[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && col < a.D) {
+    f4 s = red[0][lane];
+    for (int w = 1; w < kWaves; ++w) s += red[w][lane];
+    float *to = a.dtable + rep * a.table_rs + (long long)k * a.D + col;
+    for (int e = 0; e < 4 && col + e < a.D; ++e) to[e] = s[e] * a.scale;
+  }
+}
+
+int lane_shift_of(int groups) {
+  int s = 0;
+  while (s < 6 && (1 << s) < groups) ++s;
+  return s;
+}
+
+int digits_of(int V) {
+  int bits = 1;
+  while (bits < 31 && (V >> bits)) ++bits;  // keys are 0 .. V
+  return bits;
+}
+
+template <typename TI, typename TO>
+hipError_t fwd(hipStream_t st, const parle_embed_desc &d, const void *table, const int32_t *tokens, void *out) {
+  int shift = 3;  // 8 .. 256 lanes per row
+  while (shift < 8 && (kVec << shift) < d.dim) ++shift;
+  const int per_block = kThreads >> shift;
+  // Four rows per group keep enough loads in flight; few rows are spread over the chip instead.
+  const bool many = (long long)d.n * ceil_div(d.tokens, per_block) >= 4096;
+  const int rows = per_block * (many ? 4 : 1);
+  const dim3 grid(ceil_div(d.tokens, rows), d.n);
+  if (many)
+    k_embed_fwd<TI, TO, 4><<<grid, kThreads, 0, st>>>((const TI *)table, d.table_stride, tokens, d.tokens, d.vocab, d.dim, d.scale, shift, (TO *)out);
+  else
+    k_embed_fwd<TI, TO, 1><<<grid, kThreads, 0, st>>>((const TI *)table, d.table_stride, tokens, d.tokens, d.vocab, d.dim, d.scale, shift, (TO *)out);
+  return hipGetLastError();
+}
+
+// Scratch: keys and positions (twice where tiles are merged), then the partial sums.
+struct Scratch {
+  long long list, lists, part, Dp;
+  int chunks;
+};
+Scratch scratch_of(const parle_embed_desc &d) {
+  Scratch s;
+  s.list = round_up((long long)d.n * d.tokens * 4, 256);
+  s.lists = d.tokens > kTile ? 4 : 2;
+  s.Dp = round_up(d.dim, 8);
+  s.chunks = ceil_div(d.tokens, kChunk);
+  s.part = (long long)d.n * s.chunks * 2 * s.Dp * 4;
+  return s;
+}
+
+template <int ITEMS>
+hipError_t sort_zero(hipStream_t st, const parle_embed_desc &d, int tiles, const int32_t *tokens, uint32_t *keys, uint32_t *pos,
+               float *dtable) {
+  const long long elems = (long long)d.vocab * d.dim;
+  const int zero = (int)std::min<long long>(1024, std::max<long long>(1, d.n * elems / (4 * kSortThreads * 4)));
+  static const hipError_t lds_ok =
+      hipFuncSetAttribute((const void *)k_embed_sort_zero<ITEMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sort_lds(ITEMS));
+  if (lds_ok != hipSuccess) return lds_ok;
+  k_embed_sort_zero<ITEMS><<<tiles * d.n + zero, kSortThreads, sort_lds(ITEMS), st>>>(
+      tokens, d.tokens, d.vocab, digits_of(d.vocab), tiles, d.n, keys, pos, dtable, d.table_stride, elems);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embed_fwd(hipStream_t st, const parle_embed_desc &d, const void *table, const int32_t *tokens, void *out) {
+  if (d.table_dtype) return d.dtype ? fwd<bf16_t, bf16_t>(st, d, table, tokens, out) : fwd<bf16_t, float>(st, d, table, tokens, out);
+  return d.dtype ? fwd<float, bf16_t>(st, d, table, tokens, out) : fwd<float, float>(st, d, table, tokens, out);
+}
+
+int64_t embed_scratch_bytes(const parle_embed_desc &d) {
+  const Scratch s = scratch_of(d);
+  return s.list * s.lists + s.part;
+}
+
+hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int32_t *tokens, const void *dout, void *scratch,
+                            float *dtable) {
+  const Scratch s = scratch_of(d);
+  char *at = (char *)scratch;
+  uint32_t *keys = (uint32_t *)at, *pos = (uint32_t *)(at + s.list);
+  const int tiles = d.tokens > kTile ? ceil_div(d.tokens, kTile) : d.tokens > 0 ? 1 : 0;
+  const auto sort = d.tokens > 4 * kSortThreads ? sort_zero<kMostItems> : d.tokens > kSortThreads ? sort_zero<4> : sort_zero<1>;
+  const hipError_t e = sort(st, d, tiles, tokens, keys, pos, dtable);
+  if (e != hipSuccess || d.tokens == 0) return e;
+  if (tiles > 1) {
+    uint32_t *keys2 = (uint32_t *)(at + 2 * s.list), *pos2 = (uint32_t *)(at + 3 * s.list);
+    for (long long len = kTile; len < d.tokens; len *= 2) {
+      k_embed_merge<<<dim3(ceil_div(d.tokens, kThreads), d.n), kThreads, 0, st>>>(keys, pos, d.tokens, len, keys2, pos2);
+      std::swap(keys, keys2);
+      std::swap(pos, pos2);
+    }
+  }
+  SumArgs a;
+  a.keys = keys, a.pos = pos, a.dtable = dtable, a.part = (float *)(at + s.list * s.lists);
+  a.table_rs = d.table_stride, a.T = d.tokens, a.V = d.vocab, a.D = d.dim, a.Dp = (int)s.Dp, a.chunks = s.chunks, a.scale = d.scale;
+  const int groups = ceil_div(d.dim, kVec);
+  a.lane_shift = lane_shift_of(groups);
+  const dim3 grid(ceil_div(s.chunks, kThreads >> a.lane_shift), ceil_div(groups, 1 << a.lane_shift), d.n);
+  if (d.dtype)
+    k_embed_chunks<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
+  else
+    k_embed_chunks<<<grid, kThreads, 0, st>>>((const float *)dout, a);
+  if (s.chunks > 1) k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}

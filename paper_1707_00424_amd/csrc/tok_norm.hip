@@ -1,0 +1,400 @@
+// Root-mean-square norm behind a residual addition, its result in the activation format or in 8 bits with a scale for
+// 128 values of a row, and its gradient.
+//
+//   h = x + resid,  rstd = 1 / sqrt(mean h^2 + eps),  y = w h rstd
+//   g = dy w,       dx = rstd (g - h rstd^2 mean(g h)) + dresid,   dw = sum over rows of dy h rstd
+//
+// Both directions read a row once into registers, reduce over it, and write: what they must move is what they move.  A
+// row belongs to a group of LANES threads, each with CH vectors of eight elements, LANES * 8 elements apart.
+#include <algorithm>
+
+#include "tok.h"
+
+namespace {
+
+using namespace tok;
+
+template <typename W>
+struct FwdArgs {
+  const W *w;
+  long long w_rs;
+  uint8_t *q, *scales;
+  float *rstd;
+  int rows, D, pitch, s_pitch;
+  float eps;
+};
+
+// Sum over a group of LANES threads, given to all of them.  Groups of more than a wavefront meet in LDS (`red`: one float per
+// wavefront of the workgroup and call site).
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, float *red) {
+  v = group_sum<(LANES < PARLE_WAVE ? LANES : PARLE_WAVE)>(v);
+  if (LANES > PARLE_WAVE) {
+    constexpr int kWaves = LANES / PARLE_WAVE;
+    if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) red[threadIdx.x / PARLE_WAVE] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v += red[w];
+  }
+  return v;
+}
+
+// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  `tail`: the vector reaches past D.
+template <typename T, typename W>
+__device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, int col, const float (&y)[kVec], T *yo) {
+  const int left = a.D - col;
+  if (yo && left > 0) store8(yo + row * a.D + col, left, y);
+  if (!a.q) return;
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) most = max(most, i < left ? finite_bits(y[i]) : 0u);
+  most = group_max<16>(most);
+  const uint32_t sb = scale_byte(most);
+  const float inv = scale_inverse(sb);
+  if (col < a.pitch) {  // codes up to the row's pitch: zeros past D
+    float c[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) c[i] = i < left ? scaled(y[i], inv) : 0.f;
+    *(u2 *)(a.q + row * a.pitch + col) = u2{codes4(c[0], c[1], c[2], c[3]), codes4(c[4], c[5], c[6], c[7])};
+  }
+  if ((threadIdx.x & 15) == 0 && (col >> 7) < a.s_pitch) a.scales[row * a.s_pitch + (col >> 7)] = left > 0 ? sb : 0;
+}
+
+// A row in the registers of LANES threads, four rows to a workgroup of 256 where LANES is a wavefront.
+template <typename T, typename W, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
+  constexpr int kBlock = LANES < 256 ? 256 : LANES;
+  __shared__ float red[kBlock / PARLE_WAVE];
+  const int rep = blockIdx.y, lane = threadIdx.x & (LANES - 1);
+  const int r = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES;
+  const bool live = r < a.rows;  // groups past the end go along: the shuffles below want whole groups
+  const long long row = (long long)rep * a.rows + min(r, a.rows - 1);
+  float v[CH][kVec];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * LANES + lane) * kVec;
+    load8(x + row * a.D + col, a.D - col, 0.f, v[c]);
+  }
+  if (resid) {
+    float u[CH][kVec];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * LANES + lane) * kVec;
+      load8(resid + row * a.D + col, a.D - col, 0.f, u[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[c][i] = stored<T>(v[c][i] + u[c][i]);
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * LANES + lane) * kVec;
+    if (h && live && col < a.D) store8(h + row * a.D + col, a.D - col, v[c]);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) sum += v[c][i] * v[c][i];
+  }
+  sum = row_sum<LANES>(sum, red);
+  const float rs = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+  if (a.rstd && live && lane == 0) a.rstd[row] = rs;
+  const W *w = a.w + rep * a.w_rs;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * LANES + lane) * kVec;
+    if (!live) continue;
+    float g[kVec], y[kVec];
+    load8(w + col, a.D - col, 0.f, g);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) y[i] = v[c][i] * rs * g[i];
+    emit<T, W>(a, row, col, y, yo);
+  }
+}
+
+// Rows longer than the registers of 1024 threads: read twice.  (`h`, where it is given, holds the sum on the second read.)
+template <typename T, typename W>
+__global__ __launch_bounds__(1024) void k_rmsnorm_fwd_long(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
+  constexpr int kLanes = 1024;
+  __shared__ float red[kLanes / PARLE_WAVE];
+  const long long row = (long long)blockIdx.y * a.rows + blockIdx.x;
+  const int padded = (int)round_up(a.D, 128 * 4);  // whole scales, and their padding
+  float sum = 0.f;
+  for (int col = threadIdx.x * kVec; col < a.D; col += kLanes * kVec) {
+    float v[kVec], u[kVec];
+    load8(x + row * a.D + col, a.D - col, 0.f, v);
+    if (resid) {
+      load8(resid + row * a.D + col, a.D - col, 0.f, u);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = stored<T>(v[i] + u[i]);
+    }
+    if (h) store8(h + row * a.D + col, a.D - col, v);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) sum += v[i] * v[i];
+  }
+  sum = row_sum<kLanes>(sum, red);
+  const float rs = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+  if (a.rstd && threadIdx.x == 0) a.rstd[row] = rs;
+  const W *w = a.w + blockIdx.y * a.w_rs;
+  for (int col = threadIdx.x * kVec; col < padded; col += kLanes * kVec) {
+    float v[kVec], u[kVec], g[kVec];
+    load8(x + row * a.D + col, a.D - col, 0.f, v);
+    if (resid) {
+      load8(resid + row * a.D + col, a.D - col, 0.f, u);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = stored<T>(v[i] + u[i]);
+    }
+    load8(w + col, a.D - col, 0.f, g);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = v[i] * rs * g[i];
+    emit<T, W>(a, row, col, v, yo);
+  }
+}
+
+// ---- gradient ----
+template <typename W>
+struct BwdArgs {
+  const W *w;
+  const float *rstd;
+  float *partial;  // [n][strips][Dp]
+  long long w_rs;
+  int rows, D, Dp, strip;
+};
+
+// A workgroup takes a strip of rows, LANES threads a row, and keeps its columns' part of dw in registers; groups of a
+// workgroup (LANES < 256) join theirs in LDS.
+template <typename T, typename W, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_bwd(const T *h, const T *dout, const T *dresid, T *dx, BwdArgs<W> a) {
+  constexpr int kBlock = LANES < 256 ? 256 : LANES, kGroups = kBlock / LANES;
+  __shared__ float red[2][kBlock / PARLE_WAVE];
+  __shared__ float join[kGroups > 1 ? kGroups * LANES * CH * kVec : 1];
+  const int rep = blockIdx.y, lane = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
+  const int r0 = blockIdx.x * a.strip, r1 = min(r0 + a.strip, a.rows);
+  float w[CH][kVec], dw[CH][kVec] = {};
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * LANES + lane) * kVec;
+    load8(a.w + rep * a.w_rs + col, a.D - col, 0.f, w[c]);
+  }
+  int turn = 0;
+  for (int r = r0; r < r1; r += kGroups) {  // the same number of turns for every thread: row_sum has a barrier
+    const bool live = r + group < r1;
+    const long long row = (long long)rep * a.rows + (live ? r + group : r1 - 1);
+    float hv[CH][kVec], dv[CH][kVec], ev[CH][kVec];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * LANES + lane) * kVec;
+      load8(h + row * a.D + col, a.D - col, 0.f, hv[c]);
+      load8(dout + row * a.D + col, a.D - col, 0.f, dv[c]);
+      if (dresid) load8(dresid + row * a.D + col, a.D - col, 0.f, ev[c]);
+    }
+    const float rs = a.rstd[row];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) sum += dv[c][i] * w[c][i] * hv[c][i];
+    sum = row_sum<LANES>(sum, red[turn]);
+    turn ^= 1;  // the next row's sums meet elsewhere: one barrier a row
+    const float k = sum / (float)a.D * rs * rs;
+    if (live) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * LANES + lane) * kVec;
+        float o[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          o[i] = rs * (dv[c][i] * w[c][i] - hv[c][i] * k);
+          if (dresid) o[i] += ev[c][i];
+          dw[c][i] += dv[c][i] * (hv[c][i] * rs);
+        }
+        if (col < a.D) store8(dx + row * a.D + col, a.D - col, o);
+      }
+    }
+  }
+  float *out = a.partial + ((long long)rep * gridDim.x + blockIdx.x) * a.Dp;
+  if (kGroups > 1) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) join[group * LANES * CH * kVec + (c * LANES + lane) * kVec + i] = dw[c][i];
+    __syncthreads();
+    for (int col = threadIdx.x; col < min(a.Dp, LANES * CH * kVec); col += kBlock) {
+      float s = 0.f;
+      for (int g = 0; g < kGroups; ++g) s += join[g * LANES * CH * kVec + col];
+      out[col] = s;
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * LANES + lane) * kVec;
+      if (col < a.Dp) {
+        *(f4 *)(out + col) = f4{dw[c][0], dw[c][1], dw[c][2], dw[c][3]};
+        *(f4 *)(out + col + 4) = f4{dw[c][4], dw[c][5], dw[c][6], dw[c][7]};
+      }
+    }
+  }
+}
+
+// Rows longer than the registers: three reads (sum, dx, and dw by columns in the kernel below).
+template <typename T, typename W>
+__global__ __launch_bounds__(1024) void k_rmsnorm_bwd_long(const T *h, const T *dout, const T *dresid, T *dx, BwdArgs<W> a) {
+  constexpr int kLanes = 1024;
+  __shared__ float red[kLanes / PARLE_WAVE];
+  const long long row = (long long)blockIdx.y * a.rows + blockIdx.x;
+  const W *w = a.w + blockIdx.y * a.w_rs;
+  float sum = 0.f;
+  for (int col = threadIdx.x * kVec; col < a.D; col += kLanes * kVec) {
+    float hv[kVec], dv[kVec], g[kVec];
+    load8(h + row * a.D + col, a.D - col, 0.f, hv);
+    load8(dout + row * a.D + col, a.D - col, 0.f, dv);
+    load8(w + col, a.D - col, 0.f, g);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) sum += dv[i] * g[i] * hv[i];
+  }
+  sum = row_sum<kLanes>(sum, red);
+  const float rs = a.rstd[row], k = sum / (float)a.D * rs * rs;
+  for (int col = threadIdx.x * kVec; col < a.D; col += kLanes * kVec) {
+    float hv[kVec], dv[kVec], g[kVec], o[kVec];
+    load8(h + row * a.D + col, a.D - col, 0.f, hv);
+    load8(dout + row * a.D + col, a.D - col, 0.f, dv);
+    load8(w + col, a.D - col, 0.f, g);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) o[i] = rs * (dv[i] * g[i] - hv[i] * k);
+    if (dresid) {
+      load8(dresid + row * a.D + col, a.D - col, 0.f, g);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) o[i] += g[i];
+    }
+    store8(dx + row * a.D + col, a.D - col, o);
+  }
+}
+template <typename T, typename W>
+__global__ __launch_bounds__(256) void k_rmsnorm_dw_long(const T *h, const T *dout, BwdArgs<W> a) {
+  const int rep = blockIdx.z, col = (blockIdx.x * 256 + threadIdx.x) * kVec;
+  if (col >= a.D) return;
+  const int r0 = blockIdx.y * a.strip, r1 = min(r0 + a.strip, a.rows);
+  float dw[kVec] = {};
+#pragma unroll 2
+  for (int r = r0; r < r1; ++r) {
+    const long long row = (long long)rep * a.rows + r;
+    float hv[kVec], dv[kVec];
+    load8(h + row * a.D + col, a.D - col, 0.f, hv);
+    load8(dout + row * a.D + col, a.D - col, 0.f, dv);
+    const float rs = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) dw[i] += dv[i] * (hv[i] * rs);
+  }
+  float *out = a.partial + ((long long)rep * gridDim.y + blockIdx.y) * a.Dp + col;
+  *(f4 *)out = f4{dw[0], dw[1], dw[2], dw[3]};
+  *(f4 *)(out + 4) = f4{dw[4], dw[5], dw[6], dw[7]};
+}
+
+// dw = sum of the strips' parts: 32 columns x 8 parts of the strips per workgroup.
+__global__ __launch_bounds__(256) void k_rmsnorm_dw_join(const float *partial, int strips, int D, int Dp, float *dw, long long w_rs) {
+  __shared__ float red[8][32];
+  const int c = threadIdx.x & 31, part = threadIdx.x >> 5, rep = blockIdx.y, col = blockIdx.x * 32 + c;
+  float s = 0.f;
+  if (col < D) {
+#pragma unroll 8
+    for (int i = part; i < strips; i += 8) s += partial[((long long)rep * strips + i) * Dp + col];
+  }
+  red[part][c] = s;
+  __syncthreads();
+  if (part == 0 && col < D) {
+    for (int p = 1; p < 8; ++p) s += red[p][c];
+    dw[rep * w_rs + col] = s;
+  }
+}
+
+constexpr int kLongest = 1024 * kVec * 2;  // elements of a row that fit the registers of its threads
+
+template <typename T, typename W>
+hipError_t fwd(hipStream_t st, const parle_norm_desc &d, const void *x, const void *resid, const void *w, void *h, void *y,
+               uint8_t *q, uint8_t *scales, float *rstd) {
+  FwdArgs<W> a;
+  a.w = (const W *)w, a.w_rs = d.w_stride, a.q = q, a.scales = scales, a.rstd = rstd;
+  a.rows = d.rows, a.D = d.dim, a.pitch = (int)round_up(d.dim, 16), a.s_pitch = (int)round_up(ceil_div(d.dim, 128), 4), a.eps = d.eps;
+  // whole scales and their padding: the threads of a row cover as much
+  const int D = q ? 128 * a.s_pitch : d.dim;
+#define PARLE_NORM(LANES, CH)                                                                                             \
+  k_rmsnorm_fwd<T, W, LANES, CH><<<dim3(ceil_div(d.rows, (LANES < 256 ? 256 : LANES) / LANES), d.n), LANES < 256 ? 256 : LANES, \
+                                   0, st>>>((const T *)x, (const T *)resid, (T *)h, (T *)y, a)
+  if (D <= 64 * kVec)
+    PARLE_NORM(64, 1);
+  else if (D <= 64 * kVec * 2)
+    PARLE_NORM(64, 2);
+  else if (D <= 256 * kVec)
+    PARLE_NORM(256, 1);
+  else if (D <= 256 * kVec * 2)
+    PARLE_NORM(256, 2);
+  else if (D <= 1024 * kVec)
+    PARLE_NORM(1024, 1);
+  else if (D <= kLongest)
+    PARLE_NORM(1024, 2);
+  else
+    k_rmsnorm_fwd_long<T, W><<<dim3(d.rows, d.n), 1024, 0, st>>>((const T *)x, (const T *)resid, (T *)h, (T *)y, a);
+#undef PARLE_NORM
+  return hipGetLastError();
+}
+
+// Strips of the gradient kernel: workgroups enough for the chip, and no more parts of dw than that needs.
+int strip_rows(const parle_norm_desc &d) {
+  const int want = std::max(1, 1024 / d.n);
+  return std::max(1, std::max(ceil_div(d.rows, want), d.dim <= 64 * kVec * 2 ? 16 : 2));
+}
+
+template <typename T, typename W>
+hipError_t bwd(hipStream_t st, const parle_norm_desc &d, const void *h, const void *w, const float *rstd, const void *dout,
+               const void *dresid, float *partial, void *dx, float *dw) {
+  BwdArgs<W> a;
+  a.w = (const W *)w, a.rstd = rstd, a.partial = partial, a.w_rs = d.w_stride;
+  a.rows = d.rows, a.D = d.dim, a.Dp = (int)round_up(d.dim, kVec), a.strip = strip_rows(d);
+  const int strips = ceil_div(d.rows, a.strip);
+#define PARLE_NORM(LANES, CH)                                                                                 \
+  k_rmsnorm_bwd<T, W, LANES, CH><<<dim3(strips, d.n), LANES < 256 ? 256 : LANES, 0, st>>>(                    \
+      (const T *)h, (const T *)dout, (const T *)dresid, (T *)dx, a)
+  if (strips > 0) {
+    if (d.dim <= 16 * kVec)
+      PARLE_NORM(16, 1);
+    else if (d.dim <= 64 * kVec)
+      PARLE_NORM(64, 1);
+    else if (d.dim <= 64 * kVec * 2)
+      PARLE_NORM(64, 2);
+    else if (d.dim <= 256 * kVec)
+      PARLE_NORM(256, 1);
+    else if (d.dim <= 256 * kVec * 2)
+      PARLE_NORM(256, 2);
+    else if (d.dim <= 1024 * kVec)
+      PARLE_NORM(1024, 1);
+    else if (d.dim <= kLongest)
+      PARLE_NORM(1024, 2);
+    else {
+      k_rmsnorm_bwd_long<T, W><<<dim3(d.rows, d.n), 1024, 0, st>>>((const T *)h, (const T *)dout, (const T *)dresid, (T *)dx, a);
+      k_rmsnorm_dw_long<T, W><<<dim3(ceil_div(d.dim, 256 * kVec), strips, d.n), 256, 0, st>>>((const T *)h, (const T *)dout, a);
+    }
+  }
+#undef PARLE_NORM
+  k_rmsnorm_dw_join<<<dim3(ceil_div(d.dim, 32), d.n), 256, 0, st>>>(partial, strips, d.dim, a.Dp, dw, d.w_stride);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm_fwd(hipStream_t st, const parle_norm_desc &d, const void *x, const void *resid, const void *w, void *h,
+                              void *y, uint8_t *q, uint8_t *scales, float *rstd) {
+  if (d.dtype)
+    return d.w_dtype ? fwd<bf16_t, bf16_t>(st, d, x, resid, w, h, y, q, scales, rstd) : fwd<bf16_t, float>(st, d, x, resid, w, h, y, q, scales, rstd);
+  return d.w_dtype ? fwd<float, bf16_t>(st, d, x, resid, w, h, y, q, scales, rstd) : fwd<float, float>(st, d, x, resid, w, h, y, q, scales, rstd);
+}
+
+int64_t rmsnorm_scratch_bytes(const parle_norm_desc &d) {
+  return (int64_t)d.n * ceil_div(d.rows, strip_rows(d)) * round_up(d.dim, kVec) * 4;
+}
+
+hipError_t launch_rmsnorm_bwd(hipStream_t st, const parle_norm_desc &d, const void *h, const void *w, const float *rstd,
+                              const void *dout, const void *dresid, float *partial, void *dx, float *dw) {
+  if (d.dtype)
+    return d.w_dtype ? bwd<bf16_t, bf16_t>(st, d, h, w, rstd, dout, dresid, partial, dx, dw) : bwd<bf16_t, float>(st, d, h, w, rstd, dout, dresid, partial, dx, dw);
+  return d.w_dtype ? bwd<float, bf16_t>(st, d, h, w, rstd, dout, dresid, partial, dx, dw) : bwd<float, float>(st, d, h, w, rstd, dout, dresid, partial, dx, dw);
+}

@@ -1,0 +1,706 @@
+"""The token-model operators on the GPU against plain implementations in 64 bits, through the C ABI's binding.
+
+Tolerances count roundings: u = 2^-24 for each fp32 operation, 2^-8 for a value stored in bf16, 2^-4 for an e4m3 code, and the
+length of a sum for a sum; they are derived where they are used."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {0: 2.0 ** -24, 1: 2.0 ** -8}        # half a step of a stored value
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1707_00424_amd import binding as pb
+    pb.lib()
+    return torch, pb
+
+
+def up(v, to):
+    return -(-v // to) * to
+
+
+def dt(torch, code):
+    return torch.bfloat16 if code else torch.float32
+
+
+def randn(torch, seed, *shape, dtype=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).to(dt(torch, dtype)).cuda()
+
+
+def d64(t):
+    return t.detach().cpu().double()
+
+
+def scratch(torch, nbytes, fill=0xA5):
+    return torch.full((max(nbytes, 16),), fill, dtype=torch.uint8, device="cuda")     # what scratch holds before a call does not matter
+
+
+def within(got, want, tol, what):
+    got, want = d64(got), want.double()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    bad = ~((got - want).abs() <= tol) & ~(got == want) & ~(got.isnan() & want.isnan())
+    if bad.any():
+        i = int(bad.reshape(-1).nonzero()[0])
+        t = tol.expand_as(got).reshape(-1)[i] if hasattr(tol, "expand_as") else tol
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {i}: {got.reshape(-1)[i]} for {want.reshape(-1)[i]}, tolerance {t}")
+
+
+# ---------------------------------------------------------------- embedding
+
+@pytest.mark.parametrize("dtype,table_dtype", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("n,tokens,vocab,dim", [(1, 1, 1, 1), (2, 5, 7, 3), (3, 65, 300, 33), (1, 129, 17, 64), (2, 40, 50, 1000), (1, 9, 11, 4097), (1, 33000, 19, 8)])
+def test_embed_forward(gpu, dtype, table_dtype, n, tokens, vocab, dim):
+    torch, pb = gpu
+    rs = vocab * dim + 5
+    table = randn(torch, 1, n, rs, dtype=table_dtype)
+    t = torch.randint(-2, vocab + 2, (n, tokens), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    out = torch.full((n, tokens, dim), 7.0, dtype=dt(torch, dtype), device="cuda")
+    scale = math.sqrt(dim)
+    pb.parle_k_embed_forward(pb.parle_embed_desc(dtype, table_dtype, n, tokens, vocab, dim, rs, scale), table, t.cuda(), out)
+    rows = d64(table)[:, :vocab * dim].reshape(n, vocab, dim)
+    s32 = float(np.float32(scale))
+    ok = (t >= 0) & (t < vocab)
+    want = torch.stack([rows[a][t[a].clamp(0, vocab - 1).long()] * s32 * ok[a][:, None] for a in range(n)])
+    within(out, want, want.abs() * (U + (HALF[1] if dtype else 0)), "out")       # one product, one store
+
+
+def _embed_grad_reference(torch, t, dout, vocab, scale):
+    """Sum and sum of magnitudes of every row, and how many terms it has."""
+    n, T, D = dout.shape
+    want, mass, count = torch.zeros(n, vocab, D).double(), torch.zeros(n, vocab, D).double(), torch.zeros(n, vocab).double()
+    for a in range(n):
+        ok = (t[a] >= 0) & (t[a] < vocab)
+        want[a].index_add_(0, t[a][ok].long(), dout[a][ok])
+        mass[a].index_add_(0, t[a][ok].long(), dout[a][ok].abs())
+        count[a].index_add_(0, t[a][ok].long(), torch.ones(int(ok.sum())).double())
+    return want * scale, mass * scale, count
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,tokens,vocab,dim,kind", [
+    (1, 1, 1, 1, "uniform"), (2, 31, 7, 3, "uniform"), (3, 33, 300, 33, "zipf"), (1, 64, 5, 64, "same"), (2, 1000, 50, 520, "zipf"), (1, 1025, 3000, 96, "uniform"),
+    (2, 4097, 64, 40, "zipf"), (1, 16384, 1000, 16, "zipf"), (1, 16385, 70000, 8, "uniform"), (2, 50001, 997, 24, "zipf"), (1, 40000, 3, 8, "same"), (2, 100, 9, 9, "none"),
+    (1, 3, 5, 4100, "uniform")])
+def test_embed_backward(gpu, dtype, n, tokens, vocab, dim, kind):
+    torch, pb = gpu
+    g = torch.Generator().manual_seed(3)
+    if kind == "zipf":
+        t = (torch.exp(torch.rand((n, tokens), generator=g) * math.log(vocab + 1)) - 1).int() - (torch.rand((n, tokens), generator=g) < 0.05).int() * (vocab + 2)
+    elif kind == "same":
+        t = torch.full((n, tokens), vocab - 1, dtype=torch.int32)
+    elif kind == "none":
+        t = torch.full((n, tokens), -1, dtype=torch.int32)
+        t[:, ::2] = vocab
+    else:
+        t = torch.randint(-1, vocab + 1, (n, tokens), generator=g, dtype=torch.int32)
+    dout = randn(torch, 4, n, tokens, dim, dtype=dtype)
+    rs = vocab * dim + 3
+    desc = pb.parle_embed_desc(dtype, 0, n, tokens, vocab, dim, rs, 0.75)
+    sc = scratch(torch, pb.parle_k_embed_scratch_bytes(desc))
+    got = torch.full((n, rs), 9.0, device="cuda")
+    pb.parle_k_embed_backward(desc, t.cuda(), dout, sc, got)
+    again = torch.full((n, rs), 8.0, device="cuda")
+    pb.parle_k_embed_backward(desc, t.cuda(), dout, sc, again)
+    want, mass, count = _embed_grad_reference(torch, t, d64(dout), vocab, 0.75)
+    # a sum of c terms in any order: c - 1 roundings at most on the way of each term, one more for the scale
+    within(got[:, :vocab * dim].reshape(n, vocab, dim), want, mass * (count[..., None] + 1) * U, "dtable")
+    assert (got[:, vocab * dim:] == 9.0).all(), "what lies behind the table was written"
+    assert torch.equal(got[:, :vocab * dim], again[:, :vocab * dim]), "two calls differ"
+
+
+def test_embed_without_tokens(gpu):
+    torch, pb = gpu
+    desc = pb.parle_embed_desc(1, 0, 2, 0, 5, 3, 16, 1.0)
+    got = torch.full((2, 16), 9.0, device="cuda")
+    pb.parle_k_embed_backward(desc, None, None, None, got)
+    assert (got[:, :15] == 0).all() and (got[:, 15] == 9).all()
+    pb.parle_k_embed_forward(desc, got, None, None)
+
+
+def test_embed_far_offsets(gpu):
+    """Tables of more than 2^31 elements: the last rows of the last replica, and a far row's gradient."""
+    torch, pb = gpu
+    vocab, dim = 1 << 20, 2100
+    table = torch.empty((1, vocab * dim), dtype=torch.bfloat16, device="cuda")
+    table[0, -dim:] = 3.0
+    table[0, :dim] = 1.0
+    t = torch.tensor([[vocab - 1, 0, -1]], dtype=torch.int32, device="cuda")
+    out = torch.empty((1, 3, dim), dtype=torch.bfloat16, device="cuda")
+    pb.parle_k_embed_forward(pb.parle_embed_desc(1, 1, 1, 3, vocab, dim, vocab * dim, 2.0), table, t, out)
+    assert (out[0, 0] == 6).all() and (out[0, 1] == 2).all() and (out[0, 2] == 0).all()
+    del table
+    got = torch.full((1, vocab * dim), 5.0, device="cuda")
+    desc = pb.parle_embed_desc(1, 0, 1, 3, vocab, dim, vocab * dim, 0.5)
+    pb.parle_k_embed_backward(desc, t, out, scratch(torch, pb.parle_k_embed_scratch_bytes(desc)), got)
+    assert (got[0, -dim:] == 3).all() and (got[0, :dim] == 1).all()
+    assert int((got != 0).sum()) == 2 * dim
+
+
+# ---------------------------------------------------------------- 8 bits
+
+def _codes_reference(torch, v, rows_of_block):
+    """Codes and scale bytes of v [R, C] (float64, on the CPU) by the definition; the codes as bytes."""
+    R, C = v.shape
+    Rb, Cb = up(R, rows_of_block) // rows_of_block, up(C, 128) // 128
+    p = torch.zeros(Rb * rows_of_block, Cb * 128).double()
+    p[:R, :C] = v
+    fin = torch.where(p.isfinite(), p.abs(), torch.zeros_like(p)).reshape(Rb, rows_of_block, Cb, 128).amax((1, 3))
+    e = torch.zeros_like(fin)
+    for i in range(Rb):
+        for j in range(Cb):
+            if fin[i, j] > 0:
+                k = math.frexp(float(fin[i, j]) / 448.0)[1]        # fin / 448 < 2^k
+                while float(fin[i, j]) <= 448.0 * 2.0 ** (k - 1):
+                    k -= 1
+                while float(fin[i, j]) > 448.0 * 2.0 ** k:
+                    k += 1
+                e[i, j] = max(-127, k)
+    q = p / (2.0 ** e).repeat_interleave(rows_of_block, 0).repeat_interleave(128, 1)
+    q = torch.where(q.isfinite(), q, torch.full_like(q, math.nan))
+    codes = q.float().to(torch.float8_e4m3fn).view(torch.uint8)[:R]
+    codes = torch.where(q[:R].isnan(), torch.full_like(codes, 0x7F), codes)
+    s = torch.zeros(Rb, up(Cb, 4), dtype=torch.uint8)
+    s[:, :Cb] = (e + 127).to(torch.uint8)
+    out = torch.zeros(R, up(C, 16), dtype=torch.uint8)
+    out[:, :C] = codes[:, :C]
+    return out, s
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("n,rows,cols,ld", [(1, 1, 1, 1), (2, 3, 130, 131), (1, 129, 64, 64), (2, 257, 300, 300), (1, 128, 1025, 1030), (1, 640, 128, 128)])
+def test_quantize(gpu, dtype, block, n, rows, cols, ld):
+    torch, pb = gpu
+    stride = rows * ld + 3
+    g = torch.Generator().manual_seed(5)
+    spread = torch.exp(3 * torch.randn((n, stride), generator=g))
+    src = (torch.randn((n, stride), generator=g) * spread).to(dt(torch, dtype))
+    src[:, 0] = 448.0 * 2 ** 5                                       # the border of a scale
+    if rows > 2 and cols > 2:
+        v = src.reshape(-1)
+        v[ld], v[ld + 1], v[ld + 2] = math.inf, math.nan, 0.0
+    if rows >= 129:
+        src[0, :ld * 128] = 0.0                                      # a block of zeros
+        src[0, ld * 128] = 1e-38                                     # and a tiny one
+    K = lambda c: up(up(c, 128) // 128, 4)  # noqa: E731
+    make = lambda *s: torch.full(s, 0xEE, dtype=torch.uint8, device="cuda")  # noqa: E731
+    q, s = make(n, rows, up(cols, 16)), make(n, up(rows, block) // block, K(cols))
+    qt, st = make(n, cols, up(rows, 16)), make(n, up(cols, block) // block, K(rows))
+    dev = src.cuda()
+    desc = pb.parle_quant_desc(dtype, block, n, rows, cols, ld, stride)
+    pb.parle_k_fp8_quantize(desc, dev, q, s, qt, st)
+    only_q, only_s, only_qt, only_st = torch.zeros_like(q), torch.zeros_like(s), torch.zeros_like(qt), torch.zeros_like(st)
+    pb.parle_k_fp8_quantize(desc, dev, only_q, only_s, None, None)
+    pb.parle_k_fp8_quantize(desc, dev, None, None, only_qt, only_st)
+    for a, b in ((q, only_q), (s, only_s), (qt, only_qt), (st, only_st)):
+        assert torch.equal(a, b)
+    for a in range(n):
+        m = torch.as_strided(src[a].double(), (rows, cols), (ld, 1)).contiguous()
+        for got, want in zip((q[a], s[a], qt[a], st[a]), (*_codes_reference(torch, m, block), *_codes_reference(torch, m.t().contiguous(), block))):
+            got = got.cpu()
+            nan = (want & 0x7F) == 0x7F if want.shape[-1] >= 16 else torch.zeros_like(want, dtype=torch.bool)
+            assert torch.equal(torch.where(nan, got | 0x80, got), torch.where(nan, want | 0x80, want))
+
+
+def _random_codes(torch, seed, n, rows, depth, block):
+    """Codes of all finite values and scales near 1, and what they stand for in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randint(0, 256, (n, rows, up(depth, 16)), generator=g, dtype=torch.uint8)
+    q[(q & 0x7F) == 0x7F] = 0x31
+    q[..., depth:] = 0
+    rb, kb = up(rows, block) // block, up(depth, 128) // 128
+    s = torch.zeros(n, rb, up(kb, 4), dtype=torch.uint8)
+    s[..., :kb] = torch.randint(117, 131, (n, rb, kb), generator=g).to(torch.uint8)
+    e = (s[..., :kb].double() - 127).repeat_interleave(block, 1)[:, :rows].repeat_interleave(128, 2)[..., :depth]
+    return q, s, q.view(torch.float8_e4m3fn).double()[..., :depth] * 2.0 ** e
+
+
+def _largest_of_eight(torch, a, b):
+    """Sum over groups of eight of the contraction of the largest product's magnitude: [rows, cols] of a [rows, depth], b [cols, depth]."""
+    depth = up(a.shape[1], 8)
+    a, b = (torch.nn.functional.pad(t.abs(), (0, depth - t.shape[1])) for t in (a, b))
+    total = torch.zeros(a.shape[0], b.shape[0]).double()
+    for k in range(0, depth, 8):
+        most = torch.zeros_like(total)
+        for j in range(k, k + 8):
+            most = torch.maximum(most, a[:, j, None] * b[None, :, j])
+        total += most
+    return total
+
+
+@pytest.mark.parametrize("out_dtype,b_block,accumulate,bias", [(1, 128, 0, False), (0, 1, 0, True), (1, 1, 1, True), (0, 128, 1, False)])
+@pytest.mark.parametrize("n,rows,cols,depth", [(1, 1, 1, 1), (2, 1, 300, 129), (1, 4, 1000, 640), (3, 17, 130, 48), (1, 33, 64, 2100), (2, 129, 257, 100), (1, 300, 520, 1030),
+                                               (1, 64, 5, 16), (2, 16, 16, 4096), (1, 513, 1025, 144)])
+def test_fp8_matmul(gpu, out_dtype, b_block, accumulate, bias, n, rows, cols, depth):
+    torch, pb = gpu
+    a, sa, av = _random_codes(torch, 6, n, rows, depth, 1)
+    b, sb, bv = _random_codes(torch, 7, n, cols, depth, b_block)
+    ld = cols + 3
+    stride = rows * ld + 5
+    old = randn(torch, 8, n, stride, dtype=out_dtype, scale=100.0)
+    out = old.clone()
+    c = randn(torch, 9, n, cols) if bias else None
+    desc = pb.parle_fp8_desc(out_dtype, b_block, accumulate, n, rows, cols, depth, ld, stride)
+    pb.parle_k_fp8_matmul(desc, a.cuda(), sa.cuda(), b.cuda(), sb.cuda(), c, scratch(torch, pb.parle_k_fp8_scratch_bytes(desc)), out)
+    view = lambda t: torch.stack([torch.as_strided(t[i], (rows, cols), (ld, 1)) for i in range(n)])  # noqa: E731
+    want = torch.stack([av[i] @ bv[i].t() for i in range(n)])
+    mass = torch.stack([av[i].abs() @ bv[i].abs().t() for i in range(n)])
+    terms = depth
+    for extra in ([d64(c)[:, None, :].expand_as(want)] if bias else []) + ([d64(view(old))] if accumulate else []):
+        want, mass, terms = want + extra, mass + extra.abs(), terms + 1
+    # Every product is exact; a sum of `terms` in any order; the store.  For a bf16 result the matrix instruction cuts the products of
+    # eight neighbouring values to 13 places below the largest of them.
+    cut = torch.stack([_largest_of_eight(torch, av[i], bv[i]) for i in range(n)]) * 7 * 2.0 ** -13 if out_dtype else 0.0
+    within(view(out), want, mass * terms * U + cut + want.abs() * (HALF[1] + U if out_dtype else 0), "out")
+    outside = torch.ones(stride, dtype=torch.bool)
+    torch.as_strided(outside, (rows, cols), (ld, 1)).fill_(False)
+    assert torch.equal(out[:, outside.cuda()], old[:, outside.cuda()]), "columns or rows outside were written"
+
+
+def test_fp8_without_depth(gpu):
+    torch, pb = gpu
+    out = torch.full((1, 3, 5), 7.0, device="cuda")
+    c = randn(torch, 1, 1, 5)
+    desc = pb.parle_fp8_desc(0, 1, 0, 1, 3, 5, 0, 5, 15)
+    pb.parle_k_fp8_matmul(desc, None, None, None, None, c, scratch(torch, pb.parle_k_fp8_scratch_bytes(desc)), out)
+    assert torch.equal(out[0], c.expand(3, 5))
+
+
+def test_fp8_nan_stays_in_its_row(gpu):
+    """A NaN code in one row of a, a NaN scale in one row of b: only their row and column are NaN, at every kernel's sizes."""
+    torch, pb = gpu
+    for rows, cols, depth in [(4, 200, 300), (200, 200, 300), (600, 600, 256)]:
+        a, sa, _ = _random_codes(torch, 1, 1, rows, depth, 1)
+        b, sb, _ = _random_codes(torch, 2, 1, cols, depth, 1)
+        a[0, rows - 1, depth - 1] = 0x7F
+        sb[0, cols - 1, 0] = 0xFF
+        desc = pb.parle_fp8_desc(0, 1, 0, 1, rows, cols, depth, cols, rows * cols)
+        out = torch.zeros((1, rows, cols), device="cuda")
+        pb.parle_k_fp8_matmul(desc, a.cuda(), sa.cuda(), b.cuda(), sb.cuda(), None, scratch(torch, pb.parle_k_fp8_scratch_bytes(desc)), out)
+        want = torch.zeros(1, rows, cols, dtype=torch.bool)
+        want[0, rows - 1], want[0, :, cols - 1] = True, True
+        assert torch.equal(out.isnan().cpu(), want), (rows, cols)
+
+
+def test_linear_layer_gradients(gpu):
+    """y = x w^T through 8 bits: the three products of a training step against the formulas on the quantised operands, and the
+    derivative of <y, dy> along a direction of w by a difference."""
+    torch, pb = gpu
+    n, M, N, K = 2, 70, 90, 150
+    x, w, dy = randn(torch, 1, n, M, K, dtype=1), randn(torch, 2, n, N, K, scale=0.1), randn(torch, 3, n, M, N, dtype=1)
+
+    def both(t, code, block):
+        rows, cols = t.shape[1:]
+        k = lambda v: up(up(v, 128) // 128, 4)  # noqa: E731
+        make = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")  # noqa: E731
+        r = (make(n, rows, up(cols, 16)), make(n, up(rows, block) // block, k(cols)), make(n, cols, up(rows, 16)), make(n, up(cols, block) // block, k(rows)))
+        pb.parle_k_fp8_quantize(pb.parle_quant_desc(code, block, n, rows, cols, cols, rows * cols), t, *r)
+        return r
+
+    def value(q, s, depth, block):
+        e = (s.cpu()[..., :up(depth, 128) // 128].double() - 127).repeat_interleave(block, 1)[:, :q.shape[1]].repeat_interleave(128, 2)[..., :depth]
+        return q.cpu().view(torch.float8_e4m3fn).double()[..., :depth] * 2.0 ** e
+
+    def product(a, sa, b, sb, block, rows, cols, depth):
+        out = torch.empty((n, rows, cols), device="cuda")
+        desc = pb.parle_fp8_desc(0, block, 0, n, rows, cols, depth, cols, rows * cols)
+        pb.parle_k_fp8_matmul(desc, a, sa, b, sb, None, scratch(torch, pb.parle_k_fp8_scratch_bytes(desc)), out)
+        return d64(out)
+
+    x8, w8, dy8 = both(x, 1, 1), both(w, 0, 128), both(dy, 1, 1)
+    y = product(x8[0], x8[1], w8[0], w8[1], 128, M, N, K)
+    dx = product(dy8[0], dy8[1], w8[2], w8[3], 128, M, K, N)
+    dw = product(dy8[2], dy8[3], x8[2], x8[3], 1, N, K, M)
+    xv, wv, dyv = value(*x8[:2], K, 1), value(*w8[:2], K, 128), value(*dy8[:2], N, 1)
+    assert torch.equal(wv, value(*w8[2:], N, 128).transpose(1, 2)), "the transposed weights stand for other values"
+    xt, dyt = value(*x8[2:], M, 1).transpose(1, 2), value(*dy8[2:], M, 1).transpose(1, 2)
+    for got, l, r in ((y, xv, wv.transpose(1, 2)), (dx, dyv, wv), (dw, dyt.transpose(1, 2), xt)):
+        within(got, torch.matmul(l, r), torch.matmul(l.abs(), r.abs()) * l.shape[-1] * U, "product")
+    # <y(w + t v), dy> is linear in t: the difference is exact but for the 8-bit values of x and dy that dw uses (2^-4 of each)
+    v = torch.randn(n, N, K, generator=torch.Generator().manual_seed(4)).double()
+    X, DY = d64(x), d64(dy)
+    diff = (torch.matmul(X, (wv + v).transpose(1, 2)) * DY).sum((1, 2)) - (torch.matmul(X, (wv - v).transpose(1, 2)) * DY).sum((1, 2))
+    along = 2 * (dw * v).sum((1, 2))
+    mass = 2 * (torch.matmul(DY.abs().transpose(1, 2), X.abs()) * v.abs()).sum((1, 2))
+    assert ((diff - along).abs() <= mass * 2.2 * 2.0 ** -4).all()
+
+
+# ---------------------------------------------------------------- norm
+
+@pytest.mark.parametrize("dtype,w_dtype", [(0, 0), (1, 0), (1, 1), (0, 1)])
+@pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 3, 7), (1, 5, 64), (3, 17, 129), (2, 4, 513), (1, 6, 1000), (2, 3, 1025), (1, 2, 2049), (1, 3, 4104), (1, 2, 8192), (1, 2, 8193),
+                                        (1, 2, 16384), (1, 2, 20001)])
+def test_rmsnorm_forward(gpu, dtype, w_dtype, n, rows, dim):
+    torch, pb = gpu
+    eps = 1e-6
+    ws = dim + 3
+    x, resid, w = randn(torch, 1, n, rows, dim, dtype=dtype, scale=3.0), randn(torch, 2, n, rows, dim, dtype=dtype), randn(torch, 3, n, ws, dtype=w_dtype)
+    if rows > 1:
+        x[:, 1], resid[:, 1] = 0, 0                          # a row of zeros
+    kb = up(dim, 128) // 128
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    q = torch.full((n, rows, up(dim, 16)), 0xEE, dtype=torch.uint8, device="cuda")
+    s = torch.full((n, rows, up(kb, 4)), 0xEE, dtype=torch.uint8, device="cuda")
+    rstd = torch.empty((n, rows), device="cuda")
+    desc = pb.parle_norm_desc(dtype, w_dtype, n, rows, dim, ws, eps)
+    pb.parle_k_rmsnorm_forward(desc, x, resid, w, h, y, q, s, rstd)
+    total = d64(x) + d64(resid)
+    within(h, total, total.abs() * (U + (HALF[1] if dtype else 0)), "h")
+    f, e32 = d64(h), float(np.float32(eps))
+    r = (f.square().mean(-1) + e32) ** -0.5
+    # dim squares and sums, quotient, eps; half of that through the root, and root and quotient themselves
+    tr = ((dim + 3) / 2 + 3) * U
+    within(rstd, r, r * tr, "rstd")
+    wv = d64(w)[:, None, :dim]
+    want = f * r[..., None] * wv
+    ty = tr + 2 * U
+    within(y, want, want.abs() * (ty + (HALF[1] if dtype else 0)), "y")
+    # codes: within half a step of the value under the scale that they have, and the scale is the smallest that fits
+    sb = s.cpu()
+    scale = 2.0 ** (sb[..., :kb].double() - 127)
+    values = q.cpu().view(torch.float8_e4m3fn).double()
+    assert (q.cpu()[..., dim:] == 0).all() and (sb[..., kb:] == 0).all(), "padding"
+    wide = scale.repeat_interleave(128, -1)[..., :dim]
+    within(values[..., :dim] * wide, want, torch.maximum(want.abs() * 2.0 ** -4, wide * 2.0 ** -10) * (1 + ty) + want.abs() * ty, "codes")
+    padded = torch.zeros(n, rows, kb * 128).double()
+    padded[..., :dim] = want.abs()
+    most = padded.reshape(n, rows, kb, 128).amax(-1)
+    assert (most <= 448 * scale * (1 + ty)).all() and ((most > 224 * scale * (1 - ty)) | (most == 0)).all(), "scales"
+    assert (scale[most == 0] == 1).all()
+    # outputs that are left out, a residual that is left out
+    y2, q2, s2, h2 = torch.empty_like(y), torch.empty_like(q), torch.empty_like(s), torch.empty_like(h)
+    pb.parle_k_rmsnorm_forward(desc, h, None, w, None, y2, None, None, None)
+    assert torch.equal(y2, y)
+    pb.parle_k_rmsnorm_forward(desc, x, resid, w, None, None, q2, s2, None)
+    assert torch.equal(q2, q) and torch.equal(s2, s)
+    pb.parle_k_rmsnorm_forward(desc, x, resid, w, h2, y2, None, None, None)
+    assert torch.equal(h2, h) and torch.equal(y2, y)
+
+
+def test_rmsnorm_non_finite(gpu):
+    """NaN and infinities make NaN codes in their row and nowhere else; scales stay finite."""
+    torch, pb = gpu
+    x = randn(torch, 1, 1, 3, 256, dtype=1)
+    w = torch.ones((1, 256), device="cuda")
+    w[0, 5] = math.inf
+    x[0, 1, 7] = math.nan
+    q, s = torch.empty((1, 3, 256), dtype=torch.uint8, device="cuda"), torch.empty((1, 3, 4), dtype=torch.uint8, device="cuda")
+    pb.parle_k_rmsnorm_forward(pb.parle_norm_desc(1, 0, 1, 3, 256, 256, 1e-6), x, None, w, None, None, q, s, None)
+    nan = (q.cpu() & 0x7F) == 0x7F
+    assert nan[0, 1].all() and nan[0, 0].nonzero().tolist() == [[5]] and nan[0, 2].nonzero().tolist() == [[5]]
+    assert (s.cpu()[..., :2] != 0xFF).all()
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [(0, 0), (1, 0), (1, 1), (0, 1)])
+@pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 3, 7), (1, 50, 64), (3, 17, 129), (2, 40, 513), (1, 6, 1000), (2, 300, 1025), (1, 3, 4104), (1, 5, 8193), (1, 3, 20001), (2, 2000, 40)])
+def test_rmsnorm_backward(gpu, dtype, w_dtype, n, rows, dim):
+    torch, pb = gpu
+    ws = dim + 1
+    h, w, dout, dresid = (randn(torch, 1, n, rows, dim, dtype=dtype), randn(torch, 2, n, ws, dtype=w_dtype), randn(torch, 3, n, rows, dim, dtype=dtype),
+                          randn(torch, 4, n, rows, dim, dtype=dtype))
+    rstd = (d64(h).square().mean(-1) + 1e-6).rsqrt().float().cuda()
+    desc = pb.parle_norm_desc(dtype, w_dtype, n, rows, dim, ws, 1e-6)
+    sc = scratch(torch, pb.parle_k_rmsnorm_scratch_bytes(desc))
+    f, r, wv, d = d64(h), d64(rstd)[..., None], d64(w)[:, None, :dim], d64(dout)
+    g = d * wv
+    mean, mass = (g * f).mean(-1, keepdim=True), (g * f).abs().mean(-1, keepdim=True)
+    for add in (dresid, None):
+        dx, dw = torch.empty_like(h), torch.full((n, ws), 7.0, device="cuda")
+        pb.parle_k_rmsnorm_backward(desc, h, w, rstd, dout, add, sc, dx, dw)
+        e = d64(add) if add is not None else 0.0
+        want = r * (g - f * mean * r * r) + e
+        # the mean's sum: dim + 3 roundings; seven more on the way to dx
+        tol = (r ** 3 * f.abs() * mass * (dim + 10) + r * g.abs() * 6 + (e.abs() * 2 if add is not None else 0)) * U + want.abs() * (U + (HALF[1] if dtype else 0))
+        within(dx, want, tol, "dx")
+        terms = d * f * r
+        within(dw[:, :dim], terms.sum(1), terms.abs().sum(1) * (rows + 3) * U, "dw")
+        assert (dw[:, dim:] == 7).all()
+
+
+def test_rmsnorm_gradient_by_differences(gpu):
+    """<y, dy> + <h, dr> along directions of x and w: the kernel's gradients against central differences of the formula in 64 bits."""
+    torch, pb = gpu
+    n, rows, dim, eps = 2, 5, 100, 1e-6
+    h, w, dout, dresid = randn(torch, 1, n, rows, dim), randn(torch, 2, n, dim), randn(torch, 3, n, rows, dim), randn(torch, 4, n, rows, dim)
+    rstd, y, h1 = torch.empty((n, rows), device="cuda"), torch.empty_like(h), torch.empty_like(h)
+    desc = pb.parle_norm_desc(0, 0, n, rows, dim, dim, eps)
+    pb.parle_k_rmsnorm_forward(desc, h, None, w, h1, y, None, None, rstd)
+    assert torch.equal(h, h1)
+    dx, dw = torch.empty_like(h), torch.empty_like(w)
+    pb.parle_k_rmsnorm_backward(desc, h, w, rstd, dout, dresid, scratch(torch, pb.parle_k_rmsnorm_scratch_bytes(desc)), dx, dw)
+    H, W, D, R = d64(h), d64(w), d64(dout), d64(dresid)
+    loss = lambda hh, ww: (hh / (hh.square().mean(-1, keepdim=True) + eps).sqrt() * ww[:, None] * D).sum() + (hh * R).sum()  # noqa: E731
+    g = torch.Generator().manual_seed(5)
+    vh, vw, step = torch.randn(H.shape, generator=g).double(), torch.randn(W.shape, generator=g).double(), 1e-5
+    diff = (loss(H + step * vh, W + step * vw) - loss(H - step * vh, W - step * vw)) / (2 * step)
+    along = (d64(dx) * vh).sum() + (d64(dw) * vw).sum()
+    mass = (d64(dx) * vh).abs().sum() + (d64(dw) * vw).abs().sum()
+    # fp32 gradients: about a hundred roundings of terms of this size; the difference: step^2 of third derivatives of order one
+    assert abs(diff - along) <= mass * (dim + 10) * U + 1e-7 * mass
+
+
+def test_rmsnorm_without_rows(gpu):
+    torch, pb = gpu
+    dw = torch.full((2, 9), 7.0, device="cuda")
+    pb.parle_k_rmsnorm_backward(pb.parle_norm_desc(1, 0, 2, 0, 8, 9, 1e-6), None, None, None, None, None, None, None, dw)
+    assert (dw[:, :8] == 0).all() and (dw[:, 8] == 7).all()
+
+
+# ---------------------------------------------------------------- log probabilities
+
+def _logprob_reference(torch, x, label, top):
+    """x [R, C] float64."""
+    R, C = x.shape
+    m = x.amax(-1)
+    empty = m == -math.inf
+    shift = torch.where(empty, torch.zeros_like(m), m)[:, None]
+    z = torch.exp(x - shift).sum(-1)
+    lse = torch.where(empty, m, m + torch.log(z))
+    lp = torch.where(empty[:, None], x, (x - shift) - torch.log(z)[:, None])     # not x - lse: a row of the lowest value only has lse = that
+    p = torch.exp(lp)
+    H = -torch.where(p > 0, p * lp, torch.zeros_like(p)).sum(-1)
+    inside = (label >= 0) & (label < C)
+    logp = torch.where(inside, lp.gather(-1, label.clamp(0, C - 1).long()[:, None])[:, 0], torch.zeros(R).double())
+    ids, alt = np.full((R, top), -1, np.int32), np.full((R, top), -np.inf)
+    for i in range(R):
+        v = x[i].numpy()
+        order = np.lexsort((np.arange(C), -v))[:top]
+        order = order[v[order] > -np.inf]
+        ids[i, :len(order)], alt[i, :len(order)] = order, lp[i].numpy()[order]
+    return lse, H, logp, torch.as_tensor(ids), torch.as_tensor(alt)
+
+
+def _logits(torch, kind, n, rows, classes, ld, dtype):
+    x = randn(torch, 11, n, rows, ld, scale=3.0).cpu()
+    if kind == "masked":
+        x[..., ::3] = -math.inf
+        x[:, 0] = -math.inf
+        if rows > 1:
+            x[:, 1, 1:] = torch.finfo(dt(torch, dtype)).min
+        if rows > 2:
+            x[:, 2] = torch.finfo(dt(torch, dtype)).min
+        if rows > 3:
+            x[:, 3, 5:] = -math.inf                           # fewer classes than alternatives
+    elif kind == "ties":
+        x = x.round()
+        x[:, 0] = 0.0
+        x[..., ::2] *= 0.0                                    # +0 and -0
+    elif kind == "large":
+        x = x * 1000
+    elif kind == "steps":                                     # the best of a row all in one thread's vectors
+        x = torch.where((torch.arange(ld) // 8) % 256 == 3, 50.0 + torch.arange(ld) * 0.01, x)
+    return x.to(dt(torch, dtype))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,rows,classes,top,pad,kind", [
+    (1, 1, 1, 1, 0, "normal"), (2, 3, 7, 2, 1, "normal"), (1, 4, 100, 64, 3, "masked"), (2, 5, 2049, 5, 0, "ties"), (1, 3, 5000, 20, 1, "masked"), (1, 2, 50001, 20, 0, "ties"),
+    (1, 600, 300, 3, 0, "masked"), (2, 300, 2500, 1, 5, "normal"), (1, 520, 4100, 10, 1, "ties"), (1, 4, 128000, 20, 0, "large"), (1, 515, 9000, 0, 0, "normal"), (1, 1, 40000, 0, 0, "normal"),
+    (1, 2, 40000, 64, 0, "steps"), (1, 512, 70000, 64, 0, "steps")])
+def test_logprob_forward(gpu, dtype, n, rows, classes, top, pad, kind):
+    torch, pb = gpu
+    ld = classes + pad
+    x = _logits(torch, kind, n, rows, classes, ld, dtype)
+    label = torch.randint(-1, classes + 1, (n, rows), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    desc = pb.parle_logprob_desc(dtype, n, rows, classes, top, ld)
+    new = lambda *s, **k: torch.full(s, 3, device="cuda", **k)  # noqa: E731
+    logp, ent, lse = (new(n, rows, dtype=torch.float32) for _ in range(3))
+    ids, alt = (new(n, rows, top, dtype=torch.int32), new(n, rows, top, dtype=torch.float32)) if top else (None, None)
+    sc = scratch(torch, pb.parle_k_logprob_scratch_bytes(desc))
+    pb.parle_k_logprob_forward(desc, x.cuda(), label.cuda(), sc, logp, ent, lse, ids, alt)
+    if rows > 100:                                            # the reference is slow: some rows of many
+        pick = torch.cat([torch.arange(6), torch.arange(rows - 4, rows)])
+    else:
+        pick = torch.arange(rows)
+    flat = x[:, pick, :classes].double().reshape(-1, classes)
+    some = lambda t: t[:, pick.to(t.device)].reshape(-1, *t.shape[2:])  # noqa: E731
+    wl, wh, wp, wi, wa = _logprob_reference(torch, flat, some(label), top)
+    # A term's way through the sums: a thread adds classes / 256 of them (at least 8, a vector), and some thirty roundings join lanes,
+    # wavefronts and parts; its exponential has the difference's and the product's rounding (|d| of them) times e^d, at most 1.
+    chain = (classes / 256 + 48) * U
+    tl = wl.abs().nan_to_num(posinf=0.0, neginf=0.0) * 2 * U + chain
+    within(some(lse), wl, tl, "lse")
+    within(some(logp), wp, torch.where(wp == -math.inf, torch.zeros_like(tl), tl + wp.abs().nan_to_num(neginf=0.0) * U), "logp")
+    # log z and t / z: t has the terms' chain, |t| / z is at most entropy + log z
+    within(some(ent), wh, (2 * (wh.abs() + math.log(classes)) + 2) * chain, "entropy")
+    if top:
+        assert torch.equal(some(ids).cpu(), wi), "alternatives"
+        within(some(alt), wa, torch.where(wa == -math.inf, torch.zeros(1).double(), tl[:, None] + wa.abs().nan_to_num(neginf=0.0) * U), "top_logp")
+    again = [torch.empty_like(t) for t in (logp, ent, lse)]
+    pb.parle_k_logprob_forward(desc, x.cuda(), label.cuda(), sc, *again, ids, alt)
+    assert all(torch.equal(a, b) for a, b in zip(again, (logp, ent, lse))), "two calls differ"
+    pb.parle_k_logprob_forward(desc, x.cuda(), None, sc, None, None, again[2], ids, alt)
+    assert torch.equal(again[2], lse)
+
+
+def test_logprob_non_finite(gpu):
+    torch, pb = gpu
+    for rows in (3, 600):
+        x = randn(torch, 1, 1, rows, 5000)
+        x[0, 1, 77] = math.nan
+        x[0, 2, 4999] = math.inf
+        out = [torch.zeros((1, rows), device="cuda") for _ in range(3)]
+        desc = pb.parle_logprob_desc(0, 1, rows, 5000, 0, 5000)
+        label = torch.zeros((1, rows), dtype=torch.int32, device="cuda")
+        pb.parle_k_logprob_forward(desc, x, label, scratch(torch, pb.parle_k_logprob_scratch_bytes(desc)), *out, None, None)
+        for t in out:
+            assert t.isnan().nonzero().tolist() == [[0, 1], [0, 2]]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n,rows,classes,pad,kind", [(1, 1, 1, 0, "normal"), (2, 5, 7, 2, "masked"), (1, 9, 2049, 1, "masked"), (2, 4, 5001, 0, "large"), (1, 300, 130, 3, "ties")])
+def test_logprob_backward(gpu, dtype, n, rows, classes, pad, kind):
+    torch, pb = gpu
+    ld = classes + pad
+    x = _logits(torch, kind, n, rows, classes, ld, dtype)
+    label = torch.randint(-1, classes + 1, (n, rows), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    lse, H, _, _, _ = _logprob_reference(torch, x[..., :classes].double().reshape(-1, classes), label.reshape(-1), 0)
+    lse32, H32 = lse.float(), H.float()
+    dl, dh = randn(torch, 2, n, rows), randn(torch, 3, n, rows)
+    desc = pb.parle_logprob_desc(dtype, n, rows, classes, 0, ld)
+    xv, gl, ge = x[..., :classes].double().reshape(-1, classes), d64(dl).reshape(-1, 1), d64(dh).reshape(-1, 1)
+    lab = label.reshape(-1, 1)
+    gl = gl * ((lab >= 0) & (lab < classes))
+    empty = (lse32 == -math.inf)[:, None]
+    lp = xv - torch.where(empty[:, 0], torch.zeros_like(lse), lse32.double())[:, None]
+    p = torch.exp(lp)
+    hot = torch.zeros_like(p).scatter_(1, lab.clamp(0, classes - 1).long(), 1.0)
+    for entropy in (True, False):
+        out = torch.full((n, rows, ld), 7.0, dtype=dt(torch, dtype), device="cuda")
+        pb.parle_k_logprob_backward(desc, x.cuda(), label.cuda(), lse32.cuda(), H32.cuda() if entropy else None, dl, dh if entropy else None, out)
+        e = ge if entropy else torch.zeros_like(ge)
+        inner = torch.where(p > 0, lp + H32.double()[:, None], torch.zeros_like(p))
+        want = torch.where(empty, torch.zeros_like(p), gl * (hot - p) - e * p * inner)
+        # p carries |lp| + 3 roundings, the bracket four more; p below 2^-126 counts as 0
+        mass = p * (gl.abs() + e.abs() * (lp.abs().nan_to_num(posinf=0.0) + H32.double()[:, None]))
+        tol = mass.nan_to_num() * (lp.abs().nan_to_num(posinf=0.0) * 2 + 8) * U + (gl.abs() * hot) * U + want.abs() * (U + (HALF[1] if dtype else 0)) + 2.0 ** -126 * (gl.abs() + e.abs() * 200)
+        within(out[..., :classes].reshape(-1, classes), want, tol, "dlogits")
+        assert (out[..., classes:] == 7).all()
+
+
+def test_logprob_gradient_by_differences(gpu):
+    """sum of dlogp * logp + dentropy * entropy along a direction of the logits, by central differences of the formula in 64 bits."""
+    torch, pb = gpu
+    n, rows, C = 1, 6, 50
+    x, dl, dh = randn(torch, 1, n, rows, C), randn(torch, 2, n, rows), randn(torch, 3, n, rows)
+    label = torch.randint(0, C, (n, rows), generator=torch.Generator().manual_seed(1), dtype=torch.int32).cuda()
+    desc = pb.parle_logprob_desc(0, n, rows, C, 0, C)
+    logp, ent, lse = (torch.empty((n, rows), device="cuda") for _ in range(3))
+    pb.parle_k_logprob_forward(desc, x, label, scratch(torch, pb.parle_k_logprob_scratch_bytes(desc)), logp, ent, lse, None, None)
+    out = torch.empty_like(x)
+    pb.parle_k_logprob_backward(desc, x, label, lse, ent, dl, dh, out)
+
+    def loss(v):
+        lp = torch.log_softmax(v, -1)
+        return (lp.gather(-1, label.cpu().long()[..., None])[..., 0] * d64(dl)).sum() - ((lp.exp() * lp).sum(-1) * d64(dh)).sum()
+
+    v, step = torch.randn(x.shape, generator=torch.Generator().manual_seed(5)).double(), 1e-5
+    diff = (loss(d64(x) + step * v) - loss(d64(x) - step * v)) / (2 * step)
+    terms = d64(out) * v
+    assert abs(diff - terms.sum()) <= terms.abs().sum() * (100 * U + 1e-7)
+
+
+def test_logprob_far_offsets(gpu):
+    """Logits of more than 2^32 elements."""
+    torch, pb = gpu
+    rows, ld, C = 1100, 4_000_000, 1000
+    x = torch.empty((1, rows, ld), dtype=torch.bfloat16, device="cuda")
+    last = randn(torch, 1, C, dtype=1)
+    x[..., :C] = 0.0
+    x[0, rows - 1, :C] = last
+    desc = pb.parle_logprob_desc(1, 1, rows, C, 3, ld)
+    logp, ent, lse = (torch.empty((1, rows), device="cuda") for _ in range(3))
+    ids, alt = torch.empty((1, rows, 3), dtype=torch.int32, device="cuda"), torch.empty((1, rows, 3), device="cuda")
+    label = torch.full((1, rows), 5, dtype=torch.int32, device="cuda")
+    pb.parle_k_logprob_forward(desc, x, label, scratch(torch, pb.parle_k_logprob_scratch_bytes(desc)), logp, ent, lse, ids, alt)
+    wl, wh, wp, wi, wa = _logprob_reference(torch, d64(last)[None], torch.tensor([5]), 3)
+    within(lse[0, -1:], wl, wl.abs() * 2 * U + 60 * U, "lse")
+    assert torch.equal(ids[0, -1:].cpu(), wi)
+    dl = torch.ones_like(lse)
+    pb.parle_k_logprob_backward(desc, x, label, lse, None, dl, None, x)     # in place: an element is read by the thread that writes it
+    p = torch.softmax(d64(last), -1)
+    p = torch.nn.functional.one_hot(torch.tensor(5), C) - p
+    within(x[0, -1, :C], p, p.abs() * HALF[1] + 200 * U, "dlogits")
+
+
+# ---------------------------------------------------------------- streams and graphs
+
+def test_on_another_stream_and_in_a_graph(gpu):
+    """All operators in turn on a stream of their own, then captured and replayed with new inputs: the results of plain calls."""
+    torch, pb = gpu
+    n, T, V, D = 2, 130, 501, 96
+    table, w = randn(torch, 1, n, V * D), 1 + randn(torch, 2, n, D, scale=0.1)
+    kb = 4
+    tokens, labels = torch.zeros((n, T), dtype=torch.int32, device="cuda"), torch.zeros((n, T), dtype=torch.int32, device="cuda")
+    f = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    u8 = lambda *s: f(*s, dtype=torch.uint8)  # noqa: E731
+    x, h, rstd = f(n, T, D, dtype=torch.bfloat16), f(n, T, D, dtype=torch.bfloat16), f(n, T)
+    q, s = u8(n, T, D), u8(n, T, kb)
+    w8 = (u8(n, V, D), u8(n, up(V, 128) // 128, kb), u8(n, D, up(V, 16)), u8(n, 1, kb))
+    logits = f(n, T, V, dtype=torch.bfloat16)
+    logp, ent, lse, ids, alt = f(n, T), f(n, T), f(n, T), f(n, T, 3, dtype=torch.int32), f(n, T, 3)
+    dl, dlogits, g8 = f(n, T) - 1.0 / T, f(n, T, V, dtype=torch.bfloat16), (u8(n, T, up(V, 16)), u8(n, T, kb), u8(n, V, up(T, 16)), u8(n, V, kb))
+    dy, dx, dw, dtable = f(n, T, D, dtype=torch.bfloat16), f(n, T, D, dtype=torch.bfloat16), f(n, D), f(n, V * D)
+    ed, nd = pb.parle_embed_desc(1, 0, n, T, V, D, V * D, math.sqrt(D)), pb.parle_norm_desc(1, 0, n, T, D, D, 1e-6)
+    fd, bd = pb.parle_fp8_desc(1, 128, 0, n, T, V, D, V, T * V), pb.parle_fp8_desc(1, 128, 0, n, T, D, V, D, T * D)
+    ld = pb.parle_logprob_desc(1, n, T, V, 3, V)
+    sizes = [pb.parle_k_embed_scratch_bytes(ed), pb.parle_k_rmsnorm_scratch_bytes(nd), pb.parle_k_fp8_scratch_bytes(fd), pb.parle_k_fp8_scratch_bytes(bd),
+             pb.parle_k_logprob_scratch_bytes(ld)]
+    sc = scratch(torch, max(sizes))
+
+    def step(stream=None):
+        k = dict(stream=stream)
+        pb.parle_k_embed_forward(ed, table, tokens, x, **k)
+        pb.parle_k_rmsnorm_forward(nd, x, None, w, h, None, q, s, rstd, **k)
+        pb.parle_k_fp8_quantize(pb.parle_quant_desc(0, 128, n, V, D, D, V * D), table, *w8, **k)
+        pb.parle_k_fp8_matmul(fd, q, s, w8[0], w8[1], None, sc, logits, **k)
+        pb.parle_k_logprob_forward(ld, logits, labels, sc, logp, ent, lse, ids, alt, **k)
+        pb.parle_k_logprob_backward(ld, logits, labels, lse, ent, dl, None, dlogits, **k)
+        pb.parle_k_fp8_quantize(pb.parle_quant_desc(1, 1, n, T, V, V, T * V), dlogits, *g8, **k)
+        pb.parle_k_fp8_matmul(bd, g8[0], g8[1], w8[2], w8[3], None, sc, dy, **k)
+        pb.parle_k_rmsnorm_backward(nd, h, w, rstd, dy, None, sc, dx, dw, **k)
+        pb.parle_k_embed_backward(ed, tokens, dx, sc, dtable, **k)
+
+    outs = (x, h, rstd, q, s, logits, logp, ent, lse, ids, alt, dlogits, dy, dx, dw, dtable)
+
+    def inputs(seed):
+        g = torch.Generator().manual_seed(seed)
+        tokens.copy_(torch.randint(-1, V, (n, T), generator=g, dtype=torch.int32))
+        labels.copy_(torch.randint(-1, V, (n, T), generator=g, dtype=torch.int32))
+
+    def plain(seed):
+        inputs(seed)
+        step()
+        torch.cuda.synchronize()
+        r = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        return r
+
+    want = {seed: plain(seed) for seed in (1, 2, 3)}
+    assert all(t.float().isfinite().all() for t in want[1])
+    side = torch.cuda.Stream()
+    inputs(1)
+    torch.cuda.synchronize()
+    step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want[1]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (2, 3, 1, 2):
+        inputs(seed)
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want[seed])), seed
