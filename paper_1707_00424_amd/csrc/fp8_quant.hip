@@ -41,7 +41,7 @@ __global__ __launch_bounds__(kThreads) void k_fp8_quantize(const T *src, Args a)
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) m = max(m, finite_bits(v[j][i]));
-    most[j] = group_max<16>(m);
+    most[j] = row_max16(m);
     all = max(all, most[j]);
   }
   if (a.qt) {

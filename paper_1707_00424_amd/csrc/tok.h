@@ -96,18 +96,42 @@ __device__ __forceinline__ float scaled(float v, float inv) {
   return (__float_as_uint(v) & 0x7fffffffu) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : v * inv;
 }
 
-// Sum or maximum over groups of N consecutive lanes, in all of them.
-template <int N>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, PARLE_WAVE);
-  return v;
+// Sums and maxima over lanes, in all of them.  Neighbours, quads, halves and rows of 16 lanes exchange inside the vector unit; the
+// four rows of a wavefront meet as scalars.
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
-template <int N>
-__device__ __forceinline__ uint32_t group_max(uint32_t v) {
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, PARLE_WAVE));
-  return v;
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+  return __uint_as_float(from_lane<CTRL>(__float_as_uint(v)));
+}
+constexpr int kLaneXor1 = 0xb1, kLaneXor2 = 0x4e, kHalfMirror = 0x141, kRowMirror = 0x140;
+
+__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+
+__device__ __forceinline__ float row_sum16(float v) {
+  v += from_lane<kLaneXor1>(v);
+  v += from_lane<kLaneXor2>(v);
+  v += from_lane<kHalfMirror>(v);
+  return v + from_lane<kRowMirror>(v);
+}
+__device__ __forceinline__ float wave_sum_all(float v) {
+  v = row_sum16(v);
+  return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+__device__ __forceinline__ float wave_max_all(float v) {
+  v = fmaxf(v, from_lane<kLaneXor1>(v));
+  v = fmaxf(v, from_lane<kLaneXor2>(v));
+  v = fmaxf(v, from_lane<kHalfMirror>(v));
+  v = fmaxf(v, from_lane<kRowMirror>(v));
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+__device__ __forceinline__ uint32_t row_max16(uint32_t v) {
+  v = max(v, from_lane<kLaneXor1>(v));
+  v = max(v, from_lane<kLaneXor2>(v));
+  v = max(v, from_lane<kHalfMirror>(v));
+  return max(v, from_lane<kRowMirror>(v));
 }
 
 }  // namespace tok

@@ -2,17 +2,20 @@
 //
 // Forward: one pass over a row with the running maximum m and, relative to it, z = sum e^(x-m) and t = sum (x-m) e^(x-m):
 //   lse = m + log z,   entropy = log z - t / z,   logp = (x[label] - m) - log z.
-// A row belongs to one workgroup, or to several that each take a part of the classes where rows are few; a second, small kernel
+// Odd numbers of classes put rows anywhere; vectors are taken at 16-byte boundaries of memory, whatever the row's.  A row belongs to one workgroup, or to several that each take a part of the classes where rows are few; a second, small kernel
 // joins parts.
 //
 // Alternatives.  Every thread notes the largest value of its vectors and which vector holds it.  The `top`-th best of those
-// (value, vector) pairs over the threads is a bound: `top` elements at least are as good, so an element below it is none of the
-// best.  Only threads whose own best reaches the bound, about `top` of them, read their part again; what reaches the bound
-// goes to a list in LDS, out of which the best are taken by counting.  A list that overflows, where one thread holds
-// very many of the best, is given up for `top` searches over the whole part.
+// (value, vector) pairs over 64 groups of four threads is a bound: `top` elements at least are as good, so an element below it is none
+// of the best.  Only threads whose own best reaches the bound, about `top` of them, read their part again; vectors that reach the bound
+// go to a list in LDS, their elements that do to another, out of which the best are taken by counting.  A list that overflows, where
+// few threads hold very many of the best, is given up for `top` searches over the whole part.  (The code is kept short on purpose: a
+// row to a workgroup runs through it once, and a first version of 50 KiB took 20 us for four rows of 128000, nearly all of it waiting
+// for instructions.)
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "tok.h"
 
@@ -21,9 +24,10 @@ namespace {
 using namespace tok;
 
 constexpr int kThreads = 256, kWaves = kThreads / PARLE_WAVE;
-constexpr int kList = 1024;
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kGroup = kThreads * kVec;  // classes that a workgroup takes at a time
+constexpr int kList = 1024, kVectors = 512;  // candidates, and vectors that hold any
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kFloor = -1e30f;
+constexpr int kGroup = kThreads * kVec;  // classes of one vector per thread
 
 // Order of floats as unsigned integers; -0 counts as 0, so that equal values have equal keys.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -35,11 +39,11 @@ __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k
 __device__ __forceinline__ uint64_t pair_of(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (0xffffffffu - index); }
 __device__ __forceinline__ uint32_t index_of(uint64_t pair) { return 0xffffffffu - (uint32_t)pair; }
 
-// e^d for d <= 0: the hardware's power of two, 0 below 2^-126, next to a sum of at least 1.
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// The hardware's power of two: 0 below 2^-126, next to a sum of at least 1.
+__device__ __forceinline__ float exp2_of(float d) { return __builtin_amdgcn_exp2f(d); }
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2e); }
 
-// Running statistics of a set of values.  The difference x - m is taken before it is scaled to base 2: it is exact where it
-// counts, and a mask of the type's lowest value stays finite.
+// Statistics of a set of values: the largest, and relative to it z = sum e^(x-m), t = sum (x-m) e^(x-m).
 struct Stats {
   float m = -INFINITY, z = 0.f, t = 0.f;
   // Sums relative to a maximum that is now `to` >= m.
@@ -51,61 +55,52 @@ struct Stats {
   }
   __device__ __forceinline__ void join(Stats o) {
     const float most = fmaxf(m, o.m);
-    if (most == -INFINITY) {  // nothing in either, or NaN
-      z += o.z, t += o.t;
-      return;
-    }
+    if (most == -INFINITY) return;  // nothing in either
     raise(most), o.raise(most);
     z += o.z, t += o.t;
   }
 };
 
-__device__ __forceinline__ Stats wave_join(Stats s) {
-#pragma unroll
-  for (int o = 1; o < PARLE_WAVE; o <<= 1) {
-    Stats u;
-    u.m = __shfl_xor(s.m, o, PARLE_WAVE), u.z = __shfl_xor(s.z, o, PARLE_WAVE), u.t = __shfl_xor(s.t, o, PARLE_WAVE);
-    s.join(u);
+// The same while a thread reads its values, in base 2: an element costs one multiply-add, v log2 e - m2, in front of the
+// exponential.  m2 is m log2 e rounded; what the rounding took is put back once, at the end.  m starts at kFloor rather than -inf, so that
+// no difference of infinities arises: values below it count as nothing, and a part without larger ones is summed again by
+// slow_stats.
+struct Running {
+  float m = kFloor, m2 = kFloor * kLog2e, z = 0.f, t = 0.f;
+  __device__ __forceinline__ void raise(float to) {
+    const float to2 = to * kLog2e, d = m2 - to2, f = exp2_of(d);
+    t = f > 0.f ? (t + z * d) * f : 0.f;
+    z *= f;
+    m = to, m2 = to2;
   }
+  __device__ __forceinline__ void add(float v) {
+    const float d = __builtin_fmaf(v, kLog2e, -m2), e = exp2_of(d);
+    z += e;
+    t = __builtin_fmaf(e, fmaxf(d, kFloor), t);  // 0 where e is; a NaN comes along in e
+  }
+  __device__ __forceinline__ Stats result() const {
+    Stats s;
+    if (z == 0.f) return s;
+    const float r = __builtin_fmaf(m, kLog2e, -m2), f = exp2_of(-r);
+    s.m = m, s.z = z * f, s.t = (t - z * r) * f * kLn2;
+    return s;
+  }
+};
+
+__device__ __forceinline__ Stats wave_join(Stats s) {
+  const float most = wave_max_all(s.m);
+  if (most > s.m) s.raise(most);
+  s.z = wave_sum_all(s.z), s.t = wave_sum_all(s.t);
   return s;
 }
-
-struct Part {  // of one workgroup, where several share a row
-  float m, z, t, pad;
-};
-
-struct FwdArgs {
-  const int32_t *labels;
-  float *logp, *entropy, *lse;
-  int32_t *top_ids;
-  float *top_logp;
-  Part *parts;      // [rows][splits]
-  uint64_t *best;   // [rows][splits][top]
-  long long ld, rows;
-  int C, top, splits, span;  // span: classes of a part, a multiple of kGroup
-};
-
-struct Lds {
-  Part part[kWaves];
-  uint64_t best[kThreads];
-  uint64_t list[kList];
-  int count;
-  uint64_t bound;
-};
-
-// The `top` best of the `count` pairs in lds.list, in order, to out[0 .. top); those that are missing are 0.
-__device__ __forceinline__ void take_best(Lds &lds, int count, int top, uint64_t *out) {
-  for (int i = threadIdx.x; i < top; i += kThreads)
-    if (i >= count) out[i] = 0;
-  for (int i = threadIdx.x; i < count; i += kThreads) {
-    const uint64_t me = lds.list[i];
-    int better = 0;
-    for (int j = 0; j < count; ++j) better += lds.list[j] > me;
-    if (better < top) out[better] = me;
-  }
+// The best of the pairs of four neighbouring lanes.
+__device__ __forceinline__ uint64_t best_of_four(uint64_t v) {
+  const uint64_t a = (uint64_t)from_lane<kLaneXor1>((uint32_t)(v >> 32)) << 32 | from_lane<kLaneXor1>((uint32_t)v);
+  v = a > v ? a : v;
+  const uint64_t b = (uint64_t)from_lane<kLaneXor2>((uint32_t)(v >> 32)) << 32 | from_lane<kLaneXor2>((uint32_t)v);
+  return b > v ? b : v;
 }
-
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+__device__ __forceinline__ uint64_t wave_best(uint64_t v) {
 #pragma unroll
   for (int o = PARLE_WAVE / 2; o > 0; o >>= 1) {
     const uint64_t u = __shfl_xor((unsigned long long)v, o, PARLE_WAVE);
@@ -114,187 +109,372 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   return v;
 }
 
-// The results of a row from its joined statistics (natural units) and its best pairs.
-__device__ __forceinline__ void finish_row(const FwdArgs &a, long long row, Stats s, float label_value, int label, const uint64_t *best) {
-  const float lz = logf(s.z), lse = s.m > -INFINITY ? s.m + lz : s.z != s.z ? s.z : -INFINITY;
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = s.m > -INFINITY ? lz - s.t / s.z : s.z != s.z ? s.z : 0.f;
-    if (a.logp) a.logp[row] = label < 0 || label >= a.C ? 0.f : lse == -INFINITY ? -INFINITY : (label_value - s.m) - lz;
+struct Part {  // of one workgroup, where several share a row
+  float m, z, t, pad;
+};
+__device__ __forceinline__ Part part_of(const Stats &s) { return Part{s.m, s.z, s.t, 0.f}; }
+__device__ __forceinline__ Stats stats_of(const Part &p) {
+  Stats s;
+  s.m = p.m, s.z = p.z, s.t = p.t;
+  return s;
+}
+
+struct FwdArgs {
+  const int32_t *labels;
+  float *logp, *entropy, *lse;
+  int32_t *top_ids;
+  float *top_logp;
+  Part *parts;      // [rows][splits]
+  uint64_t *best;   // [rows][splits][top], in order
+  long long ld, rows;
+  int C, top, splits, span;  // span: classes of a part, a multiple of kGroup
+};
+
+struct Lds {
+  Part part[kWaves];
+  uint64_t best[kThreads];
+  uint64_t bound;
+  uint64_t list[kList];
+  int vector[kVectors];
+  int count, vectors;
+};
+
+// A row as vectors of eight elements at boundaries of eight elements in memory: its class 0 lies `off` elements behind the boundary that
+// `base` points to, and vector j holds elements j .. j + 7 of base, of which the row's are off .. end - 1.
+template <typename T>
+struct Row {
+  const T *base;
+  int off, end;
+  __device__ __forceinline__ Row(const T *x, int C) {
+    off = (int)((uintptr_t)x % (kVec * sizeof(T)) / sizeof(T));
+    base = x - off;
+    end = off + C;
   }
-  for (int i = threadIdx.x; i < a.top; i += kThreads) {
-    const uint64_t p = best[i];
+};
+struct RawBf16 {
+  us8 v;
+  __device__ __forceinline__ float at(int i) const { return bf16_to_f32(v[i]); }
+  __device__ __forceinline__ void clear(int i) { v[i] = 0xff80; }
+};
+struct RawF32 {
+  f4 a, b;
+  __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+  __device__ __forceinline__ void clear(int i) {
+    if (i < 4)
+      a[i] = -INFINITY;
+    else
+      b[i - 4] = -INFINITY;
+  }
+};
+__device__ __forceinline__ void read(const bf16_t *p, RawBf16 &x) { x.v = *(const us8 *)p; }
+__device__ __forceinline__ void read(const float *p, RawF32 &x) { x.a = *(const f4 *)p, x.b = *(const f4 *)(p + 4); }
+template <typename T>
+using Raw = std::conditional_t<sizeof(T) == 2, RawBf16, RawF32>;
+// Vector j; -inf in the places of elements that are not the row's.  A vector that holds one of them is read whole.
+template <typename T>
+__device__ __forceinline__ Raw<T> fetch(const Row<T> &r, int j, bool live) {
+  Raw<T> x;
+  if (live) {
+    read(r.base + j, x);
+    if (j < r.off || j + kVec > r.end) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (j + i < r.off || j + i >= r.end) x.clear(i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x.clear(i);
+  }
+  return x;
+}
+template <typename R>
+__device__ __forceinline__ float most_of(const R &x) {
+  float m = x.at(0);
+#pragma unroll
+  for (int i = 1; i < kVec; ++i) m = fmaxf(m, x.at(i));
+  return m;
+}
+__device__ __forceinline__ float logit_at(const bf16_t *x, int i) { return bf16_to_f32(x[i]); }
+__device__ __forceinline__ float logit_at(const float *x, int i) { return x[i]; }
+
+// Statistics of a part whose largest value lies below kFloor: differences are taken before they are scaled.  For classes c0 .. c1 - 1.
+template <typename T>
+__device__ __forceinline__ Stats slow_stats(const T *x, int c0, int c1, float m) {
+  Stats s;
+  s.m = m;
+#pragma unroll 1
+  for (int c = c0 + threadIdx.x; c < c1; c += kThreads) {
+    const float d = logit_at(x, c) - m, e = exp_of(d);
+    s.z += e;
+    s.t += e * fmaxf(d, kFloor);
+  }
+  return s;
+}
+
+// put(place, pair) for the `top` best of the `count` pairs in lds.list; 0 in the places of those that are missing.  Four neighbouring
+// threads count what is better than a pair, a quarter of the list each.
+template <typename Put>
+__device__ __forceinline__ void take_best(const Lds &lds, int count, int top, const Put &put) {
+  for (int i = threadIdx.x; i < top; i += kThreads)
+    if (i >= count) put(i, 0);
+#pragma unroll 1
+  for (int i = threadIdx.x >> 2; i < count; i += kThreads / 4) {
+    const uint64_t me = lds.list[i];
+    uint32_t better = 0;
+#pragma unroll 8
+    for (int j = threadIdx.x & 3; j < count; j += 4) better += lds.list[j] > me;
+    better += from_lane<kLaneXor1>(better);
+    better += from_lane<kLaneXor2>(better);
+    if ((threadIdx.x & 3) == 0 && (int)better < top) put(better, me);
+  }
+}
+
+// The pair of 64 (lds.best[0], [stride], ...) that has top - 1 better ones there, 0 where there are fewer; for every wavefront by itself.
+__device__ __forceinline__ uint64_t find_bound(const Lds &lds, int stride, int top) {
+  const int lane = threadIdx.x & (PARLE_WAVE - 1);
+  const uint64_t mine = lds.best[lane * stride];
+  int better = 0;
+#pragma unroll 16
+  for (int j = 0; j < PARLE_WAVE; ++j) better += lds.best[j * stride] > mine;
+  const uint64_t found = __ballot(better == top - 1 && mine);
+  if (found == 0) return 0;
+  const int at = __builtin_ctzll(found);
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(mine >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)mine, at);
+}
+// The same over the 256 pairs of lds.best, for every thread's own one `mine`; a barrier.
+__device__ __forceinline__ uint64_t find_bound_of_all(Lds &lds, uint64_t mine, int top) {
+  int better = 0;
+#pragma unroll 16
+  for (int j = 0; j < kThreads; ++j) better += lds.best[j] > mine;
+  if (better == top - 1 && mine) lds.bound = mine;
+  __syncthreads();
+  return lds.bound;
+}
+
+// The results of a row from its joined statistics.
+struct RowOut {
+  const FwdArgs &a;
+  long long row;
+  float m, lz;
+  __device__ __forceinline__ RowOut(const FwdArgs &args, long long at, const Stats &s) : a(args), row(at), m(s.m), lz(logf(s.z)) {}
+  __device__ __forceinline__ void stats(const Stats &s, int label, float label_value) const {
+    if (threadIdx.x != 0) return;
+    if (a.lse) a.lse[row] = m > -INFINITY ? m + lz : -INFINITY;
+    if (a.entropy) a.entropy[row] = m > -INFINITY ? lz - s.t / s.z : 0.f;
+    if (a.logp) a.logp[row] = label < 0 || label >= a.C ? 0.f : m > -INFINITY ? (label_value - m) - lz : -INFINITY;
+  }
+  __device__ __forceinline__ void operator()(int i, uint64_t p) const {
     a.top_ids[row * a.top + i] = p ? (int)index_of(p) : -1;
-    a.top_logp[row * a.top + i] = p ? (value_of((uint32_t)(p >> 32)) - s.m) - lz : -INFINITY;
+    a.top_logp[row * a.top + i] = p ? (value_of((uint32_t)(p >> 32)) - m) - lz : -INFINITY;
+  }
+};
+
+// Joins the wavefronts' statistics for everyone; one barrier.
+__device__ __forceinline__ Stats block_join(Lds &lds, Stats s) {
+  s = wave_join(s);
+  if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) lds.part[threadIdx.x / PARLE_WAVE] = part_of(s);
+  __syncthreads();
+  s = stats_of(lds.part[0]);
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) s.join(stats_of(lds.part[w]));
+  return s;
+}
+
+// The best of classes c0 .. c1 - 1 by `top` searches: put(0), put(1), ...
+template <typename T, typename Put>
+__device__ __forceinline__ void search_best(Lds &lds, const T *x, int c0, int c1, int top, const Put &put) {
+  uint64_t last = ~0ull;
+#pragma unroll 1
+  for (int n = 0; n < top; ++n) {
+    uint64_t b = 0;
+#pragma unroll 1
+    for (int c = c0 + threadIdx.x; c < c1; c += kThreads) {
+      const float v = logit_at(x, c);
+      const uint64_t p = v > -INFINITY ? pair_of(order_of(v), c) : 0;
+      if (p < last && p > b) b = p;
+    }
+    b = wave_best(b);
+    __syncthreads();
+    if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) lds.best[threadIdx.x / PARLE_WAVE] = b;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) b = lds.best[w] > b ? lds.best[w] : b;
+    if (threadIdx.x == 0) put(n, b);
+    last = b;
   }
 }
 
 // grid: (splits, rows)
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprob_fwd(const T *logits, FwdArgs a) {
+  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;  // vectors in flight per thread
   __shared__ Lds lds;
-  __shared__ uint64_t best[PARLE_LOGPROB_MAX_TOP];
-  const long long row = blockIdx.y + (long long)gridDim.y * blockIdx.z;
-  if (row >= a.rows) return;
-  const T *x = logits + row * a.ld;
-  const int c0 = blockIdx.x * a.span, c1 = min(c0 + a.span, a.C);
-  Stats s;
-  float most = -INFINITY;  // this thread's best, and the vector that holds it first
+  const long long row_at = blockIdx.y + (long long)gridDim.y * blockIdx.z;
+  if (row_at >= a.rows) return;
+  const T *x = logits + row_at * a.ld;
+  const Row<T> row(x, a.C);
+  const int j0 = blockIdx.x * a.span, j1 = min(j0 + a.span, row.end);
+  const int lane = threadIdx.x & (PARLE_WAVE - 1);
+  Running run;
+  float most = -INFINITY;  // this thread's largest, and the vector that holds it first
   int at = 0;
-  for (int c = c0 + threadIdx.x * kVec; c < c1; c += kGroup) {
-    float v[kVec];
-    load8(x + c, c1 - c, -INFINITY, v);
-    float vm = v[0];
+  for (int j = j0; j < j1; j += kAhead * kGroup) {
+    const int mine = j + threadIdx.x * kVec;
+    Raw<T> raw[kAhead];
 #pragma unroll
-    for (int i = 1; i < kVec; ++i) vm = fmaxf(vm, v[i]);
-    if (vm > most) most = vm, at = c;
-    if (vm > s.m) s.raise(vm);
-    if (s.m > -INFINITY) {
+    for (int u = 0; u < kAhead; ++u) raw[u] = fetch(row, mine + u * kGroup, mine + u * kGroup < j1);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const float d = v[i] - s.m, e = exp_of(d);
-        s.z += e;
-        s.t += e * fmaxf(d, -1e30f);  // 0 where e is; a NaN comes along in e
-      }
-    } else {
+    for (int u = 0; u < kAhead; ++u) {
+      const float vm = most_of(raw[u]);
+      if (vm > most) most = vm, at = mine + u * kGroup;
+    }
+    if (most > run.m) run.raise(most);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        if (v[i] != v[i]) s.z += v[i];
+    for (int u = 0; u < kAhead; ++u) {
+      if (u > 0 && j + u * kGroup >= j1) break;  // the same for all threads
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) run.add(raw[u].at(i));
     }
   }
   const uint64_t mine = most > -INFINITY ? pair_of(order_of(most), at) : 0;
-  s = wave_join(s);
-  const int wave = threadIdx.x / PARLE_WAVE, lane = threadIdx.x & (PARLE_WAVE - 1);
-  if (lane == 0) lds.part[wave] = Part{s.m, s.z, s.t, 0.f};
   if (TOP) {
+    const uint64_t four = best_of_four(mine);
+    if ((lane & 3) == 0) lds.best[threadIdx.x] = four;
+    if (threadIdx.x == 0) lds.count = lds.vectors = 0, lds.bound = 0;
+  }
+  Stats s = block_join(lds, run.result());
+  const int c0 = max(j0 - row.off, 0), c1 = j1 - row.off;  // the part's classes
+  if (!(s.m > kFloor)) {  // nothing larger anywhere in the part: the same for all threads
+    const float w = wave_max_all(most);
+    __syncthreads();
+    if (lane == 0) lds.part[threadIdx.x / PARLE_WAVE].pad = w;
+    __syncthreads();
+    float all = lds.part[0].pad;
+#pragma unroll
+    for (int w2 = 1; w2 < kWaves; ++w2) all = fmaxf(all, lds.part[w2].pad);
+    __syncthreads();
+    if (all > -INFINITY) s = block_join(lds, slow_stats(x, c0, c1, all));
+  }
+  const int label = a.logp && a.splits == 1 ? a.labels[row_at] : -1;
+  const long long slot = row_at * a.splits + blockIdx.x;
+  RowOut out(a, row_at, s);
+  if (a.splits == 1)
+    out.stats(s, label, label >= 0 && label < a.C ? logit_at(x, label) : 0.f);
+  else if (threadIdx.x == 0)
+    a.parts[slot] = part_of(s);
+  if (!TOP) return;
+  const auto put = [&](int i, uint64_t p) {
+    if (a.splits == 1)
+      out(i, p);
+    else
+      a.best[slot * a.top + i] = p;
+  };
+  uint64_t bound = find_bound(lds, 4, a.top);
+  if (bound == 0 && a.top > 1) {  // fewer groups than that hold anything, as behind a mask: over all threads
+    __syncthreads();
     lds.best[threadIdx.x] = mine;
-    if (threadIdx.x == 0) lds.count = 0, lds.bound = 0;
+    __syncthreads();
+    bound = find_bound_of_all(lds, mine, a.top);
+  }
+  // vectors that reach the bound, by the threads that know of one
+  if (mine && mine >= bound) {
+    for (int j = j0 + threadIdx.x * kVec; j < j1; j += kAhead * kGroup) {
+      Raw<T> raw[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) raw[u] = fetch(row, j + u * kGroup, j + u * kGroup < j1);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float vm = most_of(raw[u]);
+        if (vm > -INFINITY && pair_of(order_of(vm), j + u * kGroup) >= bound) {
+          const int n = atomicAdd(&lds.vectors, 1);
+          if (n < kVectors) lds.vector[n] = j + u * kGroup;
+        }
+      }
+    }
   }
   __syncthreads();
-  s.m = lds.part[0].m, s.z = lds.part[0].z, s.t = lds.part[0].t;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    Stats u;
-    u.m = lds.part[w].m, u.z = lds.part[w].z, u.t = lds.part[w].t;
-    s.join(u);
-  }
-  if (TOP) {
-    // the bound: the pair with top - 1 better ones (0, everything, where there are fewer)
-    int better = 0;
-    for (int j = 0; j < kThreads; ++j) better += lds.best[j] > mine;
-    if (better == a.top - 1 && mine) lds.bound = mine;
-    __syncthreads();
-    const uint64_t bound = lds.bound;
-    const uint32_t b_order = (uint32_t)(bound >> 32), b_at = index_of(bound);
-    if (mine && mine >= bound) {
-      for (int c = c0 + threadIdx.x * kVec; c < c1; c += kGroup) {
-        float v[kVec];
-        load8(x + c, c1 - c, -INFINITY, v);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          const uint32_t k = order_of(v[i]);
-          if (v[i] > -INFINITY && (k > b_order || (k == b_order && (uint32_t)c <= b_at))) {
-            const int slot = atomicAdd(&lds.count, 1);
-            if (slot < kList) lds.list[slot] = pair_of(k, c + i);
-          }
-        }
-      }
+  // their elements that do
+  const int vectors = lds.vectors;
+  const uint32_t b_order = (uint32_t)(bound >> 32), b_at = index_of(bound);
+  for (int e = threadIdx.x; e < min(vectors, kVectors) * kVec; e += kThreads) {
+    const int j = lds.vector[e / kVec], c = j + e % kVec - row.off;
+    if (c < 0 || c >= a.C) continue;
+    const float v = logit_at(x, c);
+    const uint32_t k = order_of(v);
+    if (v > -INFINITY && (k > b_order || (k == b_order && (uint32_t)j <= b_at))) {
+      const int n = atomicAdd(&lds.count, 1);
+      if (n < kList) lds.list[n] = pair_of(k, c);
     }
-    __syncthreads();
-    const int count = lds.count;
-    if (count <= kList) {
-      take_best(lds, count, a.top, best);
-    } else {
-      uint64_t last = ~0ull;
-      for (int j = 0; j < a.top; ++j) {
-        uint64_t b = 0;
-        for (int c = c0 + threadIdx.x * kVec; c < c1; c += kGroup) {
-          float v[kVec];
-          load8(x + c, c1 - c, -INFINITY, v);
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) {
-            const uint64_t p = v[i] > -INFINITY ? pair_of(order_of(v[i]), c + i) : 0;
-            if (p < last && p > b) b = p;
-          }
-        }
-        b = wave_max(b);
-        __syncthreads();
-        if (lane == 0) lds.best[wave] = b;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) b = lds.best[w] > b ? lds.best[w] : b;
-        if (threadIdx.x == 0) best[j] = b;
-        last = b;
-      }
-    }
-    __syncthreads();
   }
-  if (a.splits == 1) {
-    const int label = a.logp ? a.labels[row] : -1;
-    float lv = 0.f;
-    if (label >= 0 && label < a.C) {
-      const T raw = x[label];
-      lv = sizeof(T) == 2 ? bf16_to_f32((bf16_t)raw) : (float)raw;
-    }
-    finish_row(a, row, s, lv, label, best);
-  } else {
-    const long long slot = row * a.splits + blockIdx.x;
-    if (threadIdx.x == 0) a.parts[slot] = Part{s.m, s.z, s.t, 0.f};
-    if (TOP && (int)threadIdx.x < a.top) a.best[slot * a.top + threadIdx.x] = best[threadIdx.x];
-  }
+  __syncthreads();
+  const int count = lds.count;
+  if (vectors <= kVectors && count <= kList)
+    take_best(lds, count, a.top, put);
+  else
+    search_best(lds, x, c0, c1, a.top, put);
 }
 
-// Joins the parts of a row.
+// Joins the parts of a row.  Their lists are in order: a list whose pair `depth` reaches a bound has depth + 1 pairs that do, so the
+// ceil(top / (depth + 1))-th best of the lists' pairs at that depth bounds what can be among the best.  (depth: about half of the lists
+// are to reach it.)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_logprob_join(const T *logits, FwdArgs a) {
   __shared__ Lds lds;
   __shared__ uint64_t best[PARLE_LOGPROB_MAX_TOP];
   const long long row = blockIdx.x;
-  Stats s;
-  for (int i = threadIdx.x; i < a.splits; i += kThreads) {
-    const Part p = a.parts[row * a.splits + i];
-    Stats u;
-    u.m = p.m, u.z = p.z, u.t = p.t;
-    s.join(u);
-  }
-  s = wave_join(s);
-  const int wave = threadIdx.x / PARLE_WAVE;
-  if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) lds.part[wave] = Part{s.m, s.z, s.t, 0.f};
-  __syncthreads();
-  s.m = lds.part[0].m, s.z = lds.part[0].z, s.t = lds.part[0].t;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    Stats u;
-    u.m = lds.part[w].m, u.z = lds.part[w].z, u.t = lds.part[w].t;
-    s.join(u);
-  }
-  if (a.top > 0) {
-    // splits * top pairs, at most kList at a time: the best so far stay at the list's front
-    const uint64_t *from = a.best + row * a.splits * a.top;
-    const int all = a.splits * a.top, room = kList - a.top;
-    int held = 0;
-    for (int i0 = 0; i0 < all; i0 += room) {
-      const int more = min(room, all - i0);
-      if (threadIdx.x == 0) lds.count = held;
-      __syncthreads();
-      for (int i = threadIdx.x; i < held; i += kThreads) lds.list[i] = best[i];
-      for (int i = threadIdx.x; i < more; i += kThreads) {
-        const uint64_t p = from[i0 + i];
-        if (p) lds.list[atomicAdd(&lds.count, 1)] = p;
-      }
-      __syncthreads();
-      const int count = lds.count;
-      take_best(lds, count, a.top, best);
-      __syncthreads();
-      held = min(count, a.top);
-    }
-  }
   const int label = a.logp ? a.labels[row] : -1;
-  float lv = 0.f;
-  if (label >= 0 && label < a.C) {
-    const T raw = logits[row * a.ld + label];
-    lv = sizeof(T) == 2 ? bf16_to_f32((bf16_t)raw) : (float)raw;
+  const float label_value = label >= 0 && label < a.C ? logit_at(logits + row * a.ld, label) : 0.f;
+  // a thread's pairs, all at once (the first kHeld of them)
+  constexpr int kHeld = 8;
+  const uint64_t *from = a.best + row * a.splits * a.top;
+  const int all = a.splits * a.top;
+  uint64_t mine[kHeld];
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) mine[u] = (int)threadIdx.x + u * kThreads < all ? from[threadIdx.x + u * kThreads] : 0;
+  const int lists = min(a.splits, PARLE_WAVE), depth = a.top > 0 ? (a.top - 1) / max(1, lists / 2) : 0;
+  if (threadIdx.x < PARLE_WAVE) lds.best[threadIdx.x] = a.top > 0 && (int)threadIdx.x < lists ? from[threadIdx.x * a.top + depth] : 0;
+  if (threadIdx.x == 0) lds.count = 0;
+  Stats s;
+  for (int i = threadIdx.x; i < a.splits; i += kThreads) s.join(stats_of(a.parts[row * a.splits + i]));
+  s = block_join(lds, s);
+  const RowOut out(a, row, s);
+  out.stats(s, label, label_value);
+  if (a.top == 0) return;
+  const uint64_t bound = find_bound(lds, 1, a.top / (depth + 1) + (a.top % (depth + 1) != 0));
+  const auto keep = [&](uint64_t p) {
+    if (p && p >= bound) {
+      const int slot = atomicAdd(&lds.count, 1);
+      if (slot < kList) lds.list[slot] = p;
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) keep(mine[u]);
+  for (int i = threadIdx.x + kHeld * kThreads; i < all; i += kThreads) keep(from[i]);
+  __syncthreads();
+  const int count = lds.count;
+  if (count <= kList) {
+    take_best(lds, count, a.top, out);
+    return;
   }
-  finish_row(a, row, s, lv, label, best);
+  // too many: kList at a time, the best so far at the list's front
+  const int room = kList - a.top;
+  int held = 0;
+  for (int i0 = 0; i0 < all; i0 += room) {
+    const int more = min(room, all - i0);
+    __syncthreads();
+    if (threadIdx.x == 0) lds.count = held;
+    __syncthreads();
+    for (int i = threadIdx.x; i < held; i += kThreads) lds.list[i] = best[i];
+    for (int i = threadIdx.x; i < more; i += kThreads) {
+      const uint64_t p = from[i0 + i];
+      if (p) lds.list[atomicAdd(&lds.count, 1)] = p;
+    }
+    __syncthreads();
+    const int n = lds.count;
+    take_best(lds, n, a.top, [&](int i, uint64_t p) { best[i] = p; });
+    __syncthreads();
+    held = min(n, a.top);
+  }
+  for (int i = threadIdx.x; i < a.top; i += kThreads) out(i, best[i]);
 }
 
 // d = gl (onehot - p) - dH p (log p + H) with p = e^(x - lse).  grid: (parts of a row, rows)
@@ -333,10 +513,12 @@ struct Plan {
 Plan plan_of(const parle_logprob_desc &d) {
   Plan p;
   const long long rows = (long long)d.n * d.rows;
-  const int groups = ceil_div(d.classes, kGroup);
-  // A row to a workgroup where rows fill the chip; else parts of one group of classes at least.
+  const int groups = ceil_div(d.classes + kVec - 1, kGroup);  // a row may begin inside its first vector
+  // A row to a workgroup where rows fill the chip.  Fewer are split into parts of two vectors per thread at least: four rows of 128000
+  // classes with 20 alternatives take 7.2 + 5.7 us in 63 parts of one vector and 7.3 + 5.5 in 32 of two, but a part that a mask
+  // leaves a few hundred classes of finds its bound among too few threads, and takes 11 us for 8.
   const int want = rows >= 512 || rows == 0 ? 1 : ceil_div(1024, rows);
-  const int each = ceil_div(groups, std::min(want, groups));
+  const int each = std::max(ceil_div(groups, want), want > 1 ? 2 : 1);
   p.span = each * kGroup;
   p.splits = ceil_div(groups, each);
   p.parts = p.splits > 1 ? round_up(rows * p.splits * (long long)sizeof(Part), 256) : 0;

@@ -28,7 +28,7 @@ struct FwdArgs {
 // wavefront of the workgroup and call site).
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float *red) {
-  v = group_sum<(LANES < PARLE_WAVE ? LANES : PARLE_WAVE)>(v);
+  v = LANES == 16 ? row_sum16(v) : wave_sum_all(v);
   if (LANES > PARLE_WAVE) {
     constexpr int kWaves = LANES / PARLE_WAVE;
     if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) red[threadIdx.x / PARLE_WAVE] = v;
@@ -49,7 +49,7 @@ __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, int col
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) most = max(most, i < left ? finite_bits(y[i]) : 0u);
-  most = group_max<16>(most);
+  most = row_max16(most);
   const uint32_t sb = scale_byte(most);
   const float inv = scale_inverse(sb);
   if (col < a.pitch) {  // codes up to the row's pitch: zeros past D
