@@ -17,6 +17,7 @@ namespace {
 
 using igemm_dev::buffer_desc;
 using igemm_dev::dma16;
+using igemm_dev::dma4;
 using igemm_dev::f16v;
 using tok::ceil_div;
 using tok::round_up;
@@ -27,7 +28,6 @@ typedef int i4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef igemm_dev::bf8 bf8;
 
-constexpr int kThreads = 256;
 constexpr int kBlock = 128;            // values of a scale: one step of the contraction
 constexpr uint32_t kFar = 0x80000000u;  // an offset beyond every buffer: its 16 bytes arrive as zeros
 
@@ -39,25 +39,10 @@ struct Args {
   int M, N, K, pitch, s_pitch, steps, b_shift, accumulate;
 };
 
-template <typename T>
-__device__ __forceinline__ float out_value(const T *p);
-template <>
-__device__ __forceinline__ float out_value<float>(const float *p) {
-  return *p;
-}
-template <>
-__device__ __forceinline__ float out_value<bf16_t>(const bf16_t *p) {
-  return bf16_to_f32(*p);
-}
+__device__ __forceinline__ float value(const float *p) { return *p; }
+__device__ __forceinline__ float value(const bf16_t *p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t *p, float v) { *p = f32_to_bf16(v); }
-
-// 64 codes (one row's half step) for a lane: 32 bytes, two of the row's eight 16-byte chunks.  Chunk c of row r lies in slot c ^ (r & 7).
-__device__ __forceinline__ i8v fragment(const char *rows, int row, int chunk) {
-  const char *p = rows + row * kBlock;
-  const i4v lo = *(const i4v *)(p + ((chunk ^ (row & 7)) << 4)), hi = *(const i4v *)(p + (((chunk + 1) ^ (row & 7)) << 4));
-  return i8v{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-}
 
 // Eight codes (two dwords) times a power of two, as bf16.
 __device__ __forceinline__ bf8 eight_bf16(int lo, int hi, float scale) {
@@ -68,116 +53,326 @@ __device__ __forceinline__ bf8 eight_bf16(int lo, int hi, float scale) {
 // 2^(byte - 127) of a scale dword's lowest byte
 __device__ __forceinline__ float scale_value(int s) { return __uint_as_float(((uint32_t)s & 0xffu) << 23); }
 
-// A tile of BM x BN, WM x WN wavefronts, two steps of the contraction in LDS.
-template <typename TO, bool EXACT, int BM, int BN, int WM, int WN>
+// Results of 16 columns from n on, of which the two halves of a wavefront hold four in turn (registers 4 j .. 4 j + 7 of the product):
+// the halves exchange, and each lane has eight neighbouring columns, n + 8 half .. + 7.
+template <typename TO>
+__device__ __forceinline__ void store16(const Args &g, int rep, int m, int n, int half, const f16v *acc, int j, TO *row) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint((*acc)[4 * j + i]), __float_as_uint((*acc)[4 * j + 4 + i]), false, false);
+    v[i] = __uint_as_float(x[0]), v[4 + i] = __uint_as_float(x[1]);
+  }
+  n += 8 * half;
+  const int left = g.N - n;
+  if (m >= g.M || left <= 0) return;
+  if (g.bias) {
+    float c[8];
+    tok::load8(g.bias + (long long)rep * g.N + n, left, 0.f, c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += c[i];
+  }
+  if (g.accumulate) {
+    float o[8];
+    tok::load8(row + n, left, 0.f, o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += o[i];
+  }
+  tok::store8(row + n, left, v);
+}
+
+// Tile of a workgroup.  Workgroups go to the eight dies in turn, and each die has its own second-level cache: a die gets a
+// contiguous share of an order that walks strips of four rows of tiles, column by column, so that the 32 tiles that it works on at a
+// time are about four rows by eight columns.
+__device__ __forceinline__ void tile_of(int id, int rows, int cols, int &m, int &n) {
+  constexpr int kDies = 8, kStrip = 4;
+  const int all = rows * cols, share = all / kDies, more = all % kDies, die = id % kDies;
+  const int at = die * share + min(die, more) + id / kDies;
+  const int strip = at / (kStrip * cols), first = strip * kStrip, height = min(kStrip, rows - first), in = at - first * cols;
+  m = first + in % height, n = in / height;
+}
+
+// A tile of BM x BN, WM x WN wavefronts.  Two steps of the contraction (128 codes of every row) lie in LDS; a wavefront holds the
+// fragments of one step in registers, in two halves.  Once all have theirs of step s, half of its products are made, step s + 1 has
+// arrived, and one barrier says both: step s + 2 may be loaded over step s, and the fragments of s + 1 are read while the matrix units
+// work on the other half.
+template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int kStage = (BM + BN) * kBlock;
   constexpr int kLoads = (BM + BN) / 8 / kWaves;  // 1 KiB loads of a wavefront per step: 8 rows each
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the stages, then two groups of scales
   const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PARLE_WAVE);
-  const int rep = blockIdx.z, m0 = blockIdx.y * BM, n0 = blockIdx.x * BN;
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, ceil_div(g.M, BM), ceil_div(g.N, BN), tile_m, tile_n);
+  const int rep = blockIdx.z, m0 = tile_m * BM, n0 = tile_n * BN;
   const uint8_t *a0 = g.a + ((long long)rep * g.M + m0) * g.pitch, *b0 = g.b + ((long long)rep * g.N + n0) * g.pitch;
   const u4 a_desc = buffer_desc(a0, (uint32_t)min((long long)(g.M - m0) * g.pitch, (long long)BM * g.pitch));
   const u4 b_desc = buffer_desc(b0, (uint32_t)min((long long)(g.N - n0) * g.pitch, (long long)BN * g.pitch));
-  const int chunk = (lane & 7) ^ (lane >> 3);  // of its row, so that it lands in slot lane & 7
-  const uint32_t voff = (uint32_t)(lane >> 3) * (uint32_t)g.pitch + chunk * 16;
+  // Chunk c (16 codes) of row r lies in slot c ^ (r / 2 & 7) of the row's 128 bytes: a read of one chunk of 16 neighbouring rows then
+  // touches every bank once.  A load brings 8 rows; lane l fills slot l & 7 of row l / 8, in the lower or the upper half of 16 rows.
+  const int c_even = (lane & 7) ^ (lane >> 4), c_odd = c_even ^ 4;
+  const uint32_t voff = (uint32_t)(lane >> 3) * (uint32_t)g.pitch;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
 
-  auto load = [&](int step, int stage) {
-    const uint32_t v = step * kBlock + chunk * 16 < g.pitch ? voff : kFar;
+  // piece i of a wavefront's loads of a step
+  auto load = [&](int stage, int step, int i) {
+    const int k = step * kBlock, c = i & 1 ? c_odd : c_even;
+    const int piece = wave * kLoads + i;  // 8 rows of a, then of b
+    const bool is_a = piece < BM / 8;
+    const uint32_t rows = (is_a ? piece : piece - BM / 8) * 8;
+    dma16(__builtin_amdgcn_readfirstlane(lds0 + stage + piece * 1024), is_a ? a_desc : b_desc,
+          k + c * 16 < g.pitch ? voff + c * 16 : kFar, __builtin_amdgcn_readfirstlane(rows * (uint32_t)g.pitch + k));
+  };
+  // Scales of four steps, a dword per row of the tile: 64 rows for a wavefront's load, in turn.
+  constexpr int kRows = BM + BN, kScaleLoads = kRows / PARLE_WAVE;
+  const int b_rows = (g.N + (1 << g.b_shift) - 1) >> g.b_shift, b_row0 = n0 >> g.b_shift;
+  const u4 sa_desc = buffer_desc(g.a_scales + ((long long)rep * g.M + m0) * g.s_pitch, (uint32_t)(min(BM, g.M - m0) * g.s_pitch));
+  const u4 sb_desc =
+      buffer_desc(g.b_scales + ((long long)rep * b_rows + b_row0) * g.s_pitch, (uint32_t)(min(BN, b_rows - b_row0) * g.s_pitch));
+  auto load_scales = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int piece = wave * kLoads + i;  // 8 rows of a, then of b
-      const bool is_a = piece < BM / 8;
-      const uint32_t rows = (is_a ? piece : piece - BM / 8) * 8;
-      dma16(__builtin_amdgcn_readfirstlane(lds0 + stage * kStage + piece * 1024), is_a ? a_desc : b_desc, v,
-            __builtin_amdgcn_readfirstlane(rows * (uint32_t)g.pitch + step * kBlock));
+    for (int i = 0; i < (kScaleLoads + kWaves - 1) / kWaves; ++i) {
+      const int p = (i * kWaves + wave) % kScaleLoads;
+      const bool is_a = p < BM / PARLE_WAVE;
+      const int row = (is_a ? p : p - BM / PARLE_WAVE) * PARLE_WAVE + lane;
+      const int at = is_a ? row : ((n0 + row) >> g.b_shift) - b_row0;
+      dma4(__builtin_amdgcn_readfirstlane(lds0 + STAGES * kStage + (first & 4) * kRows + p * PARLE_WAVE * 4), is_a ? sa_desc : sb_desc,
+           first < g.s_pitch ? (uint32_t)(at * g.s_pitch + first) : kFar);
     }
   };
+  static_assert(kLoads % 2 == 0 && BM % 16 == 0, "the pieces of a wavefront alternate between halves of 16 rows");
 
   const int r = lane & 31, half = lane >> 5;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  const uint8_t *sa[TM], *sb[TN];  // scale rows; those past the end read the last row's and are not stored
-#pragma unroll
-  for (int t = 0; t < TM; ++t) sa[t] = g.a_scales + ((long long)rep * g.M + min(m0 + wm + t * 32 + r, g.M - 1)) * g.s_pitch;
-  const int b_rows = (g.N + (1 << g.b_shift) - 1) >> g.b_shift;
-#pragma unroll
-  for (int t = 0; t < TN; ++t)
-    sb[t] = g.b_scales + ((long long)rep * b_rows + (min(n0 + wn + t * 32 + r, g.N - 1) >> g.b_shift)) * g.s_pitch;
-
   f16v acc[TM][TN] = {};
-  int xa[TM], xb[TN];
-  if (g.steps > 0) load(0, 0);
-  for (int step = 0; step < g.steps; ++step) {
-    if ((step & 3) == 0) {
+  int xa[TM], xb[TN];  // scales of the step, in the lowest byte
+  auto take_scales = [&](int first) {
+    const int *p = (const int *)(lds + STAGES * kStage + (first & 4) * kRows) + r;
 #pragma unroll
-      for (int t = 0; t < TM; ++t) xa[t] = *(const int *)(sa[t] + step);
+    for (int t = 0; t < TM; ++t) xa[t] = p[wm + t * 32];
 #pragma unroll
-      for (int t = 0; t < TN; ++t) xb[t] = *(const int *)(sb[t] + step);
-    }
-    igemm_dev::wait_loads<0>();
-    __syncthreads();  // this step is in LDS, and everyone has read the step whose place the next one takes
-    if (step + 1 < g.steps) load(step + 1, (step + 1) & 1);
-    const char *as = lds + (step & 1) * kStage, *bs = as + BM * kBlock;
+    for (int t = 0; t < TN; ++t) xb[t] = p[BM + wn + t * 32];
+  };
+
+  // 64 codes of a row for two lanes: chunks 4 h + 2 half and the one behind it
+  i8v fa[2][TM], fb[2][TN];
+  const int slot = (half * 2) ^ ((r >> 1) & 7);
+  // fragment t of a half step: of a, then of b
+  auto read = [&](int stage, int h, int t) {
+    const char *q = lds + stage + (r + (t < TM ? wm + t * 32 : BM + wn + (t - TM) * 32)) * kBlock;
+    const int lo = (slot ^ (h * 4)) * 16, hi = lo ^ 16;
+    const i4v x = *(const i4v *)(q + lo), y = *(const i4v *)(q + hi);
+    (t < TM ? fa[h][t] : fb[h][t - TM]) = i8v{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  };
+  // the products of a half step; between(i) is issued behind product i
+  auto multiply = [&](int h, const auto &between) {
+    if (EXACT) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i8v fa[TM], fb[TN];
+      for (int j = 0; j < 4; ++j) {
+        bf8 ea[TM], eb[TN];
 #pragma unroll
-      for (int t = 0; t < TM; ++t) fa[t] = fragment(as, wm + t * 32 + r, h * 4 + half * 2);
+        for (int t = 0; t < TM; ++t) ea[t] = eight_bf16(fa[h][t][2 * j], fa[h][t][2 * j + 1], scale_value(xa[t]));
 #pragma unroll
-      for (int t = 0; t < TN; ++t) fb[t] = fragment(bs, wn + t * 32 + r, h * 4 + half * 2);
-      if (EXACT) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bf8 ea[TM], eb[TN];
-#pragma unroll
-          for (int t = 0; t < TM; ++t) ea[t] = eight_bf16(fa[t][2 * j], fa[t][2 * j + 1], scale_value(xa[t]));
-#pragma unroll
-          for (int t = 0; t < TN; ++t) eb[t] = eight_bf16(fb[t][2 * j], fb[t][2 * j + 1], scale_value(xb[t]));
-#pragma unroll
-          for (int tm = 0; tm < TM; ++tm)
-#pragma unroll
-            for (int tn = 0; tn < TN; ++tn) acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ea[tm], eb[tn], acc[tm][tn], 0, 0, 0);
-        }
-      } else {
+        for (int t = 0; t < TN; ++t) eb[t] = eight_bf16(fb[h][t][2 * j], fb[h][t][2 * j + 1], scale_value(xb[t]));
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
-          for (int tn = 0; tn < TN; ++tn)
-            acc[tm][tn] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[tm], fb[tn], acc[tm][tn], 0, 0, 0, xa[tm], 0, xb[tn]);
+          for (int tn = 0; tn < TN; ++tn) {
+            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eb[tn], ea[tm], acc[tm][tn], 0, 0, 0);
+            if (j == 0) between(tm * TN + tn);
+          }
       }
+    } else {
+#pragma unroll
+      for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn) {
+          acc[tm][tn] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[h][tn], fa[h][tm], acc[tm][tn], 0, 0, 0, xb[tn], 0, xa[tm]);
+          __builtin_amdgcn_sched_barrier(0);
+          between(tm * TN + tn);
+          __builtin_amdgcn_sched_barrier(0);
+        }
     }
+  };
+  constexpr int kProducts = TM * TN, kFrags = TM + TN;
+  // share i of n pieces of work among the products of a half step, done by `last` products
+  auto share = [&](int i, int n, int last, const auto &work) {
 #pragma unroll
-    for (int t = 0; t < TM; ++t) xa[t] = (unsigned)xa[t] >> 8;
-#pragma unroll
-    for (int t = 0; t < TN; ++t) xb[t] = (unsigned)xb[t] >> 8;
-  }
+    for (int w = 0; w < n; ++w)
+      if (w * last / n == i) work(w);
+  };
 
+  // Loads and reads past the last step bring zeros that nothing uses: the loop's body has no branch that the products could be moved
+  // across.
+  load_scales(0);
+#pragma unroll
+  for (int p = 0; p < STAGES; ++p)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(p * kStage, p, i);
+  igemm_dev::wait_loads<(STAGES - 1) * kLoads>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int t = 0; t < kFrags; ++t) read(0, 0, t);
+  int here = 0;  // the step's stage
+  for (int first = 0; first < g.steps; first += 4) {
+    take_scales(first);
+    load_scales(first + 4);  // over those of the group before, which everyone has taken
+    const int last = min(first + 4, g.steps);
+    for (int step = first; step < last; ++step) {
+      const int next = here == (STAGES - 1) * kStage ? 0 : here + kStage;
+      multiply(0, [&](int i) { share(i, kFrags, kProducts / 2, [&](int t) { read(here, 1, t); }); });
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(1, [&](int i) {
+        share(i, kFrags, kProducts, [&](int t) { read(next, 0, t); });
+        share(i, kLoads, kProducts, [&](int p) { load(here, step + STAGES, p); });
+      });
+      __builtin_amdgcn_sched_barrier(0);
+      here = next;
+#pragma unroll
+      for (int t = 0; t < TM; ++t) xa[t] = (unsigned)xa[t] >> 8;
+#pragma unroll
+      for (int t = 0; t < TN; ++t) xb[t] = (unsigned)xb[t] >> 8;
+    }
+  }
+  igemm_dev::wait_loads<0>();
+
+  // A lane has row m = its r of a 32 x 32 product, columns 8 j + 4 half .. + 3 in registers 4 j .. 4 j + 3.
   TO *out = (TO *)g.out + rep * g.out_rs;
 #pragma unroll
-  for (int tn = 0; tn < TN; ++tn) {
-    const int n = n0 + wn + tn * 32 + r;
-    if (n >= g.N) continue;
-    const float bias = g.bias ? g.bias[(long long)rep * g.N + n] : 0.f;
+  for (int tm = 0; tm < TM; ++tm) {
+    const int m = m0 + wm + tm * 32 + r;
+    TO *row = out + m * g.ld;
 #pragma unroll
-    for (int tm = 0; tm < TM; ++tm)
+    for (int tn = 0; tn < TN; ++tn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int m = m0 + wm + tm * 32 + 8 * (v >> 2) + 4 * half + (v & 3);
-        if (m < g.M) {
-          TO *p = out + m * g.ld + n;
-          put(p, acc[tm][tn][v] + bias + (g.accumulate ? out_value<TO>(p) : 0.f));
-        }
-      }
+      for (int j = 0; j < 4; j += 2) store16<TO>(g, rep, m, n0 + wn + tn * 32 + j * 8, half, &acc[tm][tn], j, row);
   }
 }
 
-template <typename TO>
-hipError_t run(hipStream_t st, const parle_fp8_desc &d, const Args &g) {
-  const dim3 grid(ceil_div(d.cols, 128), ceil_div(d.rows, 128), d.n);
-  k_fp8_tile<TO, sizeof(TO) == 4, 128, 128, 2, 2><<<grid, kThreads, 0, st>>>(g);
+// Up to 16 rows of a: what counts is reading b once, at the rate of memory.  A wavefront multiplies 16 rows of b with all of a over its
+// share of the contraction, straight from memory into fragments and with no barrier; SPLIT wavefronts of a workgroup share a group of 16
+// rows of b and add their parts in LDS, in order.
+constexpr int kRowsWaves = 8;
+
+template <typename TO, bool EXACT, int SPLIT>
+__global__ __launch_bounds__(kRowsWaves *PARLE_WAVE) void k_fp8_rows(Args g) {
+  constexpr int kAhead = 4;  // steps whose loads are on their way together
+  __shared__ f4 part[kRowsWaves][PARLE_WAVE];
+  const int lane = threadIdx.x & (PARLE_WAVE - 1), r = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PARLE_WAVE), share = wave % SPLIT;
+  const int rep = blockIdx.y, n0 = (blockIdx.x * (kRowsWaves / SPLIT) + wave / SPLIT) * 16;
+  const int b_rows = (g.N + (1 << g.b_shift) - 1) >> g.b_shift, n = min(n0 + r, g.N - 1);  // rows past the end are not stored
+  const uint8_t *b = g.b + ((long long)rep * g.N + n) * g.pitch, *sb = g.b_scales + ((long long)rep * b_rows + (n >> g.b_shift)) * g.s_pitch;
+  const long long m = (long long)rep * g.M + min(r, g.M - 1);
+  const uint8_t *a = g.a + m * g.pitch, *sa = g.a_scales + m * g.s_pitch;
+  // 32 of a step's 128 codes of a row: chunks `quarter` and `quarter` + 4, so that four lanes read 64 bytes side by side
+  const auto codes = [&](const uint8_t *p, int k) {
+    const int at = k + quarter * 16;
+    const i4v zero = {0, 0, 0, 0}, x = at < g.pitch ? *(const i4v *)(p + at) : zero, y = at + 64 < g.pitch ? *(const i4v *)(p + at + 64) : zero;
+    return i8v{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  };
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int each = (g.steps + SPLIT - 1) / SPLIT, last = min((share + 1) * each, g.steps);
+  for (int step = share * each; step < last; step += kAhead) {
+    i8v fb[kAhead], fa[kAhead];
+    int xb[kAhead], xa[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (step + u >= last) break;
+      fb[u] = codes(b, (step + u) * kBlock), xb[u] = sb[step + u];
+      fa[u] = codes(a, (step + u) * kBlock), xa[u] = sa[step + u];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (step + u >= last) break;
+      if (EXACT) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(fb[u][2 * j], fb[u][2 * j + 1], scale_value(xb[u])),
+                                                        eight_bf16(fa[u][2 * j], fa[u][2 * j + 1], scale_value(xa[u])), acc, 0, 0, 0);
+      } else {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, 0, 0, 0, xb[u], 0, xa[u]);
+      }
+    }
+  }
+  if (SPLIT > 1) {
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (share != 0) return;
+#pragma unroll
+    for (int w = 1; w < SPLIT; ++w) acc += part[wave + w][lane];
+  }
+  // a lane has row m = lane & 15 of a, columns 4 (lane / 16) .. + 3 of the group
+  if (r >= g.M) return;
+  TO *out = (TO *)g.out + rep * g.out_rs + r * g.ld;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = n0 + quarter * 4 + i;
+    if (col < g.N) put(out + col, acc[i] + (g.bias ? g.bias[(long long)rep * g.N + col] : 0.f) + (g.accumulate ? value(out + col) : 0.f));
+  }
+}
+
+template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
+hipError_t run_tile(hipStream_t st, const Args &g, int replicas) {
+  constexpr int kLds = (BM + BN) * (STAGES * kBlock + 2 * 4);
+  static const hipError_t lds_ok =
+      hipFuncSetAttribute((const void *)k_fp8_tile<TO, EXACT, BM, BN, WM, WN, STAGES>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (lds_ok != hipSuccess) return lds_ok;
+  const dim3 grid(ceil_div(g.N, BN) * ceil_div(g.M, BM), 1, replicas);
+  k_fp8_tile<TO, EXACT, BM, BN, WM, WN, STAGES><<<grid, WM * WN * PARLE_WAVE, kLds, st>>>(g);
   return hipGetLastError();
+}
+
+template <typename TO, int SPLIT>
+hipError_t run_rows(hipStream_t st, const Args &g, int replicas) {
+  const dim3 grid(ceil_div(g.N, 16 * (kRowsWaves / SPLIT)), replicas);
+  k_fp8_rows<TO, sizeof(TO) == 4, SPLIT><<<grid, kRowsWaves * PARLE_WAVE, 0, st>>>(g);
+  return hipGetLastError();
+}
+
+// What a tiling takes, in microseconds: the start and end of a tile, and a step of it with one or two tiles on a compute unit (two: 0
+// where one fills it).
+struct Tiling {
+  int bm, bn;
+  float start, one, two;
+  float cost(const Args &g, int replicas) const {
+    const long long tiles = (long long)ceil_div(g.M, bm) * ceil_div(g.N, bn) * replicas, each = (tiles + 255) / 256;
+    const float single = start + one * (float)g.steps;
+    return two == 0.f ? (float)each * single : (float)(each / 2) * (start + two * (float)g.steps) + (float)(each % 2) * single;
+  }
+};
+
+template <typename TO>
+hipError_t run(hipStream_t st, const Args &g, int replicas) {
+  constexpr bool kExact = sizeof(TO) == 4;
+#ifdef TILE
+  return run_tile<TO, kExact, TILE>(st, g, replicas);
+#else
+  if (g.M <= 16) {
+    // four steps at least for a wavefront, and no fewer wavefronts than eight for 16 rows of b
+    if (g.steps >= 32) return run_rows<TO, 8>(st, g, replicas);
+    if (g.steps >= 16) return run_rows<TO, 4>(st, g, replicas);
+    if (g.steps >= 8) return run_rows<TO, 2>(st, g, replicas);
+    return run_rows<TO, 1>(st, g, replicas);
+  }
+  const Tiling t[4] = {{256, 256, 5.5f, kExact ? 3.2f : 1.2f, 0.f},
+                       {128, 256, 5.5f, kExact ? 1.7f : 0.9f, 0.f},
+                       {128, 128, 4.f, kExact ? 1.f : 0.65f, kExact ? 1.5f : 1.2f},
+                       {64, 64, 3.f, kExact ? 0.4f : 0.25f, kExact ? 0.65f : 0.5f}};
+  int best = 0;
+  for (int i = 1; i < 4; ++i)
+    if (t[i].cost(g, replicas) < t[best].cost(g, replicas)) best = i;
+  if (best == 0) return run_tile<TO, kExact, 256, 256, 2, 4, 2>(st, g, replicas);
+  if (best == 1) return run_tile<TO, kExact, 128, 256, 2, 4, 3>(st, g, replicas);
+  if (best == 2) return run_tile<TO, kExact, 128, 128, 2, 2, 2>(st, g, replicas);
+  return run_tile<TO, kExact, 64, 64, 2, 2, 4>(st, g, replicas);
+#endif
 }
 
 }  // namespace
@@ -190,5 +385,5 @@ hipError_t launch_fp8_matmul(hipStream_t st, const parle_fp8_desc &d, const uint
   g.a = a, g.a_scales = a_scales, g.b = b, g.b_scales = b_scales, g.bias = bias, g.out = out, g.ld = d.ld_out, g.out_rs = d.out_stride;
   g.M = d.rows, g.N = d.cols, g.K = d.depth, g.pitch = (int)round_up(d.depth, 16), g.steps = ceil_div(d.depth, kBlock);
   g.s_pitch = (int)round_up(g.steps, 4), g.b_shift = d.b_block == 1 ? 0 : 7, g.accumulate = d.accumulate;
-  return d.out_dtype ? run<bf16_t>(st, d, g) : run<float>(st, d, g);
+  return d.out_dtype ? run<bf16_t>(st, g, d.n) : run<float>(st, g, d.n);
 }
