@@ -85,6 +85,22 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
   const int e = (int)(most >> 23) - 135 + ((most & 0x7fffffu) > 0x600000u);
   return most == 0 ? 127u : (uint32_t)(max(e, -127) + 127);
 }
+// Magnitudes that the plain conversions below do not take: NaN and infinities, and what would need a scale of 2^-127.
+__device__ __forceinline__ bool special_most(uint32_t most) { return most >= 0x7f800000u || (most != 0 && scale_byte(most) == 0); }
+// Two values divided by 2^(byte-127), as codes in the lower or the upper half of a dword; not for special ones.
+typedef short s2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf2_hw __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float scale_float(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ uint32_t codes4_of(float a, float b, float c, float d, float scale) {
+  s2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true));
+}
+__device__ __forceinline__ uint32_t codes4_of(uint32_t ab, uint32_t cd, float scale) {  // pairs in bf16
+  s2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf2_hw, ab), scale, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf2_hw, cd), scale, true));
+}
 // 2^-(byte-127): e is at most 120, so the result is a normal number.
 __device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 // Codes of four values that are already divided by their scale; infinity becomes NaN in front of the conversion.
