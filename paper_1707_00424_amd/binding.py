@@ -224,13 +224,23 @@ def parle_query_layout(cfg: parle_config):
 
 
 def _ptr(t):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
+
+
+_current_stream = None
 
 
 def _stream_handle(stream):
-    import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return C.c_void_p(s.cuda_stream)
+    global _current_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_stream is None:
+        import torch
+        torch.cuda.current_stream()         # initialises the device, or says why not
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        # without a Stream object around the handle a call costs 2 us less
+        _current_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _current_stream()
 
 
 def parle_k_inner_update(grad, x, y, vy, z, y_bf16, eta_inner, momentum, alpha, weight_decay, g, stream=None):
