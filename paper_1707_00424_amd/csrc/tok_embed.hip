@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_fwd(const TI *table, long lo
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / PARLE_WAVE;
 constexpr int kMostItems = 16, kTile = kSortThreads * kMostItems;  // tokens that one workgroup sorts
 constexpr int kDigitBits = 6, kDigits = 1 << kDigitBits;
-constexpr int kChunk = 32;  // sorted positions of one group of lanes
+constexpr int kChunk = 16;  // sorted positions of one group of lanes: their rows are on the way together
 
 // A stable sort of one tile by key, in LDS: thread t of wavefront w holds items w * 64 * ITEMS + 64 j + lane.
 // The rank of an item among equal digits is its rank in the wavefront's vector (from ballots) plus what earlier vectors and
@@ -213,8 +213,46 @@ struct SumArgs {
   float scale;
 };
 
-// A group of lanes sums one chunk for its columns.  grid: (chunks / groups per block, column slices, n)
+// Eight columns of a row of dout, as they came; `left` of them exist (EIGHTS: all).
 template <typename T>
+struct Rows;
+template <>
+struct Rows<bf16_t> {
+  us8 v;
+  template <bool EIGHTS>
+  __device__ __forceinline__ void load(const bf16_t *p, int left) {
+    if (EIGHTS || left >= kVec) {
+      v = *(const us8_any *)p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = p[min(i, left - 1)];
+    }
+  }
+  __device__ __forceinline__ void add(float (&acc)[kVec]) const {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) acc[i] += bf16_to_f32(v[i]);
+  }
+};
+template <>
+struct Rows<float> {
+  f4 a, b;
+  template <bool EIGHTS>
+  __device__ __forceinline__ void load(const float *p, int left) {
+    if (EIGHTS || left >= kVec) {
+      a = *(const f4_any *)p, b = *(const f4_any *)(p + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = p[min(i, left - 1)], b[i] = p[min(4 + i, left - 1)];
+    }
+  }
+  __device__ __forceinline__ void add(float (&acc)[kVec]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += a[i], acc[4 + i] += b[i];
+  }
+};
+
+// A group of lanes sums one chunk for its columns.  grid: (chunks / groups per block, column slices, n)
+template <typename T, bool EIGHTS>
 __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArgs a) {
   const int lanes = 1 << a.lane_shift, rep = blockIdx.z;
   const int chunk = blockIdx.x * (kThreads >> a.lane_shift) + (threadIdx.x >> a.lane_shift);
@@ -224,38 +262,47 @@ __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArg
   const T *src = dout + (long long)rep * a.T * a.D + col;
   float *table = a.dtable + rep * a.table_rs + col;
   float *part = a.part + ((long long)rep * a.chunks + chunk) * 2 * a.Dp + col;
-  const int first = chunk * kChunk, last = min(first + kChunk, a.T), left = a.D - col;
+  const int first = chunk * kChunk, count = min(kChunk, a.T - first), left = a.D - col;
+  // Sixteen keys and positions as vectors.  Past the last chunk's end they are what lies behind the lists in scratch, and are not used.
+  uint32_t k[kChunk + 1];
+  u4 at[kChunk / 4];
+#pragma unroll
+  for (int q = 0; q < kChunk / 4; ++q) {
+    const u4 v = *(const u4_any *)(keys + first + 4 * q);
+    at[q] = *(const u4_any *)(pos + first + 4 * q);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k[4 * q + j] = v[j];
+  }
+  k[kChunk] = first + kChunk < a.T ? keys[first + kChunk] : 0xffffffffu;
+  bool from_before = first > 0 && keys[first - 1] == k[0];
+#pragma unroll
+  for (int j = 0; j < kChunk; ++j)
+    if (j >= count) k[j] = 0xffffffffu;  // ends the run in front of it, and is none
+  Rows<T> v[kChunk];
+#pragma unroll
+  for (int j = 0; j < kChunk; ++j) {
+    const uint32_t row = k[j] < (uint32_t)a.V ? at[j / 4][j % 4] : 0;  // one that exists, and no branch
+    v[j].template load<EIGHTS>(src + (long long)row * a.D, left);
+  }
   float acc[kVec] = {};
-  bool from_before = first > 0 && keys[first - 1] == keys[first];
-  constexpr int kAhead = 8;
-  for (int i = first; i < last; i += kAhead) {
-    uint32_t k[kAhead + 1];
-    float v[kAhead][kVec];
 #pragma unroll
-    for (int j = 0; j <= kAhead; ++j) k[j] = i + j < a.T ? keys[i + j] : 0xffffffffu;
+  for (int j = 0; j < kChunk; ++j) {
+    if (k[j] >= (uint32_t)a.V) break;  // no later key is less
+    v[j].add(acc);
+    const bool ends = k[j] != k[j + 1];
+    if (ends || j + 1 == kChunk) {
+      if (ends && !from_before) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (i + j < last && k[j] < (uint32_t)a.V) load8(src + (long long)pos[i + j] * a.D, left, 0.f, v[j]);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (i + j >= last || k[j] >= (uint32_t)a.V) continue;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) acc[e] += v[j][e];
-      const bool ends = k[j] != k[j + 1];
-      if (ends || i + j + 1 == last) {
-        if (ends && !from_before) {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) acc[e] *= a.scale;
-          store8(table + (long long)k[j] * a.D, left, acc);
-        } else {
-          float *p = part + (from_before ? 0 : a.Dp);
-          *(f4 *)p = f4{acc[0], acc[1], acc[2], acc[3]};
-          *(f4 *)(p + 4) = f4{acc[4], acc[5], acc[6], acc[7]};
-        }
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) acc[e] = 0.f;
-        from_before = false;
+        for (int e = 0; e < kVec; ++e) acc[e] *= a.scale;
+        store8(table + (long long)k[j] * a.D, EIGHTS ? kVec : left, acc);
+      } else {
+        float *p = part + (from_before ? 0 : a.Dp);
+        *(f4 *)p = f4{acc[0], acc[1], acc[2], acc[3]};
+        *(f4 *)(p + 4) = f4{acc[4], acc[5], acc[6], acc[7]};
       }
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) acc[e] = 0.f;
+      from_before = false;
     }
   }
 }
@@ -391,10 +438,11 @@ hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int
   const int groups = ceil_div(d.dim, kVec);
   a.lane_shift = lane_shift_of(groups);
   const dim3 grid(ceil_div(s.chunks, kThreads >> a.lane_shift), ceil_div(groups, 1 << a.lane_shift), d.n);
+  const bool eights = d.dim % kVec == 0;
   if (d.dtype)
-    k_embed_chunks<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
+    (eights ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
   else
-    k_embed_chunks<<<grid, kThreads, 0, st>>>((const float *)dout, a);
+    (eights ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
   if (s.chunks > 1) k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
