@@ -61,6 +61,36 @@ __device__ __forceinline__ void store8(bf16_t *p, int count, const float (&v)[kV
   }
 }
 
+// Eight elements as they came, to be widened when they are used; zeros past `count`.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<bf16_t> {
+  us8 v;
+  __device__ __forceinline__ void load(const bf16_t *p, int count) {
+    if (count >= kVec) {
+      v = *(const us8_any *)p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = i < count ? p[i] : (bf16_t)0;
+    }
+  }
+  __device__ __forceinline__ float at(int i) const { return bf16_to_f32(v[i]); }
+};
+template <>
+struct Raw8<float> {
+  f4 a, b;
+  __device__ __forceinline__ void load(const float *p, int count) {
+    if (count >= kVec) {
+      a = *(const f4_any *)p, b = *(const f4_any *)(p + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = i < count ? p[i] : 0.f, b[i] = 4 + i < count ? p[4 + i] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+};
+
 // The value as it is stored in type T.
 template <typename T>
 __device__ __forceinline__ float stored(float v);

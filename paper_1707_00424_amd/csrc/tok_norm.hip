@@ -40,8 +40,9 @@ __device__ __forceinline__ float row_sum(float v, float *red) {
   return v;
 }
 
-// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  `tail`: the vector reaches past D.
-template <typename T, typename W>
+// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  SHORT: rows of one scale, whose four bytes (one and
+// three of padding) are a dword.
+template <bool SHORT, typename T, typename W>
 __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, int col, const float (&y)[kVec], T *yo) {
   const int left = a.D - col;
   if (yo && left > 0) store8(yo + row * a.D + col, left, y);
@@ -58,10 +59,14 @@ __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, int col
     for (int i = 0; i < kVec; ++i) c[i] = i < left ? scaled(y[i], inv) : 0.f;
     *(u2 *)(a.q + row * a.pitch + col) = u2{codes4(c[0], c[1], c[2], c[3]), codes4(c[4], c[5], c[6], c[7])};
   }
-  if ((threadIdx.x & 15) == 0 && (col >> 7) < a.s_pitch) a.scales[row * a.s_pitch + (col >> 7)] = left > 0 ? sb : 0;
+  if ((threadIdx.x & 15) != 0) return;
+  if (SHORT)  // one scale and the row's padding
+    *(uint32_t *)(a.scales + row * a.s_pitch) = sb;
+  else if ((col >> 7) < a.s_pitch)
+    a.scales[row * a.s_pitch + (col >> 7)] = left > 0 ? sb : 0;
 }
 
-// A row in the registers of LANES threads, four rows to a workgroup of 256 where LANES is a wavefront.
+// A row in the registers of LANES threads, sixteen or four rows to a workgroup of 256 where LANES is 16 or a wavefront.
 template <typename T, typename W, int LANES, int CH>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
   constexpr int kBlock = LANES < 256 ? 256 : LANES;
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const
     load8(w + col, a.D - col, 0.f, g);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) y[i] = v[c][i] * rs * g[i];
-    emit<T, W>(a, row, col, y, yo);
+    emit<LANES == 16, T, W>(a, row, col, y, yo);
   }
 }
 
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fwd_long(const T *x, const T *
     load8(w + col, a.D - col, 0.f, g);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = v[i] * rs * g[i];
-    emit<T, W>(a, row, col, v, yo);
+    emit<false, T, W>(a, row, col, v, yo);
   }
 }
 
@@ -176,24 +181,38 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_bwd(const
     const int col = (c * LANES + lane) * kVec;
     load8(a.w + rep * a.w_rs + col, a.D - col, 0.f, w[c]);
   }
-  int turn = 0;
-  for (int r = r0; r < r1; r += kGroups) {  // the same number of turns for every thread: row_sum has a barrier
-    const bool live = r + group < r1;
-    const long long row = (long long)rep * a.rows + (live ? r + group : r1 - 1);
-    float hv[CH][kVec], dv[CH][kVec], ev[CH][kVec];
+  // a row of this group: the loads of the next one are on their way while one is reduced
+  const auto row_of = [&](int r) { return (long long)rep * a.rows + min(r + group, r1 - 1); };
+  Raw8<T> hv[CH], dv[CH], ev[CH];
+  float next_rs;
+  const auto load = [&](long long row) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (c * LANES + lane) * kVec;
-      load8(h + row * a.D + col, a.D - col, 0.f, hv[c]);
-      load8(dout + row * a.D + col, a.D - col, 0.f, dv[c]);
-      if (dresid) load8(dresid + row * a.D + col, a.D - col, 0.f, ev[c]);
+      hv[c].load(h + row * a.D + col, a.D - col);
+      dv[c].load(dout + row * a.D + col, a.D - col);
+      if (dresid) ev[c].load(dresid + row * a.D + col, a.D - col);
     }
-    const float rs = a.rstd[row];
-    float sum = 0.f;
+    next_rs = a.rstd[row];
+  };
+  load(row_of(r0));
+  int turn = 0;
+  for (int r = r0; r < r1; r += kGroups) {  // the same number of turns for every thread: row_sum has a barrier
+    const bool live = r + group < r1;
+    const long long row = row_of(r);
+    const float rs = next_rs;
+    float sum = 0.f, g[CH][kVec], x[CH][kVec], e[CH][kVec];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += dv[c][i] * w[c][i] * hv[c][i];
+      for (int i = 0; i < kVec; ++i) {
+        x[c][i] = hv[c].at(i), e[c][i] = dresid ? ev[c].at(i) : 0.f;
+        const float d = dv[c].at(i);
+        if (live) dw[c][i] += d * (x[c][i] * rs);
+        g[c][i] = d * w[c][i];
+        sum += g[c][i] * x[c][i];
+      }
+    load(row_of(r + kGroups));
     sum = row_sum<LANES>(sum, red[turn]);
     turn ^= 1;  // the next row's sums meet elsewhere: one barrier a row
     const float k = sum / (float)a.D * rs * rs;
@@ -203,11 +222,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_bwd(const
         const int col = (c * LANES + lane) * kVec;
         float o[kVec];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          o[i] = rs * (dv[c][i] * w[c][i] - hv[c][i] * k);
-          if (dresid) o[i] += ev[c][i];
-          dw[c][i] += dv[c][i] * (hv[c][i] * rs);
-        }
+        for (int i = 0; i < kVec; ++i) o[i] = rs * (g[c][i] - x[c][i] * k) + e[c][i];
         if (col < a.D) store8(dx + row * a.D + col, a.D - col, o);
       }
     }
@@ -290,19 +305,20 @@ __global__ __launch_bounds__(256) void k_rmsnorm_dw_long(const T *h, const T *do
   *(f4 *)(out + 4) = f4{dw[4], dw[5], dw[6], dw[7]};
 }
 
-// dw = sum of the strips' parts: 32 columns x 8 parts of the strips per workgroup.
-__global__ __launch_bounds__(256) void k_rmsnorm_dw_join(const float *partial, int strips, int D, int Dp, float *dw, long long w_rs) {
-  __shared__ float red[8][32];
+// dw = sum of the strips' parts: 32 columns x kParts shares of the strips per workgroup.
+constexpr int kParts = 32;
+__global__ __launch_bounds__(32 * kParts) void k_rmsnorm_dw_join(const float *partial, int strips, int D, int Dp, float *dw, long long w_rs) {
+  __shared__ float red[kParts][32];
   const int c = threadIdx.x & 31, part = threadIdx.x >> 5, rep = blockIdx.y, col = blockIdx.x * 32 + c;
   float s = 0.f;
   if (col < D) {
 #pragma unroll 8
-    for (int i = part; i < strips; i += 8) s += partial[((long long)rep * strips + i) * Dp + col];
+    for (int i = part; i < strips; i += kParts) s += partial[((long long)rep * strips + i) * Dp + col];
   }
   red[part][c] = s;
   __syncthreads();
   if (part == 0 && col < D) {
-    for (int p = 1; p < 8; ++p) s += red[p][c];
+    for (int p = 1; p < kParts; ++p) s += red[p][c];
     dw[rep * w_rs + col] = s;
   }
 }
@@ -316,11 +332,13 @@ hipError_t fwd(hipStream_t st, const parle_norm_desc &d, const void *x, const vo
   a.w = (const W *)w, a.w_rs = d.w_stride, a.q = q, a.scales = scales, a.rstd = rstd;
   a.rows = d.rows, a.D = d.dim, a.pitch = (int)round_up(d.dim, 16), a.s_pitch = (int)round_up(ceil_div(d.dim, 128), 4), a.eps = d.eps;
   // whole scales and their padding: the threads of a row cover as much
-  const int D = q ? 128 * a.s_pitch : d.dim;
+  const int D = q && d.dim > 128 ? 128 * a.s_pitch : d.dim;
 #define PARLE_NORM(LANES, CH)                                                                                             \
   k_rmsnorm_fwd<T, W, LANES, CH><<<dim3(ceil_div(d.rows, (LANES < 256 ? 256 : LANES) / LANES), d.n), LANES < 256 ? 256 : LANES, \
                                    0, st>>>((const T *)x, (const T *)resid, (T *)h, (T *)y, a)
-  if (D <= 64 * kVec)
+  if (D <= 16 * kVec)
+    PARLE_NORM(16, 1);
+  else if (D <= 64 * kVec)
     PARLE_NORM(64, 1);
   else if (D <= 64 * kVec * 2)
     PARLE_NORM(64, 2);
@@ -375,7 +393,7 @@ hipError_t bwd(hipStream_t st, const parle_norm_desc &d, const void *h, const vo
     }
   }
 #undef PARLE_NORM
-  k_rmsnorm_dw_join<<<dim3(ceil_div(d.dim, 32), d.n), 256, 0, st>>>(partial, strips, d.dim, a.Dp, dw, d.w_stride);
+  k_rmsnorm_dw_join<<<dim3(ceil_div(d.dim, 32), d.n), 32 * kParts, 0, st>>>(partial, strips, d.dim, a.Dp, dw, d.w_stride);
   return hipGetLastError();
 }
 
