@@ -10,6 +10,8 @@
 // of the rounding of a result in bf16.  A result in fp32, such as the gradient of a parameter, is to have fp32 sums: there the codes
 // become bf16 numbers times their scale, which is exact, and the bf16 instructions add them without such a cut, at half
 // the rate.  (A scale of 2^-127 counts as 0 in that conversion.)
+#include <algorithm>
+
 #include "igemm_dev.h"
 #include "tok.h"
 
@@ -35,8 +37,10 @@ struct Args {
   const uint8_t *a, *a_scales, *b, *b_scales;
   const float *bias;
   void *out;
-  long long ld, out_rs;
+  long long ld, out_rs, split_rs;  // split_rs: from the results of one share of the contraction to the next one's
   int M, N, K, pitch, s_pitch, steps, b_shift, accumulate;
+  int share;  // steps of a workgroup, a multiple of four where there are more
+
 };
 
 __device__ __forceinline__ float value(const float *p) { return *p; }
@@ -117,8 +121,8 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
 
   // piece i of a wavefront's loads of a step
   auto load = [&](int stage, int step, int i) {
-    const int k = step * kBlock, c = i & 1 ? c_odd : c_even;
     const int piece = wave * kLoads + i;  // 8 rows of a, then of b
+    const int k = step * kBlock, c = (kLoads % 2 ? piece : i) & 1 ? c_odd : c_even;
     const bool is_a = piece < BM / 8;
     const uint32_t rows = (is_a ? piece : piece - BM / 8) * 8;
     dma16(__builtin_amdgcn_readfirstlane(lds0 + stage + piece * 1024), is_a ? a_desc : b_desc,
@@ -141,7 +145,7 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
            first < g.s_pitch ? (uint32_t)(at * g.s_pitch + first) : kFar);
     }
   };
-  static_assert(kLoads % 2 == 0 && BM % 16 == 0, "the pieces of a wavefront alternate between halves of 16 rows");
+  static_assert((BM + BN) % (8 * kWaves) == 0 && BM % 16 == 0, "whole pieces for every wavefront, that alternate between halves of 16 rows");
 
   const int r = lane & 31, half = lane >> 5;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
@@ -205,21 +209,22 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
 
   // Loads and reads past the last step bring zeros that nothing uses: the loop's body has no branch that the products could be moved
   // across.
-  load_scales(0);
+  const int from = blockIdx.y * g.share, to = min(from + g.share, g.steps);
+  load_scales(from);
 #pragma unroll
   for (int p = 0; p < STAGES; ++p)
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(p * kStage, p, i);
+    for (int i = 0; i < kLoads; ++i) load(p * kStage, from + p, i);
   igemm_dev::wait_loads<(STAGES - 1) * kLoads>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int t = 0; t < kFrags; ++t) read(0, 0, t);
   int here = 0;  // the step's stage
-  for (int first = 0; first < g.steps; first += 4) {
+  for (int first = from; first < to; first += 4) {
     take_scales(first);
     load_scales(first + 4);  // over those of the group before, which everyone has taken
-    const int last = min(first + 4, g.steps);
+    const int last = min(first + 4, to);
     for (int step = first; step < last; ++step) {
       const int next = here == (STAGES - 1) * kStage ? 0 : here + kStage;
       multiply(0, [&](int i) { share(i, kFrags, kProducts / 2, [&](int t) { read(here, 1, t); }); });
@@ -243,7 +248,7 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   igemm_dev::wait_loads<0>();
 
   // A lane has row m = its r of a 32 x 32 product, columns 8 j + 4 half .. + 3 in registers 4 j .. 4 j + 3.
-  TO *out = (TO *)g.out + rep * g.out_rs;
+  TO *out = (TO *)g.out + rep * g.out_rs + blockIdx.y * g.split_rs;
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm) {
     const int m = m0 + wm + tm * 32 + r;
@@ -318,13 +323,40 @@ __global__ __launch_bounds__(kRowsWaves *PARLE_WAVE) void k_fp8_rows(Args g) {
   }
 }
 
+// Adds the shares of the contraction, in order: out = their sum + bias (+ out).  grid: (vectors of a row's, rows, replicas)
+template <typename TO>
+__global__ __launch_bounds__(256) void k_fp8_join(const float *part, int splits, Args g) {
+  const int n = (blockIdx.x * 256 + threadIdx.x) * tok::kVec, left = g.N - n, rep = blockIdx.z;
+  if (left <= 0) return;
+  for (int m = blockIdx.y; m < g.M; m += gridDim.y) {
+    float v[tok::kVec] = {};
+    if (g.bias) tok::load8(g.bias + (long long)rep * g.N + n, left, 0.f, v);
+    const float *p = part + ((long long)rep * g.M + m) * g.N + n;
+    const long long step = (long long)gridDim.z * g.M * g.N;
+    for (int s = 0; s < splits; s += 2) {  // an even number of shares
+      tok::Raw8<float> u, w;
+      u.load(p + s * step, left), w.load(p + (s + 1) * step, left);
+#pragma unroll
+      for (int i = 0; i < tok::kVec; ++i) v[i] = (v[i] + u.at(i)) + w.at(i);
+    }
+    TO *to = (TO *)g.out + rep * g.out_rs + m * g.ld + n;
+    if (g.accumulate) {
+      float o[tok::kVec];
+      tok::load8(to, left, 0.f, o);
+#pragma unroll
+      for (int i = 0; i < tok::kVec; ++i) v[i] += o[i];
+    }
+    tok::store8(to, left, v);
+  }
+}
+
 template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
-hipError_t run_tile(hipStream_t st, const Args &g, int replicas) {
+hipError_t run_tile(hipStream_t st, const Args &g, int replicas, int splits = 1) {
   constexpr int kLds = (BM + BN) * (STAGES * kBlock + 2 * 4);
   static const hipError_t lds_ok =
       hipFuncSetAttribute((const void *)k_fp8_tile<TO, EXACT, BM, BN, WM, WN, STAGES>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (lds_ok != hipSuccess) return lds_ok;
-  const dim3 grid(ceil_div(g.N, BN) * ceil_div(g.M, BM), 1, replicas);
+  const dim3 grid(ceil_div(g.N, BN) * ceil_div(g.M, BM), splits, replicas);
   k_fp8_tile<TO, EXACT, BM, BN, WM, WN, STAGES><<<grid, WM * WN * PARLE_WAVE, kLds, st>>>(g);
   return hipGetLastError();
 }
@@ -337,53 +369,91 @@ hipError_t run_rows(hipStream_t st, const Args &g, int replicas) {
 }
 
 // What a tiling takes, in microseconds: the start and end of a tile, and a step of it with one or two tiles on a compute unit (two: 0
-// where one fills it).
+// where one fills it).  Measured at 8192 x 8192 x 4096, 2050 x 4000 x 1024, 2050 x 1024 x 4000, 4000 x 1024 x 2050 (three replicas) and
+// 128 x 8192 x 4096: what decides is how many rounds of tiles there are and how full the last one is.  bf16 and fp32 results.
 struct Tiling {
   int bm, bn;
-  float start, one, two;
-  float cost(const Args &g, int replicas) const {
-    const long long tiles = (long long)ceil_div(g.M, bm) * ceil_div(g.N, bn) * replicas, each = (tiles + 255) / 256;
-    const float single = start + one * (float)g.steps;
-    return two == 0.f ? (float)each * single : (float)(each / 2) * (start + two * (float)g.steps) + (float)(each % 2) * single;
+  float start, one[2], two[2];
+  float cost(const parle_fp8_desc &d, int splits) const {
+    const int steps = ceil_div(d.depth, kBlock), share = splits > 1 ? (int)round_up(ceil_div(steps, splits), 4) : steps, wide = d.out_dtype ? 0 : 1;
+    const long long tiles = (long long)ceil_div(d.rows, bm) * ceil_div(d.cols, bn) * d.n * splits, each = (tiles + 255) / 256;
+    const float single = start + one[wide] * (float)share, pair = start + two[wide] * (float)share;
+    const float join = splits > 1 ? 3.f + (float)d.n * d.rows * d.cols * (8.f * splits + 4.f) / 4e6f : 0.f;
+    return join + (two[0] == 0.f ? (float)each * single : (float)(each / 2) * pair + (float)(each % 2) * single);
   }
 };
+constexpr Tiling kTilings[] = {{256, 256, 5.5f, {1.5f, 3.2f}, {0.f, 0.f}},
+                               {192, 256, 5.5f, {1.3f, 2.7f}, {0.f, 0.f}},
+                               {128, 256, 5.5f, {0.95f, 1.75f}, {0.f, 0.f}},
+                               {128, 128, 4.f, {0.65f, 1.f}, {1.1f, 1.7f}},
+                               {64, 64, 3.f, {0.25f, 0.4f}, {0.5f, 0.65f}}};
+constexpr int kSmallest = 4;
+
+constexpr int kFewRows = 16;
+
+struct Plan {
+  int tiling, splits;
+};
+// The tiling that takes least; the contraction of the smallest one may be shared, where the whole product is a few tiles.
+Plan plan_of(const parle_fp8_desc &d) {
+  Plan best = {0, 1};
+  float least = kTilings[0].cost(d, 1);
+  const auto consider = [&](int tiling, int splits) {
+    const float c = kTilings[tiling].cost(d, splits);
+    if (c < least) least = c, best = Plan{tiling, splits};
+  };
+  for (int i = 1; i <= kSmallest; ++i) consider(i, 1);
+  for (int splits = 2; splits <= 8; splits *= 2)
+    if (ceil_div(d.depth, kBlock) >= 4 * splits) consider(kSmallest, splits);
+  return best;
+}
 
 template <typename TO>
-hipError_t run(hipStream_t st, const Args &g, int replicas) {
+hipError_t run(hipStream_t st, const parle_fp8_desc &d, Args g, float *partial) {
   constexpr bool kExact = sizeof(TO) == 4;
 #ifdef TILE
-  return run_tile<TO, kExact, TILE>(st, g, replicas);
+  return run_tile<TO, kExact, TILE>(st, g, d.n);
 #else
-  if (g.M <= 16) {
+  if (g.M <= kFewRows) {
     // four steps at least for a wavefront, and no fewer wavefronts than eight for 16 rows of b
-    if (g.steps >= 32) return run_rows<TO, 8>(st, g, replicas);
-    if (g.steps >= 16) return run_rows<TO, 4>(st, g, replicas);
-    if (g.steps >= 8) return run_rows<TO, 2>(st, g, replicas);
-    return run_rows<TO, 1>(st, g, replicas);
+    if (g.steps >= 32) return run_rows<TO, 8>(st, g, d.n);
+    if (g.steps >= 16) return run_rows<TO, 4>(st, g, d.n);
+    if (g.steps >= 8) return run_rows<TO, 2>(st, g, d.n);
+    return run_rows<TO, 1>(st, g, d.n);
   }
-  const Tiling t[4] = {{256, 256, 5.5f, kExact ? 3.2f : 1.2f, 0.f},
-                       {128, 256, 5.5f, kExact ? 1.7f : 0.9f, 0.f},
-                       {128, 128, 4.f, kExact ? 1.f : 0.65f, kExact ? 1.5f : 1.2f},
-                       {64, 64, 3.f, kExact ? 0.4f : 0.25f, kExact ? 0.65f : 0.5f}};
-  int best = 0;
-  for (int i = 1; i < 4; ++i)
-    if (t[i].cost(g, replicas) < t[best].cost(g, replicas)) best = i;
-  if (best == 0) return run_tile<TO, kExact, 256, 256, 2, 4, 2>(st, g, replicas);
-  if (best == 1) return run_tile<TO, kExact, 128, 256, 2, 4, 3>(st, g, replicas);
-  if (best == 2) return run_tile<TO, kExact, 128, 128, 2, 2, 2>(st, g, replicas);
-  return run_tile<TO, kExact, 64, 64, 2, 2, 4>(st, g, replicas);
+  const Plan p = plan_of(d);
+  if (p.splits > 1) {
+    Args part = g;
+    part.out = partial, part.ld = g.N, part.out_rs = (long long)g.M * g.N, part.split_rs = part.out_rs * d.n;
+    part.bias = nullptr, part.accumulate = 0, part.share = (int)round_up(ceil_div(g.steps, p.splits), 4);
+    const hipError_t e = run_tile<float, kExact, 64, 64, 2, 2, 4>(st, part, d.n, p.splits);
+    if (e != hipSuccess) return e;
+    k_fp8_join<TO><<<dim3(ceil_div(g.N, 256 * tok::kVec), std::min(g.M, 1024), d.n), 256, 0, st>>>(partial, p.splits, g);
+    return hipGetLastError();
+  }
+  switch (p.tiling) {
+    case 0: return run_tile<TO, kExact, 256, 256, 2, 4, 2>(st, g, d.n);
+    case 1: return run_tile<TO, kExact, 192, 256, 2, 4, 2>(st, g, d.n);
+    case 2: return run_tile<TO, kExact, 128, 256, 2, 4, 3>(st, g, d.n);
+    case 3: return run_tile<TO, kExact, 128, 128, 2, 2, 2>(st, g, d.n);
+    default: return run_tile<TO, kExact, 64, 64, 2, 2, 4>(st, g, d.n);
+  }
 #endif
 }
 
 }  // namespace
 
-int64_t fp8_scratch_bytes(const parle_fp8_desc &d) { return 0; }
+int64_t fp8_scratch_bytes(const parle_fp8_desc &d) {
+  if (d.rows <= kFewRows) return 0;
+  const int splits = plan_of(d).splits;
+  return splits > 1 ? (int64_t)splits * d.n * d.rows * d.cols * 4 : 0;
+}
 
 hipError_t launch_fp8_matmul(hipStream_t st, const parle_fp8_desc &d, const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
                              const uint8_t *b_scales, const float *bias, float *partial, void *out) {
   Args g;
   g.a = a, g.a_scales = a_scales, g.b = b, g.b_scales = b_scales, g.bias = bias, g.out = out, g.ld = d.ld_out, g.out_rs = d.out_stride;
   g.M = d.rows, g.N = d.cols, g.K = d.depth, g.pitch = (int)round_up(d.depth, 16), g.steps = ceil_div(d.depth, kBlock);
-  g.s_pitch = (int)round_up(g.steps, 4), g.b_shift = d.b_block == 1 ? 0 : 7, g.accumulate = d.accumulate;
-  return d.out_dtype ? run<bf16_t>(st, g, d.n) : run<float>(st, g, d.n);
+  g.s_pitch = (int)round_up(g.steps, 4), g.b_shift = d.b_block == 1 ? 0 : 7, g.accumulate = d.accumulate, g.share = g.steps, g.split_rs = 0;
+  return d.out_dtype ? run<bf16_t>(st, d, g, partial) : run<float>(st, d, g, partial);
 }
