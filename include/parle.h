@@ -510,7 +510,7 @@ typedef struct {
  * first where two are equal; -1 and -inf where a row has no more classes above -inf.  logp, entropy, lse may each be NULL;
  * top_ids and top_logp are NULL where top is 0.  A label outside 0 .. classes-1 gives logp 0.  A row of -inf only has lse = -inf,
  * entropy 0 and logp = -inf.  A NaN or +inf in a row makes its logp, entropy and lse NaN, and its alternatives unspecified.
- * Groups of eight elements at multiples of eight elements in memory are read whole where they hold one of a row. */
+ * Of memory next to a row, the 16 aligned bytes that its first and its last element lie in are read. */
 parle_status parle_k_logprob_forward(void *hip_stream, const parle_logprob_desc *desc, const void *logits, const int32_t *labels,
                                      void *scratch, int64_t scratch_bytes, float *logp, float *entropy, float *lse,
                                      int32_t *top_ids, float *top_logp);

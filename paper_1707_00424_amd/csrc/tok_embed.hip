@@ -12,6 +12,8 @@
 //      chunks.  A group of lanes sums the runs of its chunk; a run that ends inside goes to the table, one that crosses a border
 //      to scratch.
 //   3. Runs of several chunks are joined, chunk by chunk in order.
+// Up to kDirect tokens need none of this: every workgroup owns a few rows of the table, looks through all tokens for them, and writes its
+// rows whole, one launch at the rate of the stores (85 tokens into 25376 x 1652: 39 us in three launches, 31 in one).
 #include <algorithm>
 
 #include "tok.h"
@@ -347,6 +349,102 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(SumArgs a) {
   }
 }
 
+// ---- gradient, few tokens ----
+constexpr int kDirect = 512, kDirectRows = 64;
+
+// Columns col .. col + 3 of a row, of which those from `from` to `to` - 1 exist; what comes in the others' places is not used.
+__device__ __forceinline__ f4 load4(const float *row, int col, int from, int to) {
+  const float *p = row + col;
+  if (to - from == 4) return *(const f4_any *)p;
+  return f4{p[min(max(0, from), to - 1)], p[min(max(1, from), to - 1)], p[min(max(2, from), to - 1)], p[min(max(3, from), to - 1)]};
+}
+__device__ __forceinline__ f4 load4(const bf16_t *row, int col, int from, int to) {
+  const bf16_t *p = row + col;
+  us4 v;
+  if (to - from == 4) {
+    v = *(const us4_any *)p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = p[min(max(i, from), to - 1)];
+  }
+  return f4{bf16_to_f32(v.x), bf16_to_f32(v.y), bf16_to_f32(v.z), bf16_to_f32(v.w)};
+}
+
+// `lanes` = 2^lane_shift threads per row; a workgroup owns `rows` rows of the table.  Rows of the table are written in the aligned
+// 16 bytes that they lie in, wherever they begin: misaligned stores of 16 bytes took twice as long.  grid: (V / rows, n)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_direct(const int32_t *tokens, const T *dout, int count, int V, int D, float scale,
+                                                           int rows, int lane_shift, float *dtable, long long table_rs) {
+  constexpr int kWaves = kThreads / PARLE_WAVE, kAhead = 8;
+  __shared__ int hit[kDirect], sorted[kDirect];  // row of the workgroup's << 16 | position: by position, then by row and position
+  __shared__ int start[kDirectRows + 1];         // of a row's hits
+  __shared__ int found[kDirect / kThreads][kWaves];
+  const int rep = blockIdx.y, v0 = blockIdx.x * rows, mine = min(rows, V - v0);
+  const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = threadIdx.x / PARLE_WAVE;
+  int row_of[kDirect / kThreads];
+  uint64_t in[kDirect / kThreads];
+#pragma unroll
+  for (int k = 0; k < kDirect / kThreads; ++k) {
+    const int i = k * kThreads + threadIdx.x;
+    row_of[k] = i < count ? tokens[(long long)rep * count + i] - v0 : -1;
+    in[k] = __ballot(row_of[k] >= 0 && row_of[k] < mine);
+    if (lane == 0) found[k][wave] = __popcll(in[k]);
+  }
+  __syncthreads();
+  int hits = 0;
+#pragma unroll
+  for (int k = 0; k < kDirect / kThreads; ++k)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == wave && row_of[k] >= 0 && row_of[k] < mine)
+        hit[hits + __popcll(in[k] & ((1ull << lane) - 1))] = row_of[k] << 16 | (k * kThreads + threadIdx.x);
+      hits += found[k][w];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < hits; i += kThreads) {
+    const int me = hit[i];
+    int before = 0;
+#pragma unroll 8
+    for (int j = 0; j < hits; ++j) before += hit[j] < me;
+    sorted[before] = me;
+  }
+  if ((int)threadIdx.x <= mine) {
+    int before = 0;
+#pragma unroll 8
+    for (int j = 0; j < hits; ++j) before += hit[j] < (int)threadIdx.x << 16;
+    start[threadIdx.x] = before;
+  }
+  __syncthreads();
+  const int lanes = 1 << lane_shift;
+  const T *src = dout + (long long)rep * count * D;
+  float *table = dtable + rep * table_rs + (long long)v0 * D;
+  for (int r = threadIdx.x >> lane_shift; r < mine; r += kThreads >> lane_shift) {
+    float *row = table + (long long)r * D;
+    const int first = start[r], last = start[r + 1];
+    const int before = (int)((uintptr_t)row / 4 % 4);  // elements of the row's first 16 bytes that are not its
+    for (int col = (threadIdx.x & (lanes - 1)) * 4 - before; col < D; col += lanes * 4) {
+      const int from = max(0, -col), to = min(4, D - col);
+      f4 acc = {0.f, 0.f, 0.f, 0.f};
+      for (int h = first; h < last; h += kAhead) {
+        f4 x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = load4(src + (long long)(sorted[min(h + u, last - 1)] & 0xffff) * D, col, from, to);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (h + u < last) acc += x[u];
+      }
+      acc *= scale;
+      if (to - from == 4) {
+        *(f4 *)(row + col) = acc;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e >= from && e < to) row[col + e] = acc[e];
+      }
+    }
+  }
+}
+
 int lane_shift_of(int groups) {
   int s = 0;
   while (s < 6 && (1 << s) < groups) ++s;
@@ -375,13 +473,28 @@ hipError_t fwd(hipStream_t st, const parle_embed_desc &d, const void *table, con
   return hipGetLastError();
 }
 
+template <typename T>
+hipError_t direct(hipStream_t st, const parle_embed_desc &d, const int32_t *tokens, const void *dout, float *dtable) {
+  int shift = 3;  // 8 .. 256 lanes per row, 16 bytes side by side of each
+  while (shift < 8 && (4 << shift) < d.dim + 3) ++shift;
+  // Rows of 32 KiB together: fewer look through the tokens more often, more leave the frequent tokens to too few workgroups (25376 x 1652
+  // with 85 tokens: 35 us with 64 KiB, 31 with 32, 32 with 16, 38 with 8).  Workgroups enough for the chip where the table is small.
+  const long long all = (long long)d.vocab * d.n;
+  const int rows = (int)std::max<long long>(1, std::min<long long>({8192 / d.dim, all / 2048, kDirectRows}));
+  const dim3 grid(ceil_div(d.vocab, rows), d.n);
+  k_embed_direct<T><<<grid, kThreads, 0, st>>>(
+      tokens, (const T *)dout, d.tokens, d.vocab, d.dim, d.scale, rows, shift, dtable, d.table_stride);
+  return hipGetLastError();
+}
+
 // Scratch: keys and positions (twice where tiles are merged), then the partial sums.
 struct Scratch {
   long long list, lists, part, Dp;
   int chunks;
 };
 Scratch scratch_of(const parle_embed_desc &d) {
-  Scratch s;
+  Scratch s = {};
+  if (d.tokens <= kDirect) return s;
   s.list = round_up((long long)d.n * d.tokens * 4, 256);
   s.lists = d.tokens > kTile ? 4 : 2;
   s.Dp = round_up(d.dim, 8);
@@ -417,13 +530,17 @@ int64_t embed_scratch_bytes(const parle_embed_desc &d) {
 
 hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int32_t *tokens, const void *dout, void *scratch,
                             float *dtable) {
+  if (d.tokens <= kDirect) return d.dtype ? direct<bf16_t>(st, d, tokens, dout, dtable) : direct<float>(st, d, tokens, dout, dtable);
   const Scratch s = scratch_of(d);
   char *at = (char *)scratch;
   uint32_t *keys = (uint32_t *)at, *pos = (uint32_t *)(at + s.list);
-  const int tiles = d.tokens > kTile ? ceil_div(d.tokens, kTile) : d.tokens > 0 ? 1 : 0;
-  const auto sort = d.tokens > 4 * kSortThreads ? sort_zero<kMostItems> : d.tokens > kSortThreads ? sort_zero<4> : sort_zero<1>;
+  const int tiles = ceil_div(d.tokens, kTile);
+  const auto sort = d.tokens > 8 * kSortThreads   ? sort_zero<kMostItems>
+                    : d.tokens > 4 * kSortThreads ? sort_zero<8>
+                    : d.tokens > kSortThreads     ? sort_zero<4>
+                                                  : sort_zero<1>;
   const hipError_t e = sort(st, d, tiles, tokens, keys, pos, dtable);
-  if (e != hipSuccess || d.tokens == 0) return e;
+  if (e != hipSuccess) return e;
   if (tiles > 1) {
     uint32_t *keys2 = (uint32_t *)(at + 2 * s.list), *pos2 = (uint32_t *)(at + 3 * s.list);
     for (long long len = kTile; len < d.tokens; len *= 2) {
@@ -443,6 +560,6 @@ hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int
     (eights ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
   else
     (eights ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
-  if (s.chunks > 1) k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
+  k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -139,14 +139,14 @@ struct Lds {
   int count, vectors;
 };
 
-// A row as vectors of eight elements at boundaries of eight elements in memory: its class 0 lies `off` elements behind the boundary that
-// `base` points to, and vector j holds elements j .. j + 7 of base, of which the row's are off .. end - 1.
+// A row as vectors of eight elements from a boundary of 16 bytes on: its class 0 lies `off` elements behind the boundary that `base`
+// points to, and vector j holds elements j .. j + 7 of base, of which the row's are off .. end - 1.
 template <typename T>
 struct Row {
   const T *base;
   int off, end;
   __device__ __forceinline__ Row(const T *x, int C) {
-    off = (int)((uintptr_t)x % (kVec * sizeof(T)) / sizeof(T));
+    off = (int)((uintptr_t)x % 16 / sizeof(T));
     base = x - off;
     end = off + C;
   }
@@ -166,16 +166,20 @@ struct RawF32 {
       b[i - 4] = -INFINITY;
   }
 };
-__device__ __forceinline__ void read(const bf16_t *p, RawBf16 &x) { x.v = *(const us8 *)p; }
-__device__ __forceinline__ void read(const float *p, RawF32 &x) { x.a = *(const f4 *)p, x.b = *(const f4 *)(p + 4); }
+// 16 bytes that hold an element of the row are read whole, no others; `left`: elements from p to the row's end.
+__device__ __forceinline__ void read(const bf16_t *p, int left, RawBf16 &x) { x.v = *(const us8 *)p; }
+__device__ __forceinline__ void read(const float *p, int left, RawF32 &x) {
+  x.a = *(const f4 *)p;
+  x.b = left > 4 ? *(const f4 *)(p + 4) : f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+}
 template <typename T>
 using Raw = std::conditional_t<sizeof(T) == 2, RawBf16, RawF32>;
-// Vector j; -inf in the places of elements that are not the row's.  A vector that holds one of them is read whole.
+// Vector j < end; -inf in the places of elements that are not the row's.
 template <typename T>
 __device__ __forceinline__ Raw<T> fetch(const Row<T> &r, int j, bool live) {
   Raw<T> x;
   if (live) {
-    read(r.base + j, x);
+    read(r.base + j, r.end - j, x);
     if (j < r.off || j + kVec > r.end) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i)
