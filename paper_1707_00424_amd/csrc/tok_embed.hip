@@ -1,7 +1,8 @@
 // Rows of a table by token, scaled, and the table's gradient.
 //
-// Forward: out[i] = scale * table[tokens[i]], a copy whose source rows are anywhere.  Groups of lanes walk a row in
-// steps of eight elements.
+// Forward: out[i] = scale * table[tokens[i]], a copy whose source rows are anywhere; memory bounds it.  Groups of lanes walk a row in
+// steps of eight elements; four rows per group are on their way together where there are many (24576 rows of 1024 fp32: 37 us, 5.5
+// TB/s, what a plain copy reaches), one where there are few (16 rows: 2.5 us, the latency of a token and of its row).
 //
 // Gradient: dtable[v] = scale * sum of dout[i] over the positions i with tokens[i] = v.  A row of the table belongs to a run of
 // equal keys of the sorted tokens, so nothing is added atomically and the order of a sum depends on the tokens alone:
@@ -12,6 +13,8 @@
 //      chunks.  A group of lanes sums the runs of its chunk; a run that ends inside goes to the table, one that crosses a border
 //      to scratch.
 //   3. Runs of several chunks are joined, chunk by chunk in order.
+// 3 x 8192 tokens into 50001 x 512: 48 us for the zeros (6.4 TB/s; the sort takes less beside them), 18 for the chunks (latency: keys, then
+// rows from memory, 6 wavefronts a compute unit; chunks of 8 or 32 take the same or longer), 7 for the joins.
 // Up to kDirect tokens need none of this: every workgroup owns a few rows of the table, looks through all tokens for them, and writes its
 // rows whole, one launch at the rate of the stores (85 tokens into 25376 x 1652: 39 us in three launches, 31 in one).
 #include <algorithm>

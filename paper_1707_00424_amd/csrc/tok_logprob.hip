@@ -2,16 +2,19 @@
 //
 // Forward: one pass over a row with the running maximum m and, relative to it, z = sum e^(x-m) and t = sum (x-m) e^(x-m):
 //   lse = m + log z,   entropy = log z - t / z,   logp = (x[label] - m) - log z.
-// Odd numbers of classes put rows anywhere; vectors are taken at 16-byte boundaries of memory, whatever the row's.  A row belongs to one workgroup, or to several that each take a part of the classes where rows are few; a second, small kernel
-// joins parts.
+// Odd numbers of classes put rows anywhere; vectors are taken at 16-byte boundaries of memory, whatever the row's.  A row belongs to one
+// workgroup, or to several that each take a part of the classes where rows are few; a second, small kernel joins parts.
+//
+// 4096 rows of 50001 bf16 with 5 alternatives: 93 us, 4.4 TB/s; memory bounds it, with exponentials close behind (one per element at a quarter
+// of the vector unit's rate: about 60 us).  Four rows of 128000 with 20: 7.7 + 4.8 us, latency.  The gradient, a pass that reads and
+// writes: 6144 rows of 32000 in 139 us, 5.6 TB/s.
 //
 // Alternatives.  Every thread notes the largest value of its vectors and which vector holds it.  The `top`-th best of those
 // (value, vector) pairs over 64 groups of four threads is a bound: `top` elements at least are as good, so an element below it is none
 // of the best.  Only threads whose own best reaches the bound, about `top` of them, read their part again; vectors that reach the bound
 // go to a list in LDS, their elements that do to another, out of which the best are taken by counting.  A list that overflows, where
-// few threads hold very many of the best, is given up for `top` searches over the whole part.  (The code is kept short on purpose: a
-// row to a workgroup runs through it once, and a first version of 50 KiB took 20 us for four rows of 128000, nearly all of it waiting
-// for instructions.)
+// few threads hold very many of the best, is given up for `top` searches over the whole part.  (The code is kept short on purpose, as a
+// workgroup runs through it once: with 53 KiB of it the 4096 rows took 137 us, with 13 KiB 96.)
 #include <math.h>
 
 #include <algorithm>
