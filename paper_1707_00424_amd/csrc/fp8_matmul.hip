@@ -109,9 +109,9 @@ __device__ __forceinline__ void tile_of(int id, int rows, int cols, int &m, int 
 template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int kStage = (BM + BN) * kBlock;
+  constexpr int kRows = BM + BN, kStage = kRows * kBlock;
   constexpr int kLoads = (BM + BN) / 8 / kWaves;  // 1 KiB loads of a wavefront per step: 8 rows each
-  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the stages, then two groups of scales
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the stages, then scales of twice sixteen steps, then what is touched
   const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PARLE_WAVE);
   int tile_m, tile_n;
   tile_of(blockIdx.x, ceil_div(g.M, BM), ceil_div(g.N, BN), tile_m, tile_n);
@@ -134,8 +134,21 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
     dma16(__builtin_amdgcn_readfirstlane(lds0 + stage + piece * 1024), is_a ? a_desc : b_desc,
           k + c * 16 < g.pitch ? voff + c * 16 : kFar, __builtin_amdgcn_readfirstlane(rows * (uint32_t)g.pitch + k));
   };
-  // Scales of four steps, a dword per row of the tile: 64 rows for a wavefront's load, in turn.
-  constexpr int kRows = BM + BN, kScaleLoads = kRows / PARLE_WAVE;
+  // The first workgroup that needs a line waits for memory, longer than a step of 1.2 us takes, and its neighbours with it.  So lines are
+  // touched a step before they are loaded, a lane for a line, into 256 bytes per wavefront that nobody reads: of a's rows a quarter by
+  // each of four tiles side by side, of b's by each of four one below the other, which run on this die at the same time.  8192 x
+  // 8192 x 4096 on operands that no cache holds: 254 -> 228 us (ahead by 2 or 3 steps 230, 231).  Three stages, or the longer steps of an
+  // fp32 result, have the time without it, and lose 2 %.
+  constexpr int kTouch = kWaves == 8 && STAGES == 2 && !EXACT, kTouchAhead = 1;
+  auto touch = [&](int step) {
+    if (!kTouch) return;
+    const bool is_a = wave < kWaves / 2;
+    const int each = (is_a ? BM : BN) / 4 / (kWaves / 2), first = ((is_a ? tile_n : tile_m) & 3) * ((is_a ? BM : BN) / 4) + wave % (kWaves / 2) * each;
+    dma4(__builtin_amdgcn_readfirstlane(lds0 + STAGES * kStage + 32 * kRows + wave * 256), is_a ? a_desc : b_desc,
+         lane < each && step < g.steps ? (uint32_t)(first + lane) * (uint32_t)g.pitch + step * kBlock : kFar);
+  };
+  // Scales of sixteen steps, 16 bytes per row of the tile: 64 rows for a wavefront's load, in turn.
+  constexpr int kScaleLoads = kRows / PARLE_WAVE;
   const int b_rows = (g.N + (1 << g.b_shift) - 1) >> g.b_shift, b_row0 = n0 >> g.b_shift;
   const u4 sa_desc = buffer_desc(g.a_scales + ((long long)rep * g.M + m0) * g.s_pitch, (uint32_t)(min(BM, g.M - m0) * g.s_pitch));
   const u4 sb_desc =
@@ -147,8 +160,8 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
       const bool is_a = p < BM / PARLE_WAVE;
       const int row = (is_a ? p : p - BM / PARLE_WAVE) * PARLE_WAVE + lane;
       const int at = is_a ? row : ((n0 + row) >> g.b_shift) - b_row0;
-      dma4(__builtin_amdgcn_readfirstlane(lds0 + STAGES * kStage + (first & 4) * kRows + p * PARLE_WAVE * 4), is_a ? sa_desc : sb_desc,
-           first < g.s_pitch ? (uint32_t)(at * g.s_pitch + first) : kFar);
+      dma16(__builtin_amdgcn_readfirstlane(lds0 + STAGES * kStage + (first & 16) * kRows + p * PARLE_WAVE * 16), is_a ? sa_desc : sb_desc,
+            first < g.s_pitch ? (uint32_t)(at * g.s_pitch + first) : kFar, 0);
     }
   };
   static_assert((BM + BN) % (8 * kWaves) == 0 && BM % 16 == 0, "whole pieces for every wavefront, that alternate between halves of 16 rows");
@@ -158,11 +171,11 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   f16v acc[TM][TN] = {};
   int xa[TM], xb[TN];  // scales of the step, in the lowest byte
   auto take_scales = [&](int first) {
-    const int *p = (const int *)(lds + STAGES * kStage + (first & 4) * kRows) + r;
+    const int *p = (const int *)(lds + STAGES * kStage + (first & 16) * kRows) + r * 4 + (first >> 2 & 3);
 #pragma unroll
-    for (int t = 0; t < TM; ++t) xa[t] = p[wm + t * 32];
+    for (int t = 0; t < TM; ++t) xa[t] = p[(wm + t * 32) * 4];
 #pragma unroll
-    for (int t = 0; t < TN; ++t) xb[t] = p[BM + wn + t * 32];
+    for (int t = 0; t < TN; ++t) xb[t] = p[(BM + wn + t * 32) * 4];
   };
 
   // 64 codes of a row for two lanes: chunks 4 h + 2 half and the one behind it
@@ -216,7 +229,7 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   // Loads and reads past the last step bring zeros that nothing uses: the loop's body has no branch that the products could be moved
   // across.
   const int from = blockIdx.y * g.share, to = min(from + g.share, g.steps);
-  load_scales(from);
+  load_scales(from & ~15);
 #pragma unroll
   for (int p = 0; p < STAGES; ++p)
 #pragma unroll
@@ -229,19 +242,20 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   int here = 0;  // the step's stage
   for (int first = from; first < to; first += 4) {
     take_scales(first);
-    load_scales(first + 4);  // over those of the group before, which everyone has taken
+    if (first == from || (first & 15) == 0) load_scales((first & ~15) + 16);  // over those of the sixteen before, which everyone has taken
     const int last = min(first + 4, to);
     for (int step = first; step < last; ++step) {
       const int next = here == (STAGES - 1) * kStage ? 0 : here + kStage;
       multiply(0, [&](int i) { share(i, kFrags, kProducts / 2, [&](int t) { read(here, 1, t); }); });
       __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * (kLoads + kTouch) + kTouch) : "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       multiply(1, [&](int i) {
         share(i, kFrags, kProducts, [&](int t) { read(next, 0, t); });
         share(i, kLoads, kProducts, [&](int p) { load(here, step + STAGES, p); });
+        if (i == kProducts - 1) touch(step + STAGES + kTouchAhead);
       });
       __builtin_amdgcn_sched_barrier(0);
       here = next;
@@ -358,7 +372,7 @@ __global__ __launch_bounds__(256) void k_fp8_join(const float *part, int splits,
 
 template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 hipError_t run_tile(hipStream_t st, const Args &g, int replicas, int splits = 1) {
-  constexpr int kLds = (BM + BN) * (STAGES * kBlock + 2 * 4);
+  constexpr int kLds = (BM + BN) * (STAGES * kBlock + 2 * 16) + WM * WN * 256;
   static const hipError_t lds_ok =
       hipFuncSetAttribute((const void *)k_fp8_tile<TO, EXACT, BM, BN, WM, WN, STAGES>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (lds_ok != hipSuccess) return lds_ok;
