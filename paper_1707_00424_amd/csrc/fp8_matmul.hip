@@ -234,7 +234,8 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   for (int p = 0; p < STAGES; ++p)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(p * kStage, from + p, i);
-  igemm_dev::wait_loads<(STAGES - 1) * kLoads>();
+  touch(from + STAGES);
+  igemm_dev::wait_loads<(STAGES - 1) * kLoads + kTouch>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
