@@ -218,50 +218,28 @@ struct SumArgs {
   float scale;
 };
 
-// Eight columns of a row of dout, as they came; `left` of them exist (EIGHTS: all).
-template <typename T>
-struct Rows;
-template <>
-struct Rows<bf16_t> {
-  us8 v;
-  template <bool EIGHTS>
-  __device__ __forceinline__ void load(const bf16_t *p, int left) {
-    if (EIGHTS || left >= kVec) {
-      v = *(const us8_any *)p;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) v[i] = p[min(i, left - 1)];
-    }
-  }
-  __device__ __forceinline__ void add(float (&acc)[kVec]) const {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) acc[i] += bf16_to_f32(v[i]);
-  }
-};
-template <>
-struct Rows<float> {
-  f4 a, b;
-  template <bool EIGHTS>
-  __device__ __forceinline__ void load(const float *p, int left) {
-    if (EIGHTS || left >= kVec) {
-      a = *(const f4_any *)p, b = *(const f4_any *)(p + 4);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = p[min(i, left - 1)], b[i] = p[min(4 + i, left - 1)];
-    }
-  }
-  __device__ __forceinline__ void add(float (&acc)[kVec]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += a[i], acc[4 + i] += b[i];
-  }
-};
+// Four columns of a row of dout, as they came; `left` of them exist (FOURS: all), and the others' places are not used.
+template <bool FOURS>
+__device__ __forceinline__ us4 load_raw(const bf16_t *p, int left) {
+  if (FOURS || left >= 4) return *(const us4_any *)p;
+  return us4{p[0], p[min(1, left - 1)], p[min(2, left - 1)], 0};
+}
+template <bool FOURS>
+__device__ __forceinline__ f4 load_raw(const float *p, int left) {
+  if (FOURS || left >= 4) return *(const f4_any *)p;
+  return f4{p[0], p[min(1, left - 1)], p[min(2, left - 1)], 0.f};
+}
+__device__ __forceinline__ f4 widen(us4 v) { return f4{bf16_to_f32(v.x), bf16_to_f32(v.y), bf16_to_f32(v.z), bf16_to_f32(v.w)}; }
+__device__ __forceinline__ f4 widen(f4 v) { return v; }
 
-// A group of lanes sums one chunk for its columns.  grid: (chunks / groups per block, column slices, n)
-template <typename T, bool EIGHTS>
+// A group of lanes sums one chunk for its columns, four to a lane: a wavefront stores a kilobyte of a row at once, and there are twice
+// the wavefronts that eight columns to a lane give (3 x 8192 tokens of 512: 3 % of the whole call).
+// grid: (chunks / groups per block, column slices, n)
+template <typename T, bool FOURS>
 __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArgs a) {
   const int lanes = 1 << a.lane_shift, rep = blockIdx.z;
   const int chunk = blockIdx.x * (kThreads >> a.lane_shift) + (threadIdx.x >> a.lane_shift);
-  const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * kVec;
+  const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * 4;
   if (chunk >= a.chunks || col >= a.D) return;
   const uint32_t *keys = a.keys + (long long)rep * a.T, *pos = a.pos + (long long)rep * a.T;
   const T *src = dout + (long long)rep * a.T * a.D + col;
@@ -283,30 +261,31 @@ __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArg
 #pragma unroll
   for (int j = 0; j < kChunk; ++j)
     if (j >= count) k[j] = 0xffffffffu;  // ends the run in front of it, and is none
-  Rows<T> v[kChunk];
+  decltype(load_raw<FOURS>(src, left)) v[kChunk];
 #pragma unroll
   for (int j = 0; j < kChunk; ++j) {
     const uint32_t row = k[j] < (uint32_t)a.V ? at[j / 4][j % 4] : 0;  // one that exists, and no branch
-    v[j].template load<EIGHTS>(src + (long long)row * a.D, left);
+    v[j] = load_raw<FOURS>(src + (long long)row * a.D, left);
   }
-  float acc[kVec] = {};
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < kChunk; ++j) {
     if (k[j] >= (uint32_t)a.V) break;  // no later key is less
-    v[j].add(acc);
+    acc += widen(v[j]);
     const bool ends = k[j] != k[j + 1];
     if (ends || j + 1 == kChunk) {
       if (ends && !from_before) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) acc[e] *= a.scale;
-        store8(table + (long long)k[j] * a.D, EIGHTS ? kVec : left, acc);
+        float *to = table + (long long)k[j] * a.D;
+        acc *= a.scale;
+        if (FOURS || left >= 4) {
+          *(f4_any *)to = acc;
+        } else {
+          for (int e = 0; e < left; ++e) to[e] = acc[e];
+        }
       } else {
-        float *p = part + (from_before ? 0 : a.Dp);
-        *(f4 *)p = f4{acc[0], acc[1], acc[2], acc[3]};
-        *(f4 *)(p + 4) = f4{acc[4], acc[5], acc[6], acc[7]};
+        *(f4 *)(part + (from_before ? 0 : a.Dp)) = acc;
       }
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) acc[e] = 0.f;
+      acc = f4{0.f, 0.f, 0.f, 0.f};
       from_before = false;
     }
   }
@@ -555,14 +534,14 @@ hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int
   SumArgs a;
   a.keys = keys, a.pos = pos, a.dtable = dtable, a.part = (float *)(at + s.list * s.lists);
   a.table_rs = d.table_stride, a.T = d.tokens, a.V = d.vocab, a.D = d.dim, a.Dp = (int)s.Dp, a.chunks = s.chunks, a.scale = d.scale;
-  const int groups = ceil_div(d.dim, kVec);
+  const int groups = ceil_div(d.dim, 4);
   a.lane_shift = lane_shift_of(groups);
   const dim3 grid(ceil_div(s.chunks, kThreads >> a.lane_shift), ceil_div(groups, 1 << a.lane_shift), d.n);
-  const bool eights = d.dim % kVec == 0;
+  const bool fours = d.dim % 4 == 0;
   if (d.dtype)
-    (eights ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
+    (fours ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
   else
-    (eights ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
+    (fours ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
   k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
