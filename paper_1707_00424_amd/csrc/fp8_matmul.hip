@@ -40,7 +40,6 @@ struct Args {
   long long ld, out_rs, split_rs;  // split_rs: from the results of one share of the contraction to the next one's
   int M, N, K, pitch, s_pitch, steps, b_shift, accumulate;
   int share;  // steps of a workgroup, a multiple of four where there are more
-
 };
 
 __device__ __forceinline__ float value(const float *p) { return *p; }
@@ -432,9 +431,6 @@ Plan plan_of(const parle_fp8_desc &d) {
 template <typename TO>
 hipError_t run(hipStream_t st, const parle_fp8_desc &d, Args g, float *partial) {
   constexpr bool kExact = sizeof(TO) == 4;
-#ifdef TILE
-  return run_tile<TO, kExact, TILE>(st, g, d.n);
-#else
   if (g.M <= kFewRows) {
     // four steps at least for a wavefront, and no fewer wavefronts than eight for 16 rows of b
     if (g.steps >= 32) return run_rows<TO, 8>(st, g, d.n);
@@ -459,7 +455,6 @@ hipError_t run(hipStream_t st, const parle_fp8_desc &d, Args g, float *partial) 
     case 3: return run_tile<TO, kExact, 128, 128, 2, 2, 2>(st, g, d.n);
     default: return run_tile<TO, kExact, 64, 64, 2, 2, 4>(st, g, d.n);
   }
-#endif
 }
 
 }  // namespace
