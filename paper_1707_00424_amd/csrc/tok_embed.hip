@@ -7,14 +7,16 @@
 // Gradient: dtable[v] = scale * sum of dout[i] over the positions i with tokens[i] = v.  A row of the table belongs to a run of
 // equal keys of the sorted tokens, so nothing is added atomically and the order of a sum depends on the tokens alone:
 //   1. One workgroup per replica sorts (token, position) in LDS, a stable radix sort by 6 bits a pass; the other workgroups
-//      meanwhile write the table's zeros, which is most of the bytes.  More tokens than a workgroup sorts are
+//      meanwhile clear as much of the table as can be written in that time.  More tokens than a workgroup sorts are
 //      sorted in tiles, and tiles are merged in pairs.
 //   2. The sorted positions are cut into chunks of kChunk, whatever the tokens: a frequent token spreads over many
 //      chunks.  A group of lanes sums the runs of its chunk; a run that ends inside goes to the table, one that crosses a border
-//      to scratch.
+//      to scratch.  More workgroups clear the rest of the table, except for the rows that the sorted keys name: sums wait for
+//      keys and rows, and leave the memory to them.
 //   3. Runs of several chunks are joined, chunk by chunk in order.
-// 3 x 8192 tokens into 50001 x 512: 48 us for the zeros (6.4 TB/s; the sort takes less beside them), 18 for the chunks (latency: keys, then
-// rows from memory, 6 wavefronts a compute unit; chunks of 8 or 32 take the same or longer), 7 for the joins.
+// 3 x 8192 tokens into 50001 x 512: 75 us, of them 25 for the sort with 127 MB of zeros, 44 for the sums with 180 MB of zeros (250 MB
+// together, 5.7 TB/s) and 7 for the joins; 78 with all zeros beside the sort.  1000 tokens into 100000 x 1024: 94 and 82.  Chunks of 8 or 32 take
+// the same or longer; rows to clear in 64 to 256 KiB a workgroup instead of 32: 77 to 80 and 83 to 85.
 // Up to kDirect tokens need none of this: every workgroup owns a few rows of the table, looks through all tokens for them, and writes its
 // rows whole, one launch at the rate of the stores (85 tokens into 25376 x 1652: 39 us in three launches, 31 in one).
 #include <algorithm>
@@ -216,36 +218,92 @@ struct SumArgs {
   long long table_rs;
   int T, V, D, Dp, chunks, lane_shift;
   float scale;
+  int chunk_x, chunk_y, chunk_blocks;     // workgroups of the sums: per column slice, slices, all
+  int zero_first, zero_rows, zero_blocks;  // the table's rows that are still to be cleared, rows of a workgroup, workgroups of a replica
 };
+constexpr int kZeroRows = 1024;
 
-// Four columns of a row of dout, as they came; `left` of them exist (FOURS: all), and the others' places are not used.
-template <bool FOURS>
-__device__ __forceinline__ us4 load_raw(const bf16_t *p, int left) {
-  if (FOURS || left >= 4) return *(const us4_any *)p;
-  return us4{p[0], p[min(1, left - 1)], p[min(2, left - 1)], 0};
+// First of the `count` ascending keys that is not below `v`; a whole wavefront, 64 keys a step.
+__device__ __forceinline__ int first_not_below(const uint32_t *keys, int count, uint32_t v) {
+  const int lane = threadIdx.x & (PARLE_WAVE - 1);
+  int at = 0, left = count;
+  while (left > 0) {
+    const int step = (left + PARLE_WAVE - 1) / PARLE_WAVE, probe = (lane + 1) * step - 1;
+    const int below = __popcll(__ballot(probe < left && keys[at + min(probe, left - 1)] < v));
+    at += below * step;
+    left = min(step - 1, left - below * step);
+  }
+  return at;
 }
-template <bool FOURS>
-__device__ __forceinline__ f4 load_raw(const float *p, int left) {
-  if (FOURS || left >= 4) return *(const f4_any *)p;
-  return f4{p[0], p[min(1, left - 1)], p[min(2, left - 1)], 0.f};
+
+// Clears those of zero_rows rows that no token has: their keys are sorted by now.  In vectors of 16 bytes of memory, wherever rows begin;
+// a row has four elements at least, so a vector lies in two rows at most.
+__device__ __forceinline__ void clear_rows(const SumArgs &a, int block) {
+  __shared__ uint8_t touched[kZeroRows];
+  __shared__ int bound[2];
+  const int rep = block / a.zero_blocks, v0 = a.zero_first + block % a.zero_blocks * a.zero_rows, rows = min(a.zero_rows, a.V - v0);
+  const uint32_t *keys = a.keys + (long long)rep * a.T;
+  const int wave = threadIdx.x / PARLE_WAVE;
+  if (wave < 2) {
+    const int at = first_not_below(keys, a.T, (uint32_t)(wave ? v0 + rows : v0));
+    if (threadIdx.x % PARLE_WAVE == 0) bound[wave] = at;
+  }
+  for (int i = threadIdx.x; i < rows; i += kThreads) touched[i] = 0;
+  __syncthreads();
+  for (int i = bound[0] + threadIdx.x; i < bound[1]; i += kThreads) touched[keys[i] - v0] = 1;
+  __syncthreads();
+  float *table = a.dtable + rep * a.table_rs + (long long)v0 * a.D;
+  const int all = rows * a.D, before = (int)((uintptr_t)table / 4 % 4);  // elements of the first 16 bytes that are not the table's
+  constexpr int kStep = kThreads * 4;
+  const int step_rows = kStep / a.D, step_cols = kStep % a.D;
+  int e = (int)threadIdx.x * 4 - before, row = e < 0 ? -1 : e / a.D, col = e - row * a.D;
+  for (; e < all; e += kStep) {
+    const int next = min(row + (col + 3 >= a.D), rows - 1);
+    const bool first = touched[max(row, 0)], second = touched[next];
+    if (e >= 0 && e + 4 <= all && !first && !second) {
+      *(f4 *)(table + e) = f4{0.f, 0.f, 0.f, 0.f};
+    } else if (!first || !second) {
+      for (int k = 0; k < 4; ++k)
+        if (e + k >= 0 && e + k < all && !(col + k < a.D ? first : second)) table[e + k] = 0.f;
+    }
+    row += step_rows, col += step_cols;
+    if (col >= a.D) col -= a.D, ++row;
+  }
+}
+
+// Columns of a row of dout, as they came: four, or the `count` < 4 of a shorter row (the others' places are not used).
+template <bool FOUR>
+__device__ __forceinline__ us4 load_raw(const bf16_t *p, int count) {
+  if (FOUR) return *(const us4_any *)p;
+  return us4{p[0], p[min(1, count - 1)], p[min(2, count - 1)], 0};
+}
+template <bool FOUR>
+__device__ __forceinline__ f4 load_raw(const float *p, int count) {
+  if (FOUR) return *(const f4_any *)p;
+  return f4{p[0], p[min(1, count - 1)], p[min(2, count - 1)], 0.f};
 }
 __device__ __forceinline__ f4 widen(us4 v) { return f4{bf16_to_f32(v.x), bf16_to_f32(v.y), bf16_to_f32(v.z), bf16_to_f32(v.w)}; }
 __device__ __forceinline__ f4 widen(f4 v) { return v; }
 
 // A group of lanes sums one chunk for its columns, four to a lane: a wavefront stores a kilobyte of a row at once, and there are twice
-// the wavefronts that eight columns to a lane give (3 x 8192 tokens of 512: 3 % of the whole call).
-// grid: (chunks / groups per block, column slices, n)
-template <typename T, bool FOURS>
+// the wavefronts that eight columns to a lane give (3 x 8192 tokens of 512: 3 % of the whole call).  The workgroups behind these clear
+// rows.  grid: chunk_x * chunk_y * n + zero_blocks * n
+template <typename T, bool FOUR>
 __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArgs a) {
-  const int lanes = 1 << a.lane_shift, rep = blockIdx.z;
-  const int chunk = blockIdx.x * (kThreads >> a.lane_shift) + (threadIdx.x >> a.lane_shift);
-  const int col = (blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * 4;
+  if ((int)blockIdx.x >= a.chunk_blocks) {
+    clear_rows(a, blockIdx.x - a.chunk_blocks);
+    return;
+  }
+  const int lanes = 1 << a.lane_shift, slice = blockIdx.x / a.chunk_x, rep = slice / a.chunk_y;
+  const int chunk = blockIdx.x % a.chunk_x * (kThreads >> a.lane_shift) + (threadIdx.x >> a.lane_shift);
+  int col = (slice % a.chunk_y * lanes + (threadIdx.x & (lanes - 1))) * 4;
   if (chunk >= a.chunks || col >= a.D) return;
+  if (FOUR) col = min(col, a.D - 4);  // the last four columns; a lane that shares some with its neighbour stores the same sums
   const uint32_t *keys = a.keys + (long long)rep * a.T, *pos = a.pos + (long long)rep * a.T;
   const T *src = dout + (long long)rep * a.T * a.D + col;
   float *table = a.dtable + rep * a.table_rs + col;
   float *part = a.part + ((long long)rep * a.chunks + chunk) * 2 * a.Dp + col;
-  const int first = chunk * kChunk, count = min(kChunk, a.T - first), left = a.D - col;
+  const int first = chunk * kChunk, count = min(kChunk, a.T - first);
   // Sixteen keys and positions as vectors.  Past the last chunk's end they are what lies behind the lists in scratch, and are not used.
   uint32_t k[kChunk + 1];
   u4 at[kChunk / 4];
@@ -261,11 +319,11 @@ __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArg
 #pragma unroll
   for (int j = 0; j < kChunk; ++j)
     if (j >= count) k[j] = 0xffffffffu;  // ends the run in front of it, and is none
-  decltype(load_raw<FOURS>(src, left)) v[kChunk];
+  decltype(load_raw<FOUR>(src, a.D)) v[kChunk];
 #pragma unroll
   for (int j = 0; j < kChunk; ++j) {
     const uint32_t row = k[j] < (uint32_t)a.V ? at[j / 4][j % 4] : 0;  // one that exists, and no branch
-    v[j] = load_raw<FOURS>(src + (long long)row * a.D, left);
+    v[j] = load_raw<FOUR>(src + (long long)row * a.D, a.D);
   }
   f4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -274,16 +332,13 @@ __global__ __launch_bounds__(kThreads) void k_embed_chunks(const T *dout, SumArg
     acc += widen(v[j]);
     const bool ends = k[j] != k[j + 1];
     if (ends || j + 1 == kChunk) {
-      if (ends && !from_before) {
-        float *to = table + (long long)k[j] * a.D;
-        acc *= a.scale;
-        if (FOURS || left >= 4) {
-          *(f4_any *)to = acc;
-        } else {
-          for (int e = 0; e < left; ++e) to[e] = acc[e];
-        }
+      const bool whole = ends && !from_before;
+      float *to = whole ? table + (long long)k[j] * a.D : part + (from_before ? 0 : a.Dp);
+      acc *= whole ? a.scale : 1.f;
+      if (FOUR) {
+        *(f4_any *)to = acc;
       } else {
-        *(f4 *)(part + (from_before ? 0 : a.Dp)) = acc;
+        for (int e = 0; e < a.D; ++e) to[e] = acc[e];
       }
       acc = f4{0.f, 0.f, 0.f, 0.f};
       from_before = false;
@@ -487,8 +542,13 @@ Scratch scratch_of(const parle_embed_desc &d) {
 
 template <int ITEMS>
 hipError_t sort_zero(hipStream_t st, const parle_embed_desc &d, int tiles, const int32_t *tokens, uint32_t *keys, uint32_t *pos,
-               float *dtable) {
-  const long long elems = (long long)d.vocab * d.dim;
+                     float *dtable, int &cleared) {
+  // A sort takes 2 us and, for each pass, 1.2 and 0.65 for each item of a thread; meanwhile the others clear 6 MB a microsecond.  What
+  // they leave is cleared beside the sums.  Rows of less than a vector are all cleared here.
+  const int passes = ceil_div(digits_of(d.vocab), kDigitBits);
+  const double most = 6e6 * (2. + passes * (1.2 + 0.65 * ITEMS)) / (4. * d.n * d.dim);
+  cleared = d.dim < 4 || most >= d.vocab ? d.vocab : (int)most;
+  const long long elems = (long long)cleared * d.dim;
   const int zero = (int)std::min<long long>(1024, std::max<long long>(1, d.n * elems / (4 * kSortThreads * 4)));
   static const hipError_t lds_ok =
       hipFuncSetAttribute((const void *)k_embed_sort_zero<ITEMS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sort_lds(ITEMS));
@@ -521,7 +581,8 @@ hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int
                     : d.tokens > 4 * kSortThreads ? sort_zero<8>
                     : d.tokens > kSortThreads     ? sort_zero<4>
                                                   : sort_zero<1>;
-  const hipError_t e = sort(st, d, tiles, tokens, keys, pos, dtable);
+  int cleared = 0;
+  const hipError_t e = sort(st, d, tiles, tokens, keys, pos, dtable, cleared);
   if (e != hipSuccess) return e;
   if (tiles > 1) {
     uint32_t *keys2 = (uint32_t *)(at + 2 * s.list), *pos2 = (uint32_t *)(at + 3 * s.list);
@@ -536,12 +597,15 @@ hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int
   a.table_rs = d.table_stride, a.T = d.tokens, a.V = d.vocab, a.D = d.dim, a.Dp = (int)s.Dp, a.chunks = s.chunks, a.scale = d.scale;
   const int groups = ceil_div(d.dim, 4);
   a.lane_shift = lane_shift_of(groups);
-  const dim3 grid(ceil_div(s.chunks, kThreads >> a.lane_shift), ceil_div(groups, 1 << a.lane_shift), d.n);
-  const bool fours = d.dim % 4 == 0;
+  a.chunk_x = ceil_div(s.chunks, kThreads >> a.lane_shift), a.chunk_y = ceil_div(groups, 1 << a.lane_shift);
+  a.chunk_blocks = a.chunk_x * a.chunk_y * d.n;
+  a.zero_first = cleared, a.zero_rows = std::max(1, std::min(kZeroRows, 8192 / d.dim));  // 32 KiB together
+  a.zero_blocks = ceil_div(d.vocab - cleared, a.zero_rows);
+  const int grid = a.chunk_blocks + a.zero_blocks * d.n;
   if (d.dtype)
-    (fours ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
+    (d.dim >= 4 ? k_embed_chunks<bf16_t, true> : k_embed_chunks<bf16_t, false>)<<<grid, kThreads, 0, st>>>((const bf16_t *)dout, a);
   else
-    (fours ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
+    (d.dim >= 4 ? k_embed_chunks<float, true> : k_embed_chunks<float, false>)<<<grid, kThreads, 0, st>>>((const float *)dout, a);
   k_embed_join<<<dim3(s.chunks - 1, ceil_div(d.dim, 4 * PARLE_WAVE), d.n), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }

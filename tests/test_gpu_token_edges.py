@@ -26,6 +26,36 @@ def test_embed_backward_limits(gpu, dtype, n, tokens, vocab, dim, same):
     assert (got[:, vocab * dim:] == 9.0).all()
 
 
+@pytest.mark.parametrize("kind", ["uniform", "tail", "same", "none"])
+@pytest.mark.parametrize("dtype,n,tokens,vocab,dim,gap", [
+    (1, 2, 600, 24001, 515, 1), (0, 1, 600, 3000000, 7, 0), (1, 2, 700, 6000, 2050, 2), (0, 2, 520, 1500, 9001, 3), (1, 1, 4100, 50001, 1024, 0), (1, 2, 1000, 3 << 20, 5, 3),
+    (0, 1, 17000, 60000, 1028, 0), (1, 2, 600, 1 << 22, 4, 1), (1, 1, 600, 1 << 22, 3, 0)])
+def test_embed_backward_long_tables(gpu, dtype, n, tokens, vocab, dim, gap, kind):
+    """Tables that are cleared beside the sums as well: the tokens' rows by the formula, zeros in all others, nothing behind a table."""
+    torch, pb = gpu
+    g = torch.Generator().manual_seed(11)
+    low = {"uniform": -1, "tail": vocab - 300, "same": vocab - 1, "none": vocab}[kind]
+    t = torch.randint(low, vocab + 1, (n, tokens), generator=g, dtype=torch.int32) if kind in ("uniform", "tail") else torch.full((n, tokens), low, dtype=torch.int32)
+    dout = randn(torch, 12, n, tokens, dim, dtype=dtype)
+    rs = vocab * dim + gap
+    desc = pb.parle_embed_desc(dtype, 0, n, tokens, vocab, dim, rs, 1.25)
+    got = torch.full((n, rs), 9.0, device="cuda")
+    pb.parle_k_embed_backward(desc, t.cuda(), dout, scratch(torch, pb.parle_k_embed_scratch_bytes(desc)), got)
+    assert (got[:, vocab * dim:] == 9.0).all(), "what lies behind the table was written"
+    for a in range(n):
+        rows, at = torch.unique(t[a].clamp(min=-1), return_inverse=True)
+        at = torch.where((t[a] >= 0) & (t[a] < vocab), at, -1)
+        want, mass, count = _embed_grad_reference(torch, at[None].int(), d64(dout[a:a + 1]), len(rows), 1.25)
+        kept = (rows >= 0) & (rows < vocab)
+        table = got[a, :vocab * dim].view(vocab, dim)
+        of = rows[kept].long().cuda()
+        # a sum of c terms in any order: c - 1 roundings at most on the way of each term, one more for the scale
+        within(table[of][None], want[:, kept], mass[:, kept] * (count[:, kept, None] + 1) * U, "dtable")
+        table[of] = 0.0
+        assert not table.any(), "a row without tokens is not zero"
+
+
+
 @pytest.mark.parametrize("out_dtype", [0, 1])
 @pytest.mark.parametrize("n,rows,cols,depth,b_block", [
     (1, 16, 40, 1024, 1), (1, 17, 40, 1024, 128), (1, 17, 130, 1025, 1), (2, 40, 70, 4224, 128), (1, 100, 520, 2048, 128), (3, 500, 260, 130, 1), (1, 16, 33, 2048, 128),
