@@ -17,8 +17,8 @@
 // 3 x 8192 tokens into 50001 x 512: 75 us, of them 25 for the sort with 127 MB of zeros, 44 for the sums with 180 MB of zeros (250 MB
 // together, 5.7 TB/s) and 7 for the joins; 78 with all zeros beside the sort.  1000 tokens into 100000 x 1024: 94 and 82.  Chunks of 8 or 32 take
 // the same or longer; rows to clear in 64 to 256 KiB a workgroup instead of 32: 77 to 80 and 83 to 85.
-// Up to kDirect tokens need none of this: every workgroup owns a few rows of the table, looks through all tokens for them, and writes its
-// rows whole, one launch at the rate of the stores (85 tokens into 25376 x 1652: 39 us in three launches, 31 in one).
+// Few tokens need none of this (in_one_launch): every workgroup owns a few rows of the table, looks through all tokens for them, sums
+// those rows and clears the others (20 tokens into 12000 x 1024: 11 us, 4.5 TB/s, against 15 in three launches).
 #include <algorithm>
 
 #include "tok.h"
@@ -236,8 +236,28 @@ __device__ __forceinline__ int first_not_below(const uint32_t *keys, int count, 
   return at;
 }
 
-// Clears those of zero_rows rows that no token has: their keys are sorted by now.  In vectors of 16 bytes of memory, wherever rows begin;
-// a row has four elements at least, so a vector lies in two rows at most.
+// Clears those of `rows` rows that are not `touched`, in vectors of 16 bytes of memory, wherever rows begin: misaligned stores of 16
+// bytes take twice as long.  A vector of a row of four elements or more lies in two rows at most.
+__device__ __forceinline__ void clear_others(float *table, int rows, int D, const uint8_t *touched) {
+  const int all = rows * D, before = (int)((uintptr_t)table / 4 % 4);  // elements of the first 16 bytes that are not the table's
+  constexpr int kStep = kThreads * 4;
+  const int step_rows = kStep / D, step_cols = kStep % D;
+  int e = (int)threadIdx.x * 4 - before, row = e < 0 ? -1 : e / D, col = e - row * D;
+  for (; e < all; e += kStep) {
+    const bool one = D >= 4 && e >= 0 && col + 4 <= D;  // in one row
+    if (D >= 4 && e >= 0 && e + 4 <= all && !touched[row] && !touched[one ? row : row + 1]) {
+      *(f4 *)(table + e) = f4{0.f, 0.f, 0.f, 0.f};
+    } else if (!one) {
+#pragma unroll 1
+      for (int i = max(e, 0); i < min(e + 4, all); ++i)
+        if (!touched[i / D]) table[i] = 0.f;
+    }
+    row += step_rows, col += step_cols;
+    if (col >= D) col -= D, ++row;
+  }
+}
+
+// Clears those of zero_rows rows that no token has: their keys are sorted by now.
 __device__ __forceinline__ void clear_rows(const SumArgs &a, int block) {
   __shared__ uint8_t touched[kZeroRows];
   __shared__ int bound[2];
@@ -252,23 +272,7 @@ __device__ __forceinline__ void clear_rows(const SumArgs &a, int block) {
   __syncthreads();
   for (int i = bound[0] + threadIdx.x; i < bound[1]; i += kThreads) touched[keys[i] - v0] = 1;
   __syncthreads();
-  float *table = a.dtable + rep * a.table_rs + (long long)v0 * a.D;
-  const int all = rows * a.D, before = (int)((uintptr_t)table / 4 % 4);  // elements of the first 16 bytes that are not the table's
-  constexpr int kStep = kThreads * 4;
-  const int step_rows = kStep / a.D, step_cols = kStep % a.D;
-  int e = (int)threadIdx.x * 4 - before, row = e < 0 ? -1 : e / a.D, col = e - row * a.D;
-  for (; e < all; e += kStep) {
-    const int next = min(row + (col + 3 >= a.D), rows - 1);
-    const bool first = touched[max(row, 0)], second = touched[next];
-    if (e >= 0 && e + 4 <= all && !first && !second) {
-      *(f4 *)(table + e) = f4{0.f, 0.f, 0.f, 0.f};
-    } else if (!first || !second) {
-      for (int k = 0; k < 4; ++k)
-        if (e + k >= 0 && e + k < all && !(col + k < a.D ? first : second)) table[e + k] = 0.f;
-    }
-    row += step_rows, col += step_cols;
-    if (col >= a.D) col -= a.D, ++row;
-  }
+  clear_others(a.dtable + rep * a.table_rs + (long long)v0 * a.D, rows, a.D, touched);
 }
 
 // Columns of a row of dout, as they came: four, or the `count` < 4 of a shorter row (the others' places are not used).
@@ -389,32 +393,18 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(SumArgs a) {
 // ---- gradient, few tokens ----
 constexpr int kDirect = 512, kDirectRows = 64;
 
-// Columns col .. col + 3 of a row, of which those from `from` to `to` - 1 exist; what comes in the others' places is not used.
-__device__ __forceinline__ f4 load4(const float *row, int col, int from, int to) {
-  const float *p = row + col;
-  if (to - from == 4) return *(const f4_any *)p;
-  return f4{p[min(max(0, from), to - 1)], p[min(max(1, from), to - 1)], p[min(max(2, from), to - 1)], p[min(max(3, from), to - 1)]};
-}
-__device__ __forceinline__ f4 load4(const bf16_t *row, int col, int from, int to) {
-  const bf16_t *p = row + col;
-  us4 v;
-  if (to - from == 4) {
-    v = *(const us4_any *)p;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = p[min(max(i, from), to - 1)];
-  }
-  return f4{bf16_to_f32(v.x), bf16_to_f32(v.y), bf16_to_f32(v.z), bf16_to_f32(v.w)};
-}
+__device__ __forceinline__ float value(const float *p) { return *p; }
+__device__ __forceinline__ float value(const bf16_t *p) { return bf16_to_f32(*p); }
 
-// `lanes` = 2^lane_shift threads per row; a workgroup owns `rows` rows of the table.  Rows of the table are written in the aligned
-// 16 bytes that they lie in, wherever they begin: misaligned stores of 16 bytes took twice as long.  grid: (V / rows, n)
+// A workgroup owns `rows` rows of the table: it clears those that no token has, and its wavefronts sum the others, 256 columns at a
+// time.  grid: (V / rows, n)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_embed_direct(const int32_t *tokens, const T *dout, int count, int V, int D, float scale,
-                                                           int rows, int lane_shift, float *dtable, long long table_rs) {
-  constexpr int kWaves = kThreads / PARLE_WAVE, kAhead = 8;
+                                                           int rows, float *dtable, long long table_rs) {
+  constexpr int kWaves = kThreads / PARLE_WAVE, kAhead = 16;
   __shared__ int hit[kDirect], sorted[kDirect];  // row of the workgroup's << 16 | position: by position, then by row and position
   __shared__ int start[kDirectRows + 1];         // of a row's hits
+  __shared__ uint8_t touched[kDirectRows];
   __shared__ int found[kDirect / kThreads][kWaves];
   const int rep = blockIdx.y, v0 = blockIdx.x * rows, mine = min(rows, V - v0);
   const int lane = threadIdx.x & (PARLE_WAVE - 1), wave = threadIdx.x / PARLE_WAVE;
@@ -452,34 +442,36 @@ __global__ __launch_bounds__(kThreads) void k_embed_direct(const int32_t *tokens
     start[threadIdx.x] = before;
   }
   __syncthreads();
-  const int lanes = 1 << lane_shift;
+  if ((int)threadIdx.x < mine) touched[threadIdx.x] = start[threadIdx.x] < start[threadIdx.x + 1];
+  __syncthreads();
   const T *src = dout + (long long)rep * count * D;
   float *table = dtable + rep * table_rs + (long long)v0 * D;
-  for (int r = threadIdx.x >> lane_shift; r < mine; r += kThreads >> lane_shift) {
-    float *row = table + (long long)r * D;
-    const int first = start[r], last = start[r + 1];
-    const int before = (int)((uintptr_t)row / 4 % 4);  // elements of the row's first 16 bytes that are not its
-    for (int col = (threadIdx.x & (lanes - 1)) * 4 - before; col < D; col += lanes * 4) {
-      const int from = max(0, -col), to = min(4, D - col);
+  if (hits > 0 && D >= 4) {
+    const int slices = (D + 4 * PARLE_WAVE - 1) / (4 * PARLE_WAVE);
+    for (int it = wave; it < mine * slices; it += kWaves) {
+      const int r = it / slices, first = start[r], last = start[r + 1], at = ((it - r * slices) * PARLE_WAVE + lane) * 4;
+      if (first == last || at >= D) continue;
+      const int col = min(at, D - 4);  // the last four columns; a lane that shares some with its neighbour stores the same sums
       f4 acc = {0.f, 0.f, 0.f, 0.f};
       for (int h = first; h < last; h += kAhead) {
-        f4 x[kAhead];
+        decltype(load_raw<true>(src, D)) x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) x[u] = load4(src + (long long)(sorted[min(h + u, last - 1)] & 0xffff) * D, col, from, to);
+        for (int u = 0; u < kAhead; ++u) x[u] = load_raw<true>(src + (long long)(sorted[min(h + u, last - 1)] & 0xffff) * D + col, D);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-          if (h + u < last) acc += x[u];
+          if (h + u < last) acc += widen(x[u]);
       }
-      acc *= scale;
-      if (to - from == 4) {
-        *(f4 *)(row + col) = acc;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e >= from && e < to) row[col + e] = acc[e];
-      }
+      *(f4_any *)(table + (long long)r * D + col) = acc * scale;
+    }
+  } else if (hits > 0) {
+    for (int i = threadIdx.x; i < mine * D; i += kThreads) {
+      const int r = i / D;
+      float acc = 0.f;
+      for (int h = start[r]; h < start[r + 1]; ++h) acc += value(src + (sorted[h] & 0xffff) * D + (i - r * D));
+      if (touched[r]) table[i] = acc * scale;
     }
   }
+  clear_others(table, mine, D, touched);
 }
 
 int lane_shift_of(int groups) {
@@ -512,16 +504,22 @@ hipError_t fwd(hipStream_t st, const parle_embed_desc &d, const void *table, con
 
 template <typename T>
 hipError_t direct(hipStream_t st, const parle_embed_desc &d, const int32_t *tokens, const void *dout, float *dtable) {
-  int shift = 3;  // 8 .. 256 lanes per row, 16 bytes side by side of each
-  while (shift < 8 && (4 << shift) < d.dim + 3) ++shift;
-  // Rows of 32 KiB together: fewer look through the tokens more often, more leave the frequent tokens to too few workgroups (25376 x 1652
-  // with 85 tokens: 35 us with 64 KiB, 31 with 32, 32 with 16, 38 with 8).  Workgroups enough for the chip where the table is small.
+  // Rows of 32 KiB together: fewer look through the tokens more often, more leave the frequent tokens to too few workgroups.
+  // Workgroups enough for the chip where the table is small.
   const long long all = (long long)d.vocab * d.n;
   const int rows = (int)std::max<long long>(1, std::min<long long>({8192 / d.dim, all / 2048, kDirectRows}));
   const dim3 grid(ceil_div(d.vocab, rows), d.n);
   k_embed_direct<T><<<grid, kThreads, 0, st>>>(
-      tokens, (const T *)dout, d.tokens, d.vocab, d.dim, d.scale, rows, shift, dtable, d.table_stride);
+      tokens, (const T *)dout, d.tokens, d.vocab, d.dim, d.scale, rows, dtable, d.table_stride);
   return hipGetLastError();
+}
+
+// One launch, where its workgroups' chains of waits cost less than two more launches: they have no part in many tokens, nor in many
+// rows.  us for one launch and for three, 4 MB of tables: 8 and 14 with 500 tokens; 15 MB: 14 and 16 with 256, 18 and 16 with 500; 49 MB: 14 and 16
+// with 128, 21 and 17 with 500; 102 MB: 21 and 22 with 32, 23 and 22 with 64; 148 MB: 33 and 32 with 32, 53 and 35 with 500.
+bool in_one_launch(const parle_embed_desc &d) {
+  const double bytes = 4. * d.n * d.vocab * d.dim;
+  return d.tokens <= kChunk || (d.tokens <= kDirect && d.tokens * bytes <= 6e9);
 }
 
 // Scratch: keys and positions (twice where tiles are merged), then the partial sums.
@@ -531,7 +529,7 @@ struct Scratch {
 };
 Scratch scratch_of(const parle_embed_desc &d) {
   Scratch s = {};
-  if (d.tokens <= kDirect) return s;
+  if (in_one_launch(d)) return s;
   s.list = round_up((long long)d.n * d.tokens * 4, 256);
   s.lists = d.tokens > kTile ? 4 : 2;
   s.Dp = round_up(d.dim, 8);
@@ -572,7 +570,7 @@ int64_t embed_scratch_bytes(const parle_embed_desc &d) {
 
 hipError_t launch_embed_bwd(hipStream_t st, const parle_embed_desc &d, const int32_t *tokens, const void *dout, void *scratch,
                             float *dtable) {
-  if (d.tokens <= kDirect) return d.dtype ? direct<bf16_t>(st, d, tokens, dout, dtable) : direct<float>(st, d, tokens, dout, dtable);
+  if (in_one_launch(d)) return d.dtype ? direct<bf16_t>(st, d, tokens, dout, dtable) : direct<float>(st, d, tokens, dout, dtable);
   const Scratch s = scratch_of(d);
   char *at = (char *)scratch;
   uint32_t *keys = (uint32_t *)at, *pos = (uint32_t *)(at + s.list);

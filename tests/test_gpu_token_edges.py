@@ -29,12 +29,15 @@ def test_embed_backward_limits(gpu, dtype, n, tokens, vocab, dim, same):
 @pytest.mark.parametrize("kind", ["uniform", "tail", "same", "none"])
 @pytest.mark.parametrize("dtype,n,tokens,vocab,dim,gap", [
     (1, 2, 600, 24001, 515, 1), (0, 1, 600, 3000000, 7, 0), (1, 2, 700, 6000, 2050, 2), (0, 2, 520, 1500, 9001, 3), (1, 1, 4100, 50001, 1024, 0), (1, 2, 1000, 3 << 20, 5, 3),
-    (0, 1, 17000, 60000, 1028, 0), (1, 2, 600, 1 << 22, 4, 1), (1, 1, 600, 1 << 22, 3, 0)])
+    (0, 1, 17000, 60000, 1028, 0), (1, 2, 600, 1 << 22, 4, 1), (1, 1, 600, 1 << 22, 3, 0),
+    # few tokens: on both sides of the rule for one launch, by tokens (16, 17) and by tokens times bytes
+    (1, 1, 16, 100000, 1024, 0), (0, 1, 17, 100000, 1024, 0), (0, 2, 100, 24001, 515, 1), (1, 2, 60, 24001, 515, 1), (1, 2, 64, 24001, 515, 2), (1, 2, 512, 700, 1023, 3),
+    (0, 2, 511, 400, 2, 1), (1, 2, 300, 401, 1, 2), (0, 2, 90, 1000, 3, 3), (1, 3, 200, 3001, 5, 2), (1, 1, 300, 20, 9001, 0)])
 def test_embed_backward_long_tables(gpu, dtype, n, tokens, vocab, dim, gap, kind):
     """Tables that are cleared beside the sums as well: the tokens' rows by the formula, zeros in all others, nothing behind a table."""
     torch, pb = gpu
     g = torch.Generator().manual_seed(11)
-    low = {"uniform": -1, "tail": vocab - 300, "same": vocab - 1, "none": vocab}[kind]
+    low = {"uniform": -1, "tail": max(0, vocab - 300), "same": vocab - 1, "none": vocab}[kind]
     t = torch.randint(low, vocab + 1, (n, tokens), generator=g, dtype=torch.int32) if kind in ("uniform", "tail") else torch.full((n, tokens), low, dtype=torch.int32)
     dout = randn(torch, 12, n, tokens, dim, dtype=dtype)
     rs = vocab * dim + gap
