@@ -47,12 +47,14 @@ __global__ __launch_bounds__(kThreads) void k_embed_fwd(const TI *table, long lo
     src[r] = table + rep * table_rs + (long long)(live[r] ? t : 0) * D;
   }
   TO *dst = out + ((long long)rep * T + first) * D;
-  for (int c = (threadIdx.x & (lanes - 1)) * kVec; c < D; c += lanes * kVec) {
+  const int count = min(D, kVec);
+  for (int at = (threadIdx.x & (lanes - 1)) * kVec; at < D; at += lanes * kVec) {
+    const int c = min(at, D - count);  // a row's last eight columns; a lane that shares some with its neighbour stores the same values
     float v[ROWS][kVec];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       if (live[r]) {
-        load8(src[r] + c, D - c, 0.f, v[r]);
+        load8(src[r] + c, count, 0.f, v[r]);
       } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[r][i] = 0.f;
@@ -65,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_fwd(const TI *table, long lo
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[r][i] *= scale;
       }
-      store8(dst + (long long)r * D + c, D - c, v[r]);
+      store8(dst + (long long)r * D + c, count, v[r]);
     }
   }
 }
