@@ -156,10 +156,13 @@ constexpr int kLaneXor1 = 0xb1, kLaneXor2 = 0x4e, kHalfMirror = 0x141, kRowMirro
 
 __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
 
-__device__ __forceinline__ float row_sum16(float v) {
+__device__ __forceinline__ float row_sum8(float v) {
   v += from_lane<kLaneXor1>(v);
   v += from_lane<kLaneXor2>(v);
-  v += from_lane<kHalfMirror>(v);
+  return v + from_lane<kHalfMirror>(v);
+}
+__device__ __forceinline__ float row_sum16(float v) {
+  v = row_sum8(v);
   return v + from_lane<kRowMirror>(v);
 }
 __device__ __forceinline__ float wave_sum_all(float v) {

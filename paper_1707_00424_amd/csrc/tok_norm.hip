@@ -6,7 +6,8 @@
 //
 // Both directions read a row once into registers, reduce over it, and write: what they must move is what they move, and memory bounds
 // them.  A row belongs to a group of LANES threads, each with CH vectors of eight elements, LANES * 8 elements apart; the fewest threads
-// whose registers hold a row are taken, so that most lanes have work and most rows are in flight.
+// whose registers hold a row are taken, so that most lanes have work and most rows are in flight (12.6 M elements bf16 in rows of 256: 17 us
+// with 32 threads a row, 24 with 64).
 // 8192 rows of 4096 bf16 forward: 47 us, 5.0 TB/s, the rate of a plain copy; 8 rows 4.4 us, latency.  3 x 4099 rows of 2048
 // backward: 47 us, 4.3 TB/s, 5 of them the join of dw; without the next row's loads ahead 57.
 #include <algorithm>
@@ -31,7 +32,14 @@ struct FwdArgs {
 // wavefront of the workgroup and call site).
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float *red) {
-  v = LANES == 16 ? row_sum16(v) : wave_sum_all(v);
+  if (LANES == 8)
+    v = row_sum8(v);
+  else if (LANES == 16)
+    v = row_sum16(v);
+  else if (LANES == 32)
+    v = row_sum16(v), v += __shfl_xor(v, 16, PARLE_WAVE);
+  else
+    v = wave_sum_all(v);
   if (LANES > PARLE_WAVE) {
     constexpr int kWaves = LANES / PARLE_WAVE;
     if ((threadIdx.x & (PARLE_WAVE - 1)) == 0) red[threadIdx.x / PARLE_WAVE] = v;
@@ -60,9 +68,8 @@ __device__ __forceinline__ void store_at(T *p, int D, const float (&v)[kVec]) {
   store8(p, TINY ? D : kVec, v);
 }
 
-// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  SHORT: rows of one scale, whose four bytes (one and
-// three of padding) are a dword.
-template <bool SHORT, bool TINY, typename T, typename W>
+// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  A row's scales are padded to four bytes.
+template <int LANES, bool TINY, typename T, typename W>
 __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const Place &p, float (&y)[kVec], T *yo) {
   if (yo && p.live()) store_at<TINY>(yo + row * a.D + p.at, a.D, y);
   if (!a.q) return;
@@ -88,10 +95,15 @@ __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const P
     *(u2 *)(a.q + row * a.pitch + col) = u2{codes4(c[0], c[1], c[2], c[3]), codes4(c[4], c[5], c[6], c[7])};
   }
   if ((threadIdx.x & 15) != 0) return;
-  if (SHORT)  // one scale and the row's padding
-    *(uint32_t *)(a.scales + row * a.s_pitch) = sb;
-  else if ((col >> 7) < a.s_pitch)
-    a.scales[row * a.s_pitch + (col >> 7)] = left > 0 ? sb : 0;
+  uint8_t *scale = a.scales + row * a.s_pitch + (col >> 7);
+  if (LANES == 16) {  // one scale, and three bytes of padding
+    *(uint32_t *)scale = sb;
+  } else if (LANES == 32) {  // two, and two of padding
+    *scale = left > 0 ? sb : 0;
+    if (col > 0) *(uint16_t *)(scale + 1) = 0;
+  } else if ((col >> 7) < a.s_pitch) {
+    *scale = left > 0 ? sb : 0;
+  }
 }
 
 // A row in the registers of LANES threads, sixteen or four rows to a workgroup of 256 where LANES is 16 or a wavefront.
@@ -136,7 +148,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const
     load_at<TINY>(w + p.at, a.D, g);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) y[i] = v[c][i] * rs * g[i];
-    emit<LANES == 16, TINY, T, W>(a, row, p, y, yo);
+    emit<LANES, TINY, T, W>(a, row, p, y, yo);
   }
 }
 
@@ -176,7 +188,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fwd_long(const T *x, const T *
     load_at<false>(w + p.at, a.D, g);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = v[i] * rs * g[i];
-    emit<false, false, T, W>(a, row, p, v, yo);
+    emit<kLanes, false, T, W>(a, row, p, v, yo);
   }
 }
 
@@ -355,14 +367,18 @@ hipError_t fwd(hipStream_t st, const parle_norm_desc &d, const void *x, const vo
   a.w = (const W *)w, a.w_rs = d.w_stride, a.q = q, a.scales = scales, a.rstd = rstd;
   a.rows = d.rows, a.D = d.dim, a.pitch = (int)round_up(d.dim, 16), a.s_pitch = (int)round_up(ceil_div(d.dim, 128), 4), a.eps = d.eps;
   // whole scales and their padding: the threads of a row cover as much
-  const int D = q && d.dim > 128 ? 128 * a.s_pitch : d.dim;
+  const int D = q && d.dim > 256 ? 128 * a.s_pitch : d.dim;
 #define PARLE_NORM(LANES, CH, TINY)                                                                                             \
   k_rmsnorm_fwd<T, W, LANES, CH, TINY><<<dim3(ceil_div(d.rows, (LANES < 256 ? 256 : LANES) / LANES), d.n), LANES < 256 ? 256 : LANES, \
                                    0, st>>>((const T *)x, (const T *)resid, (T *)h, (T *)y, a)
   if (D < kVec)
     PARLE_NORM(16, 1, true);
+  else if (D <= 8 * kVec && !q)  // with q, sixteen threads find a scale
+    PARLE_NORM(8, 1, false);
   else if (D <= 16 * kVec)
     PARLE_NORM(16, 1, false);
+  else if (D <= 32 * kVec)
+    PARLE_NORM(32, 1, false);
   else if (D <= 64 * kVec)
     PARLE_NORM(64, 1, false);
   else if (D <= 64 * kVec * 2)
@@ -401,8 +417,12 @@ hipError_t bwd(hipStream_t st, const parle_norm_desc &d, const void *h, const vo
   if (strips > 0) {
     if (d.dim < kVec)
       PARLE_NORM(16, 1, true);
+    else if (d.dim <= 8 * kVec)
+      PARLE_NORM(8, 1, false);
     else if (d.dim <= 16 * kVec)
       PARLE_NORM(16, 1, false);
+    else if (d.dim <= 32 * kVec)
+      PARLE_NORM(32, 1, false);
     else if (d.dim <= 64 * kVec)
       PARLE_NORM(64, 1, false);
     else if (d.dim <= 64 * kVec * 2)

@@ -82,7 +82,7 @@ def test_fp8_matmul_limits(gpu, out_dtype, n, rows, cols, depth, b_block):
     assert torch.equal(again, out), "two calls differ"
 
 
-@pytest.mark.parametrize("dim", [16, 127, 128, 129, 512, 513, 1024, 1536, 2047, 4096, 16384, 16385])
+@pytest.mark.parametrize("dim", [3, 8, 16, 63, 127, 128, 129, 200, 256, 257, 512, 513, 1024, 1536, 2047, 4096, 16384, 16385])
 def test_rmsnorm_scales_and_padding(gpu, dim):
     """Codes, scales and their padding at every row length's kernel; nothing behind them is written."""
     torch, pb = gpu

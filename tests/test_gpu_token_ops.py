@@ -338,7 +338,7 @@ def test_linear_layer_gradients(gpu):
 
 @pytest.mark.parametrize("dtype,w_dtype", [(0, 0), (1, 0), (1, 1), (0, 1)])
 @pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 3, 7), (1, 5, 64), (3, 17, 129), (2, 4, 513), (1, 6, 1000), (2, 3, 1025), (1, 2, 2049), (1, 3, 4104), (1, 2, 8192), (1, 2, 8193),
-                                        (1, 2, 16384), (1, 2, 20001)])
+                                        (1, 2, 16384), (1, 2, 20001), (2, 37, 8), (2, 70, 57), (2, 33, 200), (1, 20, 256), (1, 3, 257)])
 def test_rmsnorm_forward(gpu, dtype, w_dtype, n, rows, dim):
     torch, pb = gpu
     eps = 1e-6
@@ -401,7 +401,7 @@ def test_rmsnorm_non_finite(gpu):
 
 
 @pytest.mark.parametrize("dtype,w_dtype", [(0, 0), (1, 0), (1, 1), (0, 1)])
-@pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 3, 7), (1, 50, 64), (3, 17, 129), (2, 40, 513), (1, 6, 1000), (2, 300, 1025), (1, 3, 4104), (1, 5, 8193), (1, 3, 20001), (2, 2000, 40)])
+@pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 3, 7), (1, 50, 64), (3, 17, 129), (2, 40, 513), (1, 6, 1000), (2, 300, 1025), (1, 3, 4104), (1, 5, 8193), (1, 3, 20001), (2, 2000, 40), (2, 37, 8), (1, 70, 57), (2, 33, 200), (3, 2500, 256), (1, 9, 257)])
 def test_rmsnorm_backward(gpu, dtype, w_dtype, n, rows, dim):
     torch, pb = gpu
     ws = dim + 1
