@@ -32,15 +32,16 @@ struct Values;
 template <>
 struct Values<float> {
   float v[kVec][kVec];
-  // Row j, of which `count` values exist; EIGHTS: all or none of them.
-  template <bool EIGHTS>
-  __device__ __forceinline__ void load(int j, const float *p, int count) {
-    if (EIGHTS && count < kVec) {
+  __device__ __forceinline__ void load(int j, const float *p) { load8(p, kVec, 0.f, v[j]); }
+  __device__ __forceinline__ void load(int j, const float *p, int count) { load8(p, count, 0.f, v[j]); }
+  // Row j without its first `skip` values, zeros behind.
+  __device__ __forceinline__ void shift(int j, int skip) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) v[j][i] = 0.f;
-    } else {
-      load8(p, EIGHTS ? kVec : count, 0.f, v[j]);
-    }
+    for (int s = 1; s <= kVec; s *= 2)
+      if (skip & s || (s == kVec && skip > s)) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[j][i] = i + s < kVec ? v[j][i + s] : 0.f;
+      }
   }
   __device__ __forceinline__ float at(int j, int i) const { return v[j][i]; }
   // Bits of the largest magnitudes, of row j and of the columns.
@@ -70,18 +71,18 @@ template <>
 struct Values<bf16_t> {
   typedef unsigned short us2 __attribute__((ext_vector_type(2)));
   u4 row[kVec];  // pairs of columns
-  template <bool EIGHTS>
+  __device__ __forceinline__ void load(int j, const bf16_t *p) { row[j] = __builtin_bit_cast(u4, (us8)*(const us8_any *)p); }
   __device__ __forceinline__ void load(int j, const bf16_t *p, int count) {
-    if (count >= kVec) {
-      row[j] = __builtin_bit_cast(u4, (us8)*(const us8_any *)p);
-    } else if (EIGHTS) {
-      row[j] = u4{0, 0, 0, 0};
-    } else {
-      us8 x;
+    us8 x;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) x[i] = i < count ? p[i] : (bf16_t)0;
-      row[j] = __builtin_bit_cast(u4, x);
-    }
+    for (int i = 0; i < kVec; ++i) x[i] = i < count ? p[i] : (bf16_t)0;
+    row[j] = __builtin_bit_cast(u4, x);
+  }
+  __device__ __forceinline__ void shift(int j, int skip) {
+    if (skip & 1) row[j] = u4{row[j][0] >> 16 | row[j][1] << 16, row[j][1] >> 16 | row[j][2] << 16, row[j][2] >> 16 | row[j][3] << 16, row[j][3] >> 16};
+    if (skip & 2) row[j] = u4{row[j][1], row[j][2], row[j][3], 0};
+    if (skip & 4) row[j] = u4{row[j][2], row[j][3], 0, 0};
+    if (skip >= kVec) row[j] = u4{0, 0, 0, 0};
   }
   __device__ __forceinline__ float at(int j, int i) const { return __uint_as_float(i & 1 ? row[j][i / 2] & 0xffff0000u : row[j][i / 2] << 16); }
   static __device__ __forceinline__ uint32_t most2(uint32_t a, uint32_t b) {
@@ -158,17 +159,34 @@ __device__ __forceinline__ void slow_tile(const T *from, const Args &a, int rep,
 }
 
 // grid: (column tiles, row tiles, n).  Thread: columns 8 lane16 .. + 7, rows 8 group .. + 7 of the tile.
-template <typename T, bool ROWS, bool EIGHTS>
+template <typename T, bool ROWS>
 __global__ __launch_bounds__(kThreads) void k_fp8_quantize(const T *src, Args a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[kTile * kPitch];
   __shared__ uint32_t most_of[kWaves][kTile];
   const int r0 = blockIdx.y * kTile, c0 = blockIdx.x * kTile, rep = blockIdx.z;
   const int lane16 = threadIdx.x & 15, group = threadIdx.x >> 4, wave = threadIdx.x / PARLE_WAVE;
-  const int c = c0 + lane16 * kVec, r = r0 + group * kVec, left = a.cols - c;
-  const T *from = src + rep * a.stride + c;
+  const int c = c0 + lane16 * kVec, r = r0 + group * kVec;
   Values<T> x;
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) x.template load<EIGHTS>(j, from + (long long)min(r + j, a.rows - 1) * a.ld, r + j < a.rows ? left : 0);
+  for (int j = 0; j < kVec; ++j) {
+    const T *row = src + rep * a.stride + (long long)min(r + j, a.rows - 1) * a.ld;
+    if (a.cols >= kVec)
+      x.load(j, row + min(c, a.cols - kVec));
+    else
+      x.load(j, row, c == 0 ? a.cols : 0);
+  }
+  // Behind the matrix are zeros.  Whatever loads got there is put right afterwards: a guard splits the wavefront, and each load waits
+  // for the one before.
+  const int skip = a.cols >= kVec ? max(0, c - (a.cols - kVec)) : 0;
+  if (skip > 0) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x.shift(j, skip);
+  }
+  if (r + kVec > a.rows) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (r + j >= a.rows) x.shift(j, kVec);
+  }
   // largest magnitudes: of rows over 16 lanes, of columns over the groups of a wavefront, then over wavefronts
   uint32_t row_most[kVec], col_most[kVec], tile_most = 0;
   bool special = false;
@@ -258,10 +276,7 @@ __global__ __launch_bounds__(kThreads) void k_fp8_quantize(const T *src, Args a)
 
 template <typename T, bool ROWS>
 void run(hipStream_t st, dim3 grid, const void *src, const Args &a) {
-  if (a.cols % kVec == 0)
-    k_fp8_quantize<T, ROWS, true><<<grid, kThreads, 0, st>>>((const T *)src, a);
-  else
-    k_fp8_quantize<T, ROWS, false><<<grid, kThreads, 0, st>>>((const T *)src, a);
+  k_fp8_quantize<T, ROWS><<<grid, kThreads, 0, st>>>((const T *)src, a);
 }
 
 }  // namespace
