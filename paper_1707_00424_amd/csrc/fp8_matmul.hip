@@ -101,9 +101,9 @@ __device__ __forceinline__ void tile_of(int id, int rows, int cols, int &m, int 
 // units work on the other half.  Loads, reads and products are interleaved by hand and pinned: left alone, the compiler moves all
 // products of a step behind its reads.
 // 8192 x 8192 x 4096 (bf16 result): 413 us with tiles of 128 x 128 and no overlap, 302 with 256 x 256 pipelined, 242 with results stored in
-// 16 bytes a lane, scales through LDS and two wavefronts on a SIMD, each with 128 x 64 of the tile.  One launch alone takes 220 us, 2.5
-// PFLOP/s: the matrix units are busy 73 % of the time at the 1.6 GHz that the power limit leaves, no LDS bank conflicts.  A fp32
-// result: 430 us, 1.28 PFLOP/s.  A loop over tiles in one workgroup, its loads running into the next tile, gained nothing: the
+// 16 bytes a lane, scales through LDS and two wavefronts on a SIMD, each with 128 x 64 of the tile; 220 on operands that the caches
+// hold, 2.5 PFLOP/s: the matrix units are busy 73 % of the time at the 1.6 GHz that the power limit leaves, LDS bank conflicts (reads of
+// scales) 3 %.  A fp32 result: 407 us, 1.35 PFLOP/s.  A loop over tiles in one workgroup, its loads running into the next tile, gained nothing: the
 // wait for loads waits for the last tile's stores as well.
 template <typename TO, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
