@@ -71,7 +71,8 @@ BAD = {
               (dict(classes=(1 << 22) + 1, ld=1 << 23), pb.PARLE_ESIZE), (dict(rows=(1 << 21) + 1), pb.PARLE_ESIZE), (dict(ld=1 << 39), pb.PARLE_ESIZE)],
 }
 # positions of pointers that may be NULL (scratch where these small sizes want none, y where q is given)
-MAY_BE_NULL = {"parle_k_rmsnorm_forward": {1, 3, 4, 7}, "parle_k_rmsnorm_backward": {4}, "parle_k_fp8_matmul": {4, 5}, "parle_k_logprob_forward": {2, 4, 5, 6},
+# scratch among them where a call of these sizes needs none
+MAY_BE_NULL = {"parle_k_embed_backward": {2}, "parle_k_rmsnorm_forward": {1, 3, 4, 7}, "parle_k_rmsnorm_backward": {4}, "parle_k_fp8_matmul": {4, 5}, "parle_k_logprob_forward": {2, 4, 5, 6},
                "parle_k_logprob_backward": {5}}
 
 
@@ -118,6 +119,11 @@ def test_scratch():
             ptrs = CALLS[call][1]
             status, text = _call(call, make(), *ptrs[:at], size - 1, *ptrs[at + 1:])
             assert status == pb.PARLE_ESIZE and "scratch" in text
+    # a call that needs scratch refuses NULL, one that needs none is asked for none
+    many = embed(tokens=600)
+    assert pb.parle_k_embed_scratch_bytes(many) > 0 and pb.parle_k_embed_scratch_bytes(embed()) == 0
+    status, text = _call("parle_k_embed_backward", many, P, P, None, BIG, P)
+    assert status == pb.PARLE_EINVAL and "scratch" in text
     # more tokens, rows or classes never want less than a part of them
     assert pb.parle_k_embed_scratch_bytes(embed(tokens=1 << 20)) > pb.parle_k_embed_scratch_bytes(embed(tokens=1 << 14)) > 0
     assert pb.parle_k_logprob_scratch_bytes(logprob(n=1, rows=4, classes=128000, ld=128000, top=20)) > 0
