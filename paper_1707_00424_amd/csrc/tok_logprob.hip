@@ -29,7 +29,7 @@ using namespace tok;
 constexpr int kThreads = 256, kWaves = kThreads / PARLE_WAVE;
 constexpr int kList = 1024, kVectors = 512;  // candidates, and vectors that hold any
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kFloor = -1e30f;
+constexpr float kNear = 1e6f, kFloor = -kNear;
 constexpr int kGroup = kThreads * kVec;  // classes of one vector per thread
 
 // Order of floats as unsigned integers; -0 counts as 0, so that equal values have equal keys.
@@ -65,9 +65,10 @@ struct Stats {
 };
 
 // The same while a thread reads its values, in base 2: an element costs one multiply-add, v log2 e - m2, in front of the
-// exponential.  m2 is m log2 e rounded; what the rounding took is put back once, at the end.  m starts at kFloor rather than -inf, so that
-// no difference of infinities arises: values below it count as nothing, and a part without larger ones is summed again by
-// slow_stats.
+// exponential.  m2 is m log2 e rounded; what the rounding took is put back once, at the end.  It is an exponent's error until then, 2^-4 at
+// kNear and 2^9 at 1e10, so this holds for maxima between kFloor and kNear.  m starts at kFloor rather than -inf, so that no difference of
+// infinities arises either: values below it count as nothing.  A part whose largest value lies outside is summed again by slow_stats, whatever
+// came out here; inside, a thread that holds only values below kFloor adds e^-(10^6), nothing, to those of the others.
 struct Running {
   float m = kFloor, m2 = kFloor * kLog2e, z = 0.f, t = 0.f;
   __device__ __forceinline__ void raise(float to) {
@@ -83,7 +84,6 @@ struct Running {
   }
   __device__ __forceinline__ Stats result() const {
     Stats s;
-    if (z == 0.f) return s;
     const float r = __builtin_fmaf(m, kLog2e, -m2), f = exp2_of(-r);
     s.m = m, s.z = z * f, s.t = (t - z * r) * f * kLn2;
     return s;
@@ -204,16 +204,25 @@ __device__ __forceinline__ float most_of(const R &x) {
 __device__ __forceinline__ float logit_at(const bf16_t *x, int i) { return bf16_to_f32(x[i]); }
 __device__ __forceinline__ float logit_at(const float *x, int i) { return x[i]; }
 
-// Statistics of a part whose largest value lies below kFloor: differences are taken before they are scaled.  For classes c0 .. c1 - 1.
+// Statistics of a part whose largest value m is far from zero: differences are taken before they are scaled.  For elements j0 .. j1 - 1.
 template <typename T>
-__device__ __forceinline__ Stats slow_stats(const T *x, int c0, int c1, float m) {
+__device__ __forceinline__ Stats slow_stats(const Row<T> &row, int j0, int j1, float m) {
+  constexpr int kAhead = 2;
   Stats s;
   s.m = m;
 #pragma unroll 1
-  for (int c = c0 + threadIdx.x; c < c1; c += kThreads) {
-    const float d = logit_at(x, c) - m, e = exp_of(d);
-    s.z += e;
-    s.t += e * fmaxf(d, kFloor);
+  for (int j = j0 + threadIdx.x * kVec; j < j1; j += kAhead * kGroup) {
+    Raw<T> raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) raw[u] = fetch(row, j + u * kGroup, j + u * kGroup < j1);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float d = raw[u].at(i) - m, e = exp_of(d);
+        s.z += e;
+        s.t += e * fmaxf(d, kFloor);
+      }
   }
   return s;
 }
@@ -350,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_fwd(const T *logits, FwdAr
   }
   Stats s = block_join(lds, run.result());
   const int c0 = max(j0 - row.off, 0), c1 = j1 - row.off;  // the part's classes
-  if (!(s.m > kFloor)) {  // nothing larger anywhere in the part: the same for all threads
+  if (!(s.m > kFloor && s.m <= kNear)) {  // s.m is the part's largest value, or kFloor: the same for all threads
     const float w = wave_max_all(most);
     __syncthreads();
     if (lane == 0) lds.part[threadIdx.x / PARLE_WAVE].pad = w;
@@ -359,7 +368,10 @@ __global__ __launch_bounds__(kThreads) void k_logprob_fwd(const T *logits, FwdAr
 #pragma unroll
     for (int w2 = 1; w2 < kWaves; ++w2) all = fmaxf(all, lds.part[w2].pad);
     __syncthreads();
-    if (all > -INFINITY) s = block_join(lds, slow_stats(x, c0, c1, all));
+    if (all > -INFINITY)
+      s = block_join(lds, slow_stats(row, j0, j1, all));
+    else if (s.z == 0.f)
+      s = Stats();  // nothing there; a NaN beside nothing stays
   }
   const int label = a.logp && a.splits == 1 ? a.labels[row_at] : -1;
   const long long slot = row_at * a.splits + blockIdx.x;
