@@ -461,12 +461,13 @@ typedef struct {
 } parle_norm_desc;
 /* h = x + resid (rounded to dtype; resid NULL: h = x), rstd = 1 / sqrt(mean_i h_i^2 + eps), y = w * h * rstd, row by row.
  * h, y, rstd [n][rows] and the pair q, scales (y with a scale for 1 x 128 values, quantised from fp32) may each be
- * NULL; y or q is wanted. */
+ * NULL; y or q is wanted.  h and y may each be x or resid, written over; they are not one buffer. */
 parle_status parle_k_rmsnorm_forward(void *hip_stream, const parle_norm_desc *desc, const void *x, const void *resid,
                                      const void *w, void *h, void *y, uint8_t *q, uint8_t *scales, float *rstd);
 /* From h and rstd of the forward pass and dout = dy:  g = dout * w,  dx = rstd * (g - h * rstd^2 * mean_i(g_i h_i)) + dresid
  * (the gradient of x and of resid; dresid, the gradient that h receives elsewhere, may be NULL),
- * dw [n][dim] fp32 (rows w_stride apart) = sum over the rows of dout * h * rstd, in a fixed order. */
+ * dw [n][dim] fp32 (rows w_stride apart) = sum over the rows of dout * h * rstd, in a fixed order.  dx may be h, dout or dresid,
+ * written over. */
 parle_status parle_k_rmsnorm_backward(void *hip_stream, const parle_norm_desc *desc, const void *h, const void *w,
                                       const float *rstd, const void *dout, const void *dresid, void *scratch,
                                       int64_t scratch_bytes, void *dx, float *dw);

@@ -150,6 +150,7 @@ parle_status parle_k_rmsnorm_forward(void *hip_stream, const parle_norm_desc *de
   if (desc->rows == 0) return PARLE_OK;
   c.given(x, "x is NULL").given(w, "w is NULL").maybe(resid).maybe(h).maybe(y).maybe(q).maybe(scales).maybe(rstd);
   c.field(y || q, "one of y and q is wanted").field(!q == !scales, "q and scales come together");
+  c.field(!h || h != y, "h and y are one buffer");
   if (c.status) return c.status;
   return c.launched(launch_rmsnorm_fwd((hipStream_t)hip_stream, *desc, x, resid, w, h, y, q, scales, rstd));
 }

@@ -10,6 +10,11 @@
 // with 32 threads a row, 24 with 64).
 // 8192 rows of 4096 bf16 forward: 47 us, 5.0 TB/s, the rate of a plain copy; 8 rows 4.4 us, latency.  3 x 4099 rows of 2048
 // backward: 47 us, 4.3 TB/s, 5 of them the join of dw; without the next row's loads ahead 57.
+//
+// Results may be written over what they come from (h or y over x or resid, dx over h, dout or dresid).  Threads at a row's end load
+// elements that are their neighbours' too (Place), so those are not stored before the barrier in the row's sum, which a thread reaches once
+// it has loaded its part of every input.  (All of h behind the barrier: 6000 rows of 8191 bf16 80 -> 85 us, as their stores start later.)
+// The kernels of long rows read twice, and each thread only what it writes itself.
 #include <algorithm>
 
 #include "tok.h"
@@ -68,20 +73,10 @@ __device__ __forceinline__ void store_at(T *p, int D, const float (&v)[kVec]) {
   store8(p, TINY ? D : kVec, v);
 }
 
-// y of one vector: stored, and as codes; 16 lanes hold the 128 values of a scale.  A row's scales are padded to four bytes.
-template <int LANES, bool TINY, typename T, typename W>
-__device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const Place &p, float (&y)[kVec], T *yo) {
-  if (yo && p.live()) store_at<TINY>(yo + row * a.D + p.at, a.D, y);
-  if (!a.q) return;
-  const int col = p.col, left = a.D - col;
-  if (p.skip > 0) {  // the vector's own elements to its front
-#pragma unroll
-    for (int s = 1; s < kVec; s *= 2)
-      if (p.skip & s) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) y[i] = i + s < kVec ? y[i + s] : 0.f;
-      }
-  }
+// Columns col .. col + 7 of y as codes; 16 lanes hold the 128 values of a scale.  A row's scales are padded to four bytes.
+template <int LANES, typename W>
+__device__ __forceinline__ void put_codes(const FwdArgs<W> &a, long long row, int col, const float (&y)[kVec]) {
+  const int left = a.D - col;
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) most = max(most, i < left ? finite_bits(y[i]) : 0u);
@@ -106,6 +101,22 @@ __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const P
   }
 }
 
+// y of one vector: stored, and as codes.
+template <int LANES, bool TINY, typename T, typename W>
+__device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const Place &p, float (&y)[kVec], T *yo) {
+  if (yo && p.live()) store_at<TINY>(yo + row * a.D + p.at, a.D, y);
+  if (!a.q) return;
+  if (p.skip > 0) {  // the vector's own elements to its front
+#pragma unroll
+    for (int s = 1; s < kVec; s *= 2)
+      if (p.skip & s) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) y[i] = i + s < kVec ? y[i + s] : 0.f;
+      }
+  }
+  put_codes<LANES, W>(a, row, p.col, y);
+}
+
 // A row in the registers of LANES threads, sixteen or four rows to a workgroup of 256 where LANES is 16 or a wavefront.
 template <typename T, typename W, int LANES, int CH, bool TINY>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
@@ -128,15 +139,24 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const
 #pragma unroll
       for (int i = 0; i < kVec; ++i) v[c][i] = stored<T>(v[c][i] + u[c][i]);
   }
+  // Elements of two threads lie in the last sixteen columns; a wavefront by itself stores behind its own loads.
+  const auto store_h = [&](bool shared) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const Place p = place(c);
+      if (h && live && p.live() && (LANES > PARLE_WAVE && p.col + 2 * kVec > a.D) == shared) store_at<TINY>(h + row * a.D + p.at, a.D, v[c]);
+    }
+  };
+  store_h(false);
   float sum = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const Place p = place(c);
-    if (h && live && p.live()) store_at<TINY>(h + row * a.D + p.at, a.D, v[c]);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) sum += i >= p.skip ? v[c][i] * v[c][i] : 0.f;
   }
   sum = row_sum<LANES>(sum, red);
+  if (LANES > PARLE_WAVE) store_h(true);
   const float rs = 1.0f / sqrtf(sum / (float)a.D + a.eps);
   if (a.rstd && live && lane == 0) a.rstd[row] = rs;
   const W *w = a.w + rep * a.w_rs;
@@ -152,7 +172,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const
   }
 }
 
-// Rows longer than the registers of 1024 threads: read twice.  (`h`, where it is given, holds the sum on the second read.)
+// Rows longer than the registers of 1024 threads: read twice, the second time from `h` where it is given.
 template <typename T, typename W>
 __global__ __launch_bounds__(1024) void k_rmsnorm_fwd_long(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
   constexpr int kLanes = 1024;
@@ -177,18 +197,19 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fwd_long(const T *x, const T *
   if (a.rstd && threadIdx.x == 0) a.rstd[row] = rs;
   const W *w = a.w + blockIdx.y * a.w_rs;
   for (int col = threadIdx.x * kVec; col < padded; col += kLanes * kVec) {
-    const Place p(col, a.D);
+    const int left = a.D - col;
     float v[kVec], u[kVec], g[kVec];
-    load_at<false>(x + row * a.D + p.at, a.D, v);
-    if (resid) {
-      load_at<false>(resid + row * a.D + p.at, a.D, u);
+    load8((h ? h : x) + row * a.D + col, left, 0.f, v);
+    if (resid && !h) {
+      load8(resid + row * a.D + col, left, 0.f, u);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) v[i] = stored<T>(v[i] + u[i]);
     }
-    load_at<false>(w + p.at, a.D, g);
+    load8(w + col, left, 0.f, g);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = v[i] * rs * g[i];
-    emit<kLanes, false, T, W>(a, row, p, v, yo);
+    if (yo) store8(yo + row * a.D + col, left, v);
+    if (a.q) put_codes<kLanes, W>(a, row, col, v);
   }
 }
 
@@ -436,8 +457,9 @@ hipError_t bwd(hipStream_t st, const parle_norm_desc &d, const void *h, const vo
     else if (d.dim <= kLongest)
       PARLE_NORM(1024, 2, false);
     else {
-      k_rmsnorm_bwd_long<T, W><<<dim3(d.rows, d.n), 1024, 0, st>>>((const T *)h, (const T *)dout, (const T *)dresid, (T *)dx, a);
+      // dw first: dx may be written over what it reads
       k_rmsnorm_dw_long<T, W><<<dim3(ceil_div(d.dim, 256 * kVec), strips, d.n), 256, 0, st>>>((const T *)h, (const T *)dout, a);
+      k_rmsnorm_bwd_long<T, W><<<dim3(d.rows, d.n), 1024, 0, st>>>((const T *)h, (const T *)dout, (const T *)dresid, (T *)dx, a);
     }
   }
 #undef PARLE_NORM
