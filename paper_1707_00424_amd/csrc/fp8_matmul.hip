@@ -9,7 +9,9 @@
 // and 2^2 is not; the same with and without scales).  For normally distributed operands that is about 2e-5 of the result, a hundredth
 // of the rounding of a result in bf16.  A result in fp32, such as the gradient of a parameter, is to have fp32 sums: there the codes
 // become bf16 numbers times their scale, which is exact, and the bf16 instructions add them without such a cut, at half
-// the rate.  (A scale of 2^-127 counts as 0 in that conversion.)
+// the rate.  So do the products of up to 16 rows whatever their result, as loads bound them (4 x 8192 x 4096: 10.6 us with the 8-bit
+// instructions, 10.9 without).
+// (A scale of 2^-127 counts as 0 in that conversion.)
 #include <algorithm>
 
 #include "igemm_dev.h"
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
 // rows of b and add their parts in LDS, in order.
 constexpr int kRowsWaves = 8;
 
-template <typename TO, bool EXACT, int SPLIT>
+template <typename TO, int SPLIT>
 __global__ __launch_bounds__(kRowsWaves *PARLE_WAVE) void k_fp8_rows(Args g) {
   constexpr int kAhead = 4;  // steps whose loads are on their way together
   __shared__ f4 part[kRowsWaves][PARLE_WAVE];
@@ -316,14 +318,10 @@ __global__ __launch_bounds__(kRowsWaves *PARLE_WAVE) void k_fp8_rows(Args g) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (step + u >= last) break;
-      if (EXACT) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(fb[u][2 * j], fb[u][2 * j + 1], scale_value(xb[u])),
-                                                        eight_bf16(fa[u][2 * j], fa[u][2 * j + 1], scale_value(xa[u])), acc, 0, 0, 0);
-      } else {
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, 0, 0, 0, xb[u], 0, xa[u]);
-      }
+      for (int j = 0; j < 4; ++j)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(fb[u][2 * j], fb[u][2 * j + 1], scale_value(xb[u])),
+                                                      eight_bf16(fa[u][2 * j], fa[u][2 * j + 1], scale_value(xa[u])), acc, 0, 0, 0);
     }
   }
   if (SPLIT > 1) {
@@ -384,7 +382,7 @@ hipError_t run_tile(hipStream_t st, const Args &g, int replicas, int splits = 1)
 template <typename TO, int SPLIT>
 hipError_t run_rows(hipStream_t st, const Args &g, int replicas) {
   const dim3 grid(ceil_div(g.N, 16 * (kRowsWaves / SPLIT)), replicas);
-  k_fp8_rows<TO, sizeof(TO) == 4, SPLIT><<<grid, kRowsWaves * PARLE_WAVE, 0, st>>>(g);
+  k_fp8_rows<TO, SPLIT><<<grid, kRowsWaves * PARLE_WAVE, 0, st>>>(g);
   return hipGetLastError();
 }
 
