@@ -11,7 +11,7 @@
 // become bf16 numbers times their scale, which is exact, and the bf16 instructions add them without such a cut, at half
 // the rate.  So do the products of up to 16 rows whatever their result, as loads bound them (4 x 8192 x 4096: 10.6 us with the 8-bit
 // instructions, 10.9 without).
-// (A scale of 2^-127 counts as 0 in that conversion.)
+// (The conversion takes a scale's exponent, 2^-127 too.  Values below 2^-126 become multiples of 2^-133, the smallest bf16 number.)
 #include <algorithm>
 
 #include "igemm_dev.h"
@@ -55,7 +55,7 @@ __device__ __forceinline__ bf8 eight_bf16(int lo, int hi, float scale) {
   const bf2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return bf8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
-// 2^(byte - 127) of a scale dword's lowest byte
+// 2^(byte - 127) of a scale dword's lowest byte, for the conversions: they read the exponent's bits, so that zeros there are 2^-127
 __device__ __forceinline__ float scale_value(int s) { return __uint_as_float(((uint32_t)s & 0xffu) << 23); }
 
 // Results of 16 columns from n on, of which the two halves of a wavefront hold four in turn (registers 4 j .. 4 j + 7 of the product):
