@@ -117,7 +117,7 @@ __device__ __forceinline__ void emit(const FwdArgs<W> &a, long long row, const P
   put_codes<LANES, W>(a, row, p.col, y);
 }
 
-// A row in the registers of LANES threads, sixteen or four rows to a workgroup of 256 where LANES is 16 or a wavefront.
+// A row in the registers of LANES threads, 256 / LANES rows to a workgroup where LANES is less than that.
 template <typename T, typename W, int LANES, int CH, bool TINY>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rmsnorm_fwd(const T *x, const T *resid, T *h, T *yo, FwdArgs<W> a) {
   constexpr int kBlock = LANES < 256 ? 256 : LANES;
@@ -418,11 +418,17 @@ hipError_t fwd(hipStream_t st, const parle_norm_desc &d, const void *x, const vo
   return hipGetLastError();
 }
 
+// Rows that a workgroup of the gradient kernel takes at a time, by the threads that the dispatch below gives a row.
+int rows_at_once(int dim) {
+  const int lanes = dim < kVec ? 16 : dim <= 8 * kVec ? 8 : dim <= 16 * kVec ? 16 : dim <= 32 * kVec ? 32 : 64;
+  return dim <= 64 * kVec * 2 ? 256 / lanes : 1;
+}
 // Strips of the gradient kernel: workgroups enough for the chip, and no more parts of dw than that needs (3 x 4099 x 2048: 53 us with 512
-// workgroups, 51 with 768, 49 with 1024, 56 with 1536).
+// workgroups, 51 with 768, 49 with 1024, 56 with 1536).  A strip is whole turns of a workgroup, or some of its threads never have a row
+// (20000 x 33 bf16: 9.8 us with strips of 20 rows, 7.9 with 32).
 int strip_rows(const parle_norm_desc &d) {
-  const int want = std::max(1, 1024 / d.n);
-  return std::max(1, std::max(ceil_div(d.rows, want), d.dim <= 64 * kVec * 2 ? 16 : 2));
+  const int want = std::max(1, 1024 / d.n), at_once = rows_at_once(d.dim);
+  return (int)round_up(std::max(ceil_div(d.rows, want), at_once > 1 ? 16 : 2), at_once);
 }
 
 template <typename T, typename W>
