@@ -423,11 +423,13 @@ int rows_at_once(int dim) {
   const int lanes = dim < kVec ? 16 : dim <= 8 * kVec ? 8 : dim <= 16 * kVec ? 16 : dim <= 32 * kVec ? 32 : 64;
   return dim <= 64 * kVec * 2 ? 256 / lanes : 1;
 }
-// Strips of the gradient kernel: workgroups enough for the chip, and no more parts of dw than that needs (3 x 4099 x 2048: 53 us with 512
-// workgroups, 51 with 768, 49 with 1024, 56 with 1536).  A strip is whole turns of a workgroup, or some of its threads never have a row
+// Strips of the gradient kernel: workgroups enough for the chip, and no more parts of dw than that needs.  bf16, 512 workgroups and 1024:
+// 8192 x 2048 30.2 and 30.0 us, 3 x 4099 x 2048 53 and 49, 40000 x 200 16.4 and 17.3; but 2000 x 4096 17.7 and 21.3, 16384 x 4096 111 and 119,
+// 2000 x 5000 22.4 and 27.3, 4096 x 8192 57 and 63, 2000 x 16384 65 and 75, as a part of a wide row is more to write
+// and to read again.  2048 take longer than 1024 everywhere (8192 x 2048 35.2, 100000 x 64 15.1 for 13.5).  A strip is whole turns of a workgroup, or some of its threads never have a row
 // (20000 x 33 bf16: 9.8 us with strips of 20 rows, 7.9 with 32).
 int strip_rows(const parle_norm_desc &d) {
-  const int want = std::max(1, 1024 / d.n), at_once = rows_at_once(d.dim);
+  const int want = std::max(1, (d.dim > 256 * kVec ? 512 : 1024) / d.n), at_once = rows_at_once(d.dim);
   return (int)round_up(std::max(ceil_div(d.rows, want), at_once > 1 ? 16 : 2), at_once);
 }
 
