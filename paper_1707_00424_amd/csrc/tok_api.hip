@@ -49,7 +49,7 @@ bool good(Check &c, const parle_embed_desc *d) {
       .field(d->table_stride >= (int64_t)d->vocab * d->dim, "table_stride is less than vocab * dim");
   if (c.status) return false;
   c.that(d->vocab <= kMostRows && d->table_stride <= kMostElems / d->n, PARLE_ESIZE, "vocab exceeds 2^22 or n * table_stride 2^40")
-      .that(d->tokens <= kMostRows, PARLE_ESIZE, "tokens exceeds 2^22")
+      .that(d->tokens <= kMostRows && d->dim <= kMostRows, PARLE_ESIZE, "tokens or dim exceeds 2^22")
       .that((long long)d->n * d->tokens <= kMostElems / d->dim, PARLE_ESIZE, "n * tokens * dim exceeds 2^40");
   return c.status == PARLE_OK;
 }

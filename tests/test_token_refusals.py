@@ -1,5 +1,5 @@
 """CPU-only: calls of the token-model operators that are refused for their buffers or the last of their sizes, and scratch by the row."""
-from test_token_api import P, _call, norm, pb
+from test_token_api import P, _call, embed, norm, pb
 
 OTHER = P + 0x1000
 
@@ -16,3 +16,13 @@ def test_norm_gradient_has_a_row_for_every_thread():
             parts = pb.parle_k_rmsnorm_scratch_bytes(norm(n=1, rows=rows, dim=dim, w_stride=dim)) // (4 * (-(-dim // 8) * 8))
             strip = next(k for k in range(1, rows + at_once + 1) if -(-rows // k) <= parts)        # the fewest rows that a part may have
             assert parts <= -(-rows // at_once) and (parts == 1 or -(-rows // (-(-strip // at_once) * at_once)) == parts), (dim, rows, parts)
+
+
+def test_embed_refuses_rows_that_its_loops_do_not_count():
+    for dim in (2 ** 31 - 1, 2 ** 31 - 2048, (1 << 22) + 1):
+        d = embed(n=1, tokens=1, vocab=1, dim=dim, table_stride=dim)
+        assert pb.parle_k_embed_scratch_bytes(d) == -1, dim
+        for name, ptrs in (("parle_k_embed_forward", (P, P, P)), ("parle_k_embed_backward", (P, P, None, 0, P))):
+            status, text = _call(name, d, *ptrs)
+            assert status == pb.PARLE_ESIZE and "2^22" in text
+    assert pb.parle_k_embed_scratch_bytes(embed(n=1, tokens=1, vocab=1, dim=1 << 22, table_stride=1 << 22)) == 0
