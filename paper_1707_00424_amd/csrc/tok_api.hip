@@ -35,8 +35,8 @@ struct Check {
   }
 };
 
-// Rows, columns, tokens: a grid of as many workgroups of 1024 threads is the largest that a launch takes, and a tile of 256
-// rows of codes is addressed with 32-bit offsets.
+// Rows, columns, tokens: a launch counts its threads in x in 32 bits, 1024 for a row at most, and a tile of 256 rows of codes is
+// addressed with 32-bit offsets.
 constexpr long long kMostRows = 1LL << 22;
 constexpr long long kMostElems = 1LL << 40;
 
@@ -63,6 +63,7 @@ bool good(Check &c, const parle_norm_desc *d) {
       .field(d->eps >= 0.f && d->eps < 3e38f, "eps is negative or not finite");
   if (c.status) return false;
   c.that(d->rows <= kMostRows && d->dim <= kMostRows, PARLE_ESIZE, "rows or dim exceeds 2^22")
+      .that(d->rows < kMostRows || d->dim <= 4096, PARLE_ESIZE, "rows of more than 4096 elements exceed 2^22 - 1")
       .that(d->w_stride <= kMostElems / d->n && (long long)d->n * d->rows <= kMostElems / d->dim, PARLE_ESIZE,
             "a tensor exceeds 2^40 elements");
   return c.status == PARLE_OK;

@@ -26,3 +26,13 @@ def test_embed_refuses_rows_that_its_loops_do_not_count():
             status, text = _call(name, d, *ptrs)
             assert status == pb.PARLE_ESIZE and "2^22" in text
     assert pb.parle_k_embed_scratch_bytes(embed(n=1, tokens=1, vocab=1, dim=1 << 22, table_stride=1 << 22)) == 0
+
+
+def test_norm_refuses_a_grid_beyond_a_launch():
+    """A launch takes less than 2^32 threads; rows of more than 4096 elements have 1024 each."""
+    for dim, rows, ok in ((4096, 1 << 22, True), (4097, 1 << 22, False), (4097, (1 << 22) - 1, True), (20000, 1 << 22, False)):
+        d = norm(n=1, rows=rows, dim=dim, w_stride=dim)
+        assert (pb.parle_k_rmsnorm_scratch_bytes(d) >= 0) == ok, (dim, rows)
+        if not ok:
+            status, text = _call("parle_k_rmsnorm_forward", d, P, None, P, OTHER, None, P, P, None)
+            assert status == pb.PARLE_ESIZE and "2^22 - 1" in text
