@@ -282,7 +282,7 @@ __global__ __launch_bounds__(WM *WN *PARLE_WAVE) void k_fp8_tile(Args g) {
   }
 }
 
-// Up to 16 rows of a: what counts is reading b once, at the rate of memory (4 x 8192 x 4096: 9.1 us, 3.7 TB/s; a tile of 128 rows took 30).  A wavefront multiplies 16 rows of b with all of a over its
+// Up to 16 rows of a: what counts is reading b once, at the rate of memory (4 x 8192 x 4096: 9.6 us, 3.5 TB/s; a tile of 128 rows took 30).  A wavefront multiplies 16 rows of b with all of a over its
 // share of the contraction, straight from memory into fragments and with no barrier; SPLIT wavefronts of a workgroup share a group of 16
 // rows of b and add their parts in LDS, in order.
 constexpr int kRowsWaves = 8;

@@ -14,8 +14,8 @@
 //      to scratch.  More workgroups clear the rest of the table, except for the rows that the sorted keys name: sums wait for
 //      keys and rows, and leave the memory to them.
 //   3. Runs of several chunks are joined, chunk by chunk in order.
-// 3 x 8192 tokens into 50001 x 512: 75 us, of them 25 for the sort with 127 MB of zeros, 44 for the sums with 180 MB of zeros (250 MB
-// together, 5.7 TB/s) and 7 for the joins; 78 with all zeros beside the sort.  1000 tokens into 100000 x 1024: 94 and 82.  Chunks of 8 or 32 take
+// 3 x 8192 tokens into 50001 x 512: 75 us, of them 26 for the sort with 127 MB of zeros, 42 for the sums with 180 MB of zeros (250 MB
+// together, 5.9 TB/s) and 7 for the joins; 78 with all zeros beside the sort.  1000 tokens into 100000 x 1024: 94 and 82.  Chunks of 8 or 32 take
 // the same or longer; rows to clear in 64 to 256 KiB a workgroup instead of 32: 77 to 80 and 83 to 85.
 // Few tokens need none of this (in_one_launch): every workgroup owns a few rows of the table, looks through all tokens for them, sums
 // those rows and clears the others (20 tokens into 12000 x 1024: 11 us, 4.5 TB/s, against 15 in three launches).

@@ -5,8 +5,8 @@
 // Odd numbers of classes put rows anywhere; vectors are taken at 16-byte boundaries of memory, whatever the row's.  A row belongs to one
 // workgroup, or to several that each take a part of the classes where rows are few; a second, small kernel joins parts.
 //
-// 4096 rows of 50001 bf16 with 5 alternatives: 93 us, 4.4 TB/s; memory bounds it, with exponentials close behind (one per element at a quarter
-// of the vector unit's rate: about 60 us).  Four rows of 128000 with 20: 7.7 + 4.8 us, latency.  The gradient, a pass that reads and
+// 4096 rows of 50001 bf16 with 5 alternatives: 94 us, 4.4 TB/s; reading alone would take 58, and the vector unit's work 53 (per element an
+// exponential at a quarter of its rate, 21 us together, and six instructions beside it): the two overlap in part.  Four rows of 128000 with 20: 7.7 + 4.8 us, latency.  The gradient, a pass that reads and
 // writes: 6144 rows of 32000 in 139 us, 5.6 TB/s.
 //
 // Alternatives.  Every thread notes the largest value of its vectors and which vector holds it.  The `top`-th best of those
