@@ -528,6 +528,94 @@ parle_status parle_k_logprob_backward(void *hip_stream, const parle_logprob_desc
                                       void *dlogits);
 int64_t parle_k_logprob_scratch_bytes(const parle_logprob_desc *desc); /* -1 on a bad descriptor */
 
+/* ------------------------------------------------------------------------------------------
+ * Attention and sampling: what lets a token see others, and what answers with one.  The rules of the operators above hold here too.
+ *
+ * Rows are tokens, n blocks of them; a row holds `heads` heads of `dim` elements one behind the other, rows of q, of k and v, and of out are
+ * ld_q, ld_kv and ld_out elements apart.  So q, k and v may be three parts of the rows that one linear layer leaves, and dq, dk and dv parts of
+ * the gradient's.  Query head h reads key and value head h / (heads / kv_heads).  What lies between the heads of two rows is not touched.
+ * ------------------------------------------------------------------------------------------ */
+#define PARLE_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t dtype;                      /* of x, out */
+  int32_t n, tokens, heads, dim;
+  int32_t axes;                       /* positions of a token, 1 .. PARLE_ROPE_MAX_AXES */
+  int32_t pairs[PARLE_ROPE_MAX_AXES]; /* pairs of a head's elements that turn with each axis, those of the first axis first; 2 * their sum P <= dim */
+  int32_t interleaved;                /* pair p is elements p and p + P (0), or 2 p and 2 p + 1 (1) */
+  int32_t inverse;                    /* 1: turned back, which is the gradient */
+  int64_t ld, stride;                 /* elements of x from token to token (>= heads * dim) and from replica to replica */
+  int64_t ld_out, out_stride;         /* of out */
+} parle_rope_desc;
+/* Rotary positions: each pair (a, b) of a head turns by t = position * freqs[p], its axis' position in positions [n][tokens][axes], freqs [P] fp32:
+ * (a cos t - b sin t, a sin t + b cos t).  The angle is formed and reduced in 64 bits, so far positions are as exact as near ones.  Elements
+ * from 2 P on are copied.  out may be x, in the same layout. */
+parle_status parle_k_rope(void *hip_stream, const parle_rope_desc *desc, const void *x, const int32_t *positions, const float *freqs, void *out);
+
+#define PARLE_ATTENTION_MAX_DIM 128
+#define PARLE_ATTENTION_MAX_SINKS 128
+typedef struct {
+  int32_t dtype;                 /* of q, k, v, out and their gradients */
+  int32_t n, tokens;
+  int32_t sequences;             /* of a replica, one behind the other in its rows */
+  int32_t heads, kv_heads, dim;  /* heads a multiple of kv_heads; dim a multiple of 8, <= PARLE_ATTENTION_MAX_DIM */
+  int32_t window, sinks;         /* token i of a sequence sees token j where j <= i and (j > i - window or j < sinks); window 0: every j <= i */
+  float scale;                   /* of the products of q and k, > 0 */
+  int64_t ld_q, q_stride;        /* elements from row to row (>= heads * dim) and from replica to replica, of q and dq */
+  int64_t ld_kv, kv_stride;      /* of k, v, dk and dv (>= kv_heads * dim) */
+  int64_t ld_out, out_stride;    /* of out and dout */
+} parle_attention_desc;
+/* out = softmax(scale * q k^T over the tokens seen) v, lse [n][heads][tokens] fp32 its log sum of exponentials (may be NULL).  Sequence b of
+ * replica a has rows offsets[a][b] .. offsets[a][b + 1] - 1, offsets [n][sequences + 1] ascending from 0 at least to `tokens` at most; NULL, with
+ * one sequence, is all rows.  Rows outside get out 0 and lse -inf.  A token that is not seen has no influence, whatever it holds; a NaN or an infinity in a
+ * value that is seen makes NaN (or that infinity) of its column of out.  Of the probabilities, bf16 tensors have their products with v in bf16, sums are fp32. */
+parle_status parle_k_attention_forward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
+                                       const int32_t *offsets, void *out, float *lse);
+/* With P = e^(scale * q k^T - lse) of the forward pass, delta = sum_d dout * out and dS = P * (dout v^T - delta):
+ * dq = scale * dS k,  dk = scale * dS^T q,  dv = P^T dout, those of a shared head summed over its query heads in a fixed order; rows outside of every
+ * sequence get zeros.  P and dS meet their products in the tensors' format. */
+parle_status parle_k_attention_backward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
+                                        const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch,
+                                        int64_t scratch_bytes, void *dq, void *dk, void *dv);
+int64_t parle_k_attention_scratch_bytes(const parle_attention_desc *desc); /* of the backward call; -1 on a bad descriptor */
+
+/* Caches for answers token by token: k_cache, v_cache [sequences][kv_heads][capacity][dim] of dtype.  Token p of a sequence lies in slot p where
+ * p < sinks, else in slot sinks + (p - sinks) % (capacity - sinks): a cache of sinks + window slots serves sequences of any length, one of as
+ * many slots as a sequence has tokens holds them in order.  Where capacity - sinks is less than the window, it is the window. */
+typedef struct {
+  int32_t dtype;                 /* of q, k, v, out and the caches */
+  int32_t sequences, capacity;   /* sinks < capacity */
+  int32_t heads, kv_heads, dim, window, sinks; /* as above */
+  float scale;
+  int64_t ld_q, ld_kv, ld_out;   /* elements from row to row; a row is a sequence's new token, in the store call one token of a prompt */
+} parle_cache_desc;
+/* The rows of k and v that belong to sequence b, offsets[b] .. offsets[b + 1] - 1 (offsets [sequences + 1] ascending, of `tokens` rows), go into its
+ * slots as its last tokens: lengths[b] tokens behind the call.  Of more rows than the cache keeps, the first sinks and the newest are stored. */
+parle_status parle_k_attention_store(void *hip_stream, const parle_cache_desc *desc, int32_t tokens, const void *k, const void *v,
+                                     const int32_t *offsets, const int32_t *lengths, void *k_cache, void *v_cache);
+/* One new token of every sequence: its k and v rows go into the caches (NULL: they are there), and its q sees what the window and the sinks
+ * leave of lengths[b] tokens, itself the last of them.  A sequence of length 0 or less gets out 0 and its caches stay. */
+parle_status parle_k_attention_decode(void *hip_stream, const parle_cache_desc *desc, const void *q, const void *k, const void *v,
+                                      const int32_t *lengths, void *scratch, int64_t scratch_bytes, void *k_cache, void *v_cache, void *out);
+int64_t parle_k_decode_scratch_bytes(const parle_cache_desc *desc); /* -1 on a bad descriptor */
+
+typedef struct {
+  int32_t dtype; /* of logits */
+  int32_t n, rows, classes;
+  int64_t ld;    /* elements from row to row, >= classes */
+} parle_sample_desc;
+/* One class of every row of logits [n][rows, ld] from its number uniform [n][rows] in [0, 1).  Row by row, temperature, top_k, top_p and min_p are
+ * arrays [n][rows] (int32 for top_k), each NULL where it is not wanted.  With w = e^((logit - largest) / temperature) and the classes above -inf in order of
+ * falling logit, the lower class first where two are equal: the first top_k stay (top_k <= 0: all); of those the shortest beginning whose sum of w is at
+ * least top_p times that of all that stayed (top_p >= 1: all of them); of those the ones with w >= min_p.  At least one stays.  The token is the first whose sum of w
+ * with those before it exceeds uniform times the whole sum.  temperature <= 0 takes the first class.  kept: how many stayed; logp: the logarithm of the
+ * token's share of their sum; both may be NULL.  w is counted in whole multiples of 2^-s, s the
+ * largest up to 50 with classes * 2^s <= 2^62.
+ * A row of -inf only gives token -1, kept 0 and logp -inf; a row with a NaN token -1, kept 0 and logp NaN; +inf leaves the classes that have it, evenly. */
+parle_status parle_k_sample(void *hip_stream, const parle_sample_desc *desc, const void *logits, const float *uniform, const float *temperature,
+                            const int32_t *top_k, const float *top_p, const float *min_p, void *scratch, int64_t scratch_bytes, int32_t *tokens,
+                            int32_t *kept, float *logp);
+int64_t parle_k_sample_scratch_bytes(const parle_sample_desc *desc); /* -1 on a bad descriptor */
+
 #ifdef __cplusplus
 }
 #endif

@@ -82,6 +82,26 @@ class parle_logprob_desc(C.Structure):
     _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "rows", "classes", "top")] + [("ld", C.c_int64)]
 
 
+class parle_rope_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "tokens", "heads", "dim", "axes")] + [
+        ("pairs", C.c_int32 * 4), ("interleaved", C.c_int32), ("inverse", C.c_int32)] + [
+        (k, C.c_int64) for k in ("ld", "stride", "ld_out", "out_stride")]
+
+
+class parle_attention_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "tokens", "sequences", "heads", "kv_heads", "dim", "window", "sinks")] + [
+        ("scale", C.c_float)] + [(k, C.c_int64) for k in ("ld_q", "q_stride", "ld_kv", "kv_stride", "ld_out", "out_stride")]
+
+
+class parle_cache_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "sequences", "capacity", "heads", "kv_heads", "dim", "window", "sinks")] + [
+        ("scale", C.c_float)] + [(k, C.c_int64) for k in ("ld_q", "ld_kv", "ld_out")]
+
+
+class parle_sample_desc(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "n", "rows", "classes")] + [("ld", C.c_int64)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -147,11 +167,24 @@ _SIGNATURES = {
                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
     "parle_k_logprob_backward": [C.c_void_p, C.POINTER(parle_logprob_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_rope": [C.c_void_p, C.POINTER(parle_rope_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_attention_forward": [C.c_void_p, C.POINTER(parle_attention_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p],
+    "parle_k_attention_backward": [C.c_void_p, C.POINTER(parle_attention_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_attention_store": [C.c_void_p, C.POINTER(parle_cache_desc), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_void_p],
+    "parle_k_attention_decode": [C.c_void_p, C.POINTER(parle_cache_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p],
+    "parle_k_sample": [C.c_void_p, C.POINTER(parle_sample_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                       C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p],
 }
 _SCRATCH_BYTES = {
     "parle_k_conv_scratch_bytes": parle_conv_desc, "parle_k_layer_scratch_bytes": parle_act_desc,
     "parle_k_embed_scratch_bytes": parle_embed_desc, "parle_k_rmsnorm_scratch_bytes": parle_norm_desc,
     "parle_k_fp8_scratch_bytes": parle_fp8_desc, "parle_k_logprob_scratch_bytes": parle_logprob_desc,
+    "parle_k_attention_scratch_bytes": parle_attention_desc, "parle_k_decode_scratch_bytes": parle_cache_desc,
+    "parle_k_sample_scratch_bytes": parle_sample_desc,
 }
 EXPORTS = sorted(list(_SIGNATURES) + list(_SCRATCH_BYTES) + ["parle_last_error", "parle_destroy"])
 
@@ -436,6 +469,54 @@ def parle_k_logprob_forward(desc, logits, labels, scratch, logp, entropy, lse, t
 def parle_k_logprob_backward(desc, logits, labels, lse, entropy, dlogp, dentropy, dlogits, stream=None):
     _check(lib().parle_k_logprob_backward(_stream_handle(stream), C.byref(desc), _ptr(logits), _ptr(labels), _ptr(lse),
                                           _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits)))
+
+
+def make_rope_desc(dtype, n, tokens, heads, dim, pairs, interleaved, inverse, ld, stride, ld_out, out_stride) -> parle_rope_desc:
+    """``pairs``: the pairs of each axis, one to four of them."""
+    pairs = list(pairs)
+    return parle_rope_desc(dtype, n, tokens, heads, dim, len(pairs), (C.c_int32 * 4)(*(pairs + [0] * (4 - len(pairs)))), interleaved, inverse,
+                           ld, stride, ld_out, out_stride)
+
+
+def parle_k_rope(desc, x, positions, freqs, out, stream=None):
+    _check(lib().parle_k_rope(_stream_handle(stream), C.byref(desc), _ptr(x), _ptr(positions), _ptr(freqs), _ptr(out)))
+
+
+def parle_k_attention_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_attention_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_attention_forward(desc, q, k, v, offsets, out, lse, stream=None):
+    _check(lib().parle_k_attention_forward(_stream_handle(stream), C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(offsets), _ptr(out),
+                                           _ptr(lse)))
+
+
+def parle_k_attention_backward(desc, q, k, v, offsets, out, lse, dout, scratch, dq, dk, dv, stream=None):
+    _check(lib().parle_k_attention_backward(_stream_handle(stream), C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(offsets), _ptr(out),
+                                            _ptr(lse), _ptr(dout), _ptr(scratch), _nbytes(scratch), _ptr(dq), _ptr(dk), _ptr(dv)))
+
+
+def parle_k_attention_store(desc, tokens, k, v, offsets, lengths, k_cache, v_cache, stream=None):
+    _check(lib().parle_k_attention_store(_stream_handle(stream), C.byref(desc), int(tokens), _ptr(k), _ptr(v), _ptr(offsets), _ptr(lengths),
+                                         _ptr(k_cache), _ptr(v_cache)))
+
+
+def parle_k_decode_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_decode_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_attention_decode(desc, q, k, v, lengths, scratch, k_cache, v_cache, out, stream=None):
+    _check(lib().parle_k_attention_decode(_stream_handle(stream), C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(lengths), _ptr(scratch),
+                                          _nbytes(scratch), _ptr(k_cache), _ptr(v_cache), _ptr(out)))
+
+
+def parle_k_sample_scratch_bytes(desc) -> int:
+    return int(lib().parle_k_sample_scratch_bytes(C.byref(desc)))
+
+
+def parle_k_sample(desc, logits, uniform, temperature, top_k, top_p, min_p, scratch, tokens, kept, logp, stream=None):
+    _check(lib().parle_k_sample(_stream_handle(stream), C.byref(desc), _ptr(logits), _ptr(uniform), _ptr(temperature), _ptr(top_k),
+                                _ptr(top_p), _ptr(min_p), _ptr(scratch), _nbytes(scratch), _ptr(tokens), _ptr(kept), _ptr(logp)))
 
 
 class Parle:

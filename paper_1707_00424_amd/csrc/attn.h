@@ -1,0 +1,229 @@
+// Shared pieces of the attention kernels: fragments of the matrix instructions, tiles in LDS, where a row's sequence lies.
+//
+// Everything is multiplied in transposed form, S^T = K Q^T and O^T = V^T P^T, so that a lane owns a query (its column of the
+// 32 x 32 accumulators: lane l holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in register i).  A row's maximum and sum are then
+// register sums and one exchange between the halves of the wavefront, and P^T, as it leaves the accumulators, is the second operand of the
+// next product: its eight values of a lane stand for keys 16 t + 8 (j / 4) + 4 (l / 32) + j % 4, and the first operand is read in that order.
+#pragma once
+#include "tok.h"
+
+namespace attn {
+
+using tok::u4;
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v lds_s4v;
+typedef u4 u4_any __attribute__((aligned(2)));
+
+constexpr int kWaves = 4, kThreads = kWaves * PARLE_WAVE;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Eight elements of a contraction.
+template <typename T>
+struct Frag {
+  u4 v[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Frag<T> zero_frag() {
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) f.v[i] = u4{0u, 0u, 0u, 0u};
+  return f;
+}
+template <typename T>
+__device__ __forceinline__ Frag<T> load_frag(const T *p) {
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) f.v[i] = *(const u4_any *)((const char *)p + 16 * i);
+  return f;
+}
+__device__ __forceinline__ float frag_at(const Frag<float> &f, int j) { return __uint_as_float(f.v[j >> 2][j & 3]); }
+__device__ __forceinline__ float frag_at(const Frag<bf16_t> &f, int j) {
+  const uint32_t w = f.v[0][j >> 1];
+  return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+}
+// Eight fp32 values as a fragment: bf16 products take P and dS rounded to nearest even, which is half a step, 2^-9 of each, at random signs.
+template <typename T>
+__device__ __forceinline__ Frag<T> make_frag(const float (&v)[8]);
+template <>
+__device__ __forceinline__ Frag<float> make_frag<float>(const float (&v)[8]) {
+  Frag<float> f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = __float_as_uint(v[j]);
+  return f;
+}
+template <>
+__device__ __forceinline__ Frag<bf16_t> make_frag<bf16_t>(const float (&v)[8]) {
+  Frag<bf16_t> f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f.v[0][j] = f32x2_to_bf16x2(v[2 * j], v[2 * j + 1]);
+  return f;
+}
+
+// acc[row of a][column of b] += sum over sixteen contraction values: eight of each half of the wavefront.
+__device__ __forceinline__ void mma(const Frag<bf16_t> &a, const Frag<bf16_t> &b, f16v &acc) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a.v[0]), __builtin_bit_cast(bf8, b.v[0]), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(const Frag<float> &a, const Frag<float> &b, f16v &acc) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(frag_at(a, j), frag_at(b, j), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f16v zero16() {
+  f16v z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// A tile of rows in LDS, kDP elements each, in 16-byte chunks whose place in the row is XORed with bits of the row, so that neither a chunk of sixteen
+// rows nor 32 columns of four rows meet in a bank.
+template <typename T, int DP>
+struct Tile {
+  static constexpr int kPitch = DP == 96 ? 128 : DP;             // elements of a row
+  static constexpr int kChunk = 16 / sizeof(T);                  // elements of a chunk
+  static constexpr int kRowBytes = kPitch * sizeof(T);
+  static __device__ __forceinline__ int turn(int r) {
+    if (sizeof(T) == 4) return (((r >> 2) & 1) << 3) | (((r >> 3) & 1) << 2) | (r & 3);
+    if (kPitch == 64) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return ((r & 3) << 2) | ((r >> 2) & 3);
+  }
+  static __device__ __forceinline__ int at(int r, int chunk) { return r * kRowBytes + ((chunk ^ turn(r)) << 4); }
+  // elements 8 c .. 8 c + 7 of row r
+  static __device__ __forceinline__ Frag<T> row(const char *tile, int r, int c) {
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) f.v[i] = *(const u4 *)(tile + at(r, c * ((int)sizeof(T) / 2) + i));
+    return f;
+  }
+  // column 32 db + l % 32 of rows r0 + 8 (j / 4) + 4 (l / 32) + j % 4, j = 0 .. 7; r0 a multiple of 16
+  static __device__ __forceinline__ Frag<T> column(const char *tile, int r0, int db, int lane) {
+    Frag<T> f;
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 4) {
+      const int d = 32 * db + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        f.v[j >> 2][j & 3] = *(const uint32_t *)(tile + at(r0 + 8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + 4 * (d & 3));
+    } else {
+      // a transposing read: lane l of sixteen addresses row l / 4, columns 4 (l % 4) .. + 3 of a 4 x 16 block and receives its column l
+      const int r = r0 + 4 * h + ((lane & 15) >> 2), d = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + at(r, d >> 3) + 2 * (d & 7)));
+      const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + at(r + 8, d >> 3) + 2 * (d & 7)));
+      f.v[0] = __builtin_bit_cast(u4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    return f;
+  }
+};
+
+// Rows of a matrix on their way into a tile of ROWS rows by all threads of a workgroup; columns from `dim` on are zeros.
+template <typename T, int DP, int ROWS>
+struct Rows {
+  using Tl = Tile<T, DP>;
+  static constexpr int kChunks = DP / Tl::kChunk, kTurns = (ROWS * kChunks + kThreads - 1) / kThreads;
+  u4 v[kTurns];
+  // rows first .. first + ROWS - 1, those behind `last` as `last`
+  __device__ __forceinline__ void load(const T *base, long long ld, int first, int last, int dim, int tid) {
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int at = tid + i * kThreads, r = at / kChunks, c = at % kChunks;
+      v[i] = u4{0u, 0u, 0u, 0u};
+      if ((ROWS * kChunks % kThreads == 0 || r < ROWS) && c * Tl::kChunk < dim)
+        v[i] = *(const u4_any *)(base + (long long)min(first + r, last) * ld + c * Tl::kChunk);
+    }
+  }
+  __device__ __forceinline__ void store(char *tile, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int at = tid + i * kThreads, r = at / kChunks, c = at % kChunks;
+      if (ROWS * kChunks % kThreads == 0 || r < ROWS) *(u4 *)(tile + Tl::at(r, c)) = v[i];
+    }
+  }
+};
+
+// The rows [start, end) of the sequence that row i of a replica belongs to; empty where there is none.  offsets NULL: one sequence of all rows.
+struct Span {
+  int start, end;
+};
+__device__ __forceinline__ Span span_of(const int32_t *offsets, int sequences, int tokens, int i) {
+  if (!offsets) return {0, tokens};
+  int lo = 0, hi = sequences;  // the last b in [0, sequences) with offsets[b] <= i, or 0
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] <= i)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const int s = max(offsets[lo], 0), e = min(offsets[lo + 1], tokens);
+  if (i < s || i >= e) return {0, 0};
+  return {s, e};
+}
+// The rows that sequences cover: all that lie in one lie in [first, end).
+__device__ __forceinline__ Span covered(const int32_t *offsets, int sequences, int tokens) {
+  if (!offsets) return {0, tokens};
+  return {min(max(offsets[0], 0), tokens), min(max(offsets[sequences], 0), tokens)};
+}
+
+// What a query sees: `count` keys from lo on, itself the last of them, and `sinks` from start on.
+struct Sight {
+  int lo, start;
+  uint32_t count, sinks;
+  __device__ __forceinline__ bool sees(int j) const { return ((uint32_t)(j - lo) < count) | ((uint32_t)(j - start) < sinks); }
+};
+__device__ __forceinline__ Sight sight_of(Span s, int i, int window, int sinks) {
+  const bool some = s.end > s.start;
+  const int lo = window > 0 ? max(s.start, i - min(i, window) + (window <= i ? 1 : 0)) : s.start;
+  return {some ? lo : 0x7fffffff, some ? s.start : 0, some ? (uint32_t)(i - lo + 1) : 0u, some ? (uint32_t)min(sinks, i + 1 - s.start) : 0u};
+}
+// In a tile of sinks, which ends where the window of the first row begins, only sinks count, and only those.
+__device__ __forceinline__ Sight only_sinks(const Sight &s, int end) {
+  return {s.lo, s.start, 0u, (uint32_t)min((int)s.sinks, max(end - s.start, 0))};
+}
+
+// Values of the other half of the wavefront, in both halves.
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ bool non_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+
+// Of a fragment's values: the finite ones, zeros for the others; and one for each of the others, zeros for the finite.
+template <typename T>
+__device__ __forceinline__ void part_finite(const Frag<T> &f, Frag<T> &finite, Frag<T> &others) {
+  float a[8], b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float x = frag_at(f, j);
+    const bool bad = non_finite(x);
+    a[j] = bad ? 0.f : x, b[j] = bad ? 1.f : 0.f;
+  }
+  finite = make_frag<T>(a), others = make_frag<T>(b);
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, float a, float b, float c, float d);
+template <>
+__device__ __forceinline__ void store4<float>(float *p, float a, float b, float c, float d) {
+  *(tok::f4_any *)p = f4{a, b, c, d};
+}
+template <>
+__device__ __forceinline__ void store4<bf16_t>(bf16_t *p, float a, float b, float c, float d) {
+  *(tok::us4_any *)p = f32x4_to_bf16x4(f4{a, b, c, d});
+}
+
+struct Args {
+  const void *q, *k, *v;
+  const int32_t *offsets;
+  void *out;
+  float *lse;
+  int n, tokens, sequences, heads, kv_heads, dim, window, sinks, tiles;
+  float scale;
+  long long ld_q, q_stride, ld_kv, kv_stride, ld_out, out_stride;
+};
+
+}  // namespace attn

@@ -1,0 +1,197 @@
+// Attention over packed sequences, forward: one pass over the keys that a tile of queries sees, with the running maximum and sum of the softmax.
+#include "attn.h"
+
+namespace {
+
+using namespace attn;
+
+constexpr int kRows = 32 * kWaves;  // queries of a workgroup, 32 to a wavefront
+
+// Keys of a tile: two of them, of K and of V, are in LDS at a time.
+template <typename T>
+constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
+  using Tl = Tile<T, DP>;
+  constexpr int BN = kKeys<T>, NB = BN / 32, ND = DP / 32, NS = DP / 16;
+  constexpr int kTileBytes = BN * Tl::kRowBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+  const int hx = blockIdx.x % g.heads, kvh = hx % g.kv_heads, head = kvh * (g.heads / g.kv_heads) + hx / g.kv_heads;
+  const int tile = g.tiles - 1 - blockIdx.x / g.heads, rep = blockIdx.y;
+  const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
+  const T *q = (const T *)g.q + rep * g.q_stride + (long long)head * g.dim;
+  const T *k = (const T *)g.k + rep * g.kv_stride + (long long)kvh * g.dim;
+  const T *v = (const T *)g.v + rep * g.kv_stride + (long long)kvh * g.dim;
+
+  const int r0 = tile * kRows, w0 = r0 + wave * 32, row = w0 + (lane & 31);
+  const Span cov = covered(offsets, g.sequences, g.tokens);
+  Sight s = sight_of({0, 0}, 0, 0, 0);
+  if (row < g.tokens) s = sight_of(span_of(offsets, g.sequences, g.tokens, row), row, g.window, g.sinks);
+  const int rv0 = max(r0, cov.start), rv1 = min(r0 + kRows, cov.end) - 1;
+
+  // Keys: [s0, s1) of the sinks in front of the window of the first row, then [klo, khi).  A sequence that begins inside the tile has its
+  // sinks in the second part.
+  int klo = 0, khi = 0, s0 = 0, s1 = 0;
+  if (rv0 <= rv1) {
+    const Sight f = sight_of(span_of(offsets, g.sequences, g.tokens, rv0), rv0, g.window, g.sinks);
+    if (f.count) klo = f.lo, khi = rv1 + 1, s0 = f.start, s1 = min(f.start + (int)f.sinks, f.lo);
+  }
+  klo = __builtin_amdgcn_readfirstlane(klo), khi = __builtin_amdgcn_readfirstlane(khi);
+  s0 = __builtin_amdgcn_readfirstlane(s0), s1 = __builtin_amdgcn_readfirstlane(s1);
+  const int nS = s1 > s0 ? (s1 - s0 + BN - 1) / BN : 0, total = nS + (khi - klo + BN - 1) / BN;
+  // of this wavefront's rows: whether all lie in sequences, the first key of the first and of the last one's window, the first one's sinks
+  const bool all_in = w0 >= cov.start && w0 + 31 < cov.end;
+  const int lo_first = __builtin_amdgcn_readlane(s.lo, 0), lo_last = __builtin_amdgcn_readlane(s.lo, 31);
+  const int sink_first = __builtin_amdgcn_readlane(s.start, 0) + g.sinks;
+
+  Frag<T> qf[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    qf[i] = zero_frag<T>();
+    if (16 * i + 8 * h < g.dim) qf[i] = load_frag(q + (long long)min(row, g.tokens - 1) * g.ld_q + 16 * i + 8 * h);
+  }
+
+  const float c = g.scale * kLog2e;
+  f16v o[ND];
+  float m, l;
+  // Masked tiles multiply the values of keys that a row does not see by zero, which is no zero where they are infinite or NaN.  That is looked
+  // for in the result, and only then is all done again with such values taken out of those tiles and their rows noted.
+  for (int safe = 0;; ++safe) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] = zero16();
+    m = -INFINITY, l = 0.f;
+    Rows<T, DP, BN> kr, vr;
+    auto base_of = [&](int t) { return t < nS ? s0 + t * BN : klo + (t - nS) * BN; };
+    auto fetch = [&](int t) {
+      const int b = base_of(t), last = (t < nS ? s1 : khi) - 1;
+      kr.load(k, g.ld_kv, b, last, g.dim, tid);
+      vr.load(v, g.ld_kv, b, last, g.dim, tid);
+    };
+    if (total > 0) {
+      fetch(0);
+      kr.store(lds[0][0], tid), vr.store(lds[0][1], tid);
+    }
+    __syncthreads();
+    for (int t = 0; t < total; ++t) {
+      if (t + 1 < total) fetch(t + 1);
+      const int kb = base_of(t);
+      const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+      const bool none = kb > w0 + 31 || (all_in && t >= nS && kb + BN - 1 < lo_first && kb >= sink_first);
+      if (!none) {
+        f16v sc[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          sc[b] = zero16();
+#pragma unroll
+          for (int i = 0; i < NS; ++i) mma(Tl::row(kt, 32 * b + (lane & 31), 2 * i + h), qf[i], sc[b]);
+        }
+        const bool whole = all_in && t >= nS && kb + BN - 1 <= w0 && kb >= lo_last;
+        uint32_t seen[NB];
+        if (!whole) {
+          const Sight now = t < nS ? only_sinks(s, s1) : s;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            seen[b] = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool ok = now.sees(kb + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3));
+              seen[b] |= (uint32_t)ok << i;
+              sc[b][i] = ok ? sc[b][i] : -INFINITY;
+            }
+          }
+        }
+        // Everything is relative to m, the largest of scale log2(e) s so far or up to eight below it: as one number m is the same for all
+        // terms of a row, so its own rounding cancels, and o need not be scaled again for each small step of the maximum.
+        float top = sc[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+        top = half_max(top) * c;
+        if (__any(top > m + 8.f)) {
+          const float now = fmaxf(m, top), f = now == m ? 1.f : __builtin_amdgcn_exp2f(m - now);
+          m = now, l *= f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float mu = m == -INFINITY ? 0.f : m;
+        Frag<T> pf[2 * NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][8 * u + j], c, -mu));
+            l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            pf[2 * b + u] = make_frag<T>(p);
+          }
+        if (!(safe && !whole)) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int u = 0; u < 2 * NB; ++u) mma(Tl::column(vt, 16 * u, d, lane), pf[u], o[d]);
+        } else {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            f16v bad = zero16();
+#pragma unroll
+            for (int u = 0; u < 2 * NB; ++u) {
+              Frag<T> fin, oth;
+              part_finite(Tl::column(vt, 16 * u, d, lane), fin, oth);
+              float ones[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) ones[j] = (seen[u >> 1] >> (8 * (u & 1) + j)) & 1u ? 1.f : 0.f;
+              mma(fin, pf[u], o[d]);
+              mma(oth, make_frag<T>(ones), bad);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              o[d][i] = bad[i] > 0.f ? NAN : o[d][i];
+          }
+        }
+      }
+      if (t + 1 < total) kr.store(lds[(t + 1) & 1][0], tid), vr.store(lds[(t + 1) & 1][1], tid);
+      __syncthreads();
+    }
+    bool odd = false;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd |= non_finite(o[d][i]);
+    if (safe || !__syncthreads_or(odd)) break;
+  }
+
+  l = half_sum(l);
+  if (row >= g.tokens) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T *out = (T *)g.out + rep * g.out_stride + (long long)row * g.ld_out + (long long)head * g.dim;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int at = 32 * d + 8 * b + 4 * h;
+      if (at < g.dim) store4(out + at, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv);
+    }
+  if (g.lse && h == 0) g.lse[((long long)rep * g.heads + head) * g.tokens + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+}  // namespace
+
+hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
+                                const int32_t *offsets, void *out, float *lse) {
+  Args g{q,       k,      v,          offsets, out,        lse,     d.n,     d.tokens, d.sequences, d.heads, d.kv_heads,
+         d.dim,   d.window, d.sinks, tok::ceil_div(d.tokens, kRows), d.scale, d.ld_q,  d.q_stride, d.ld_kv, d.kv_stride, d.ld_out, d.out_stride};
+  const dim3 grid(g.tiles * d.heads, d.n);
+  auto go = [&](auto *kernel) {
+    kernel<<<grid, kThreads, 0, st>>>(g);
+    return hipGetLastError();
+  };
+  if (d.dtype) return d.dim <= 64 ? go(k_attn_fwd<bf16_t, 64>) : d.dim <= 96 ? go(k_attn_fwd<bf16_t, 96>) : go(k_attn_fwd<bf16_t, 128>);
+  return d.dim <= 64 ? go(k_attn_fwd<float, 64>) : go(k_attn_fwd<float, 128>);
+}

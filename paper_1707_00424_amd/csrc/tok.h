@@ -207,3 +207,21 @@ hipError_t launch_logprob_fwd(hipStream_t st, const parle_logprob_desc &d, const
                               float *logp, float *entropy, float *lse, int32_t *top_ids, float *top_logp);
 hipError_t launch_logprob_bwd(hipStream_t st, const parle_logprob_desc &d, const void *logits, const int32_t *labels, const float *lse,
                               const float *entropy, const float *dlogp, const float *dentropy, void *dlogits);
+
+hipError_t launch_rope(hipStream_t st, const parle_rope_desc &d, const void *x, const int32_t *positions, const float *freqs, void *out);
+
+hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
+                                const int32_t *offsets, void *out, float *lse);
+int64_t attention_scratch_bytes(const parle_attention_desc &d);
+hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
+                                const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch, void *dq, void *dk,
+                                void *dv);
+hipError_t launch_attention_store(hipStream_t st, const parle_cache_desc &d, int tokens, const void *k, const void *v, const int32_t *offsets,
+                                  const int32_t *lengths, void *k_cache, void *v_cache);
+int64_t decode_scratch_bytes(const parle_cache_desc &d);
+hipError_t launch_attention_decode(hipStream_t st, const parle_cache_desc &d, const void *q, const void *k, const void *v, const int32_t *lengths,
+                                   void *scratch, void *k_cache, void *v_cache, void *out);
+
+int64_t sample_scratch_bytes(const parle_sample_desc &d);
+hipError_t launch_sample(hipStream_t st, const parle_sample_desc &d, const void *logits, const float *uniform, const float *temperature,
+                         const int32_t *top_k, const float *top_p, const float *min_p, void *scratch, int32_t *tokens, int32_t *kept, float *logp);

@@ -115,6 +115,91 @@ bool good(Check &c, const parle_logprob_desc *d) {
   return c.status == PARLE_OK;
 }
 
+// Rows `ld` apart and replicas `stride` apart of a tensor of rows of `width` elements.
+bool good_rows(Check &c, int n, int rows, long long width, int64_t ld, int64_t stride, const char *narrow, const char *close) {
+  c.field(ld >= width, narrow).that(ld <= kMostElems / ((long long)rows + 1), PARLE_ESIZE, "rows of a replica exceed 2^40 elements");
+  if (c.status) return false;
+  c.field(n == 1 || rows == 0 || stride >= (rows - 1) * ld + width, close)
+      .that(stride >= 0 && stride <= kMostElems / n, PARLE_ESIZE, "a tensor exceeds 2^40 elements");
+  return c.status == PARLE_OK;
+}
+bool good(Check &c, const parle_rope_desc *d) {
+  c.field(d, "desc is NULL");
+  if (c.status) return false;
+  c.field((d->dtype | 1) == 1 && (d->interleaved | 1) == 1 && (d->inverse | 1) == 1, "dtype, interleaved and inverse are 0 or 1")
+      .field(d->n >= 1 && d->n <= 65535, "1 <= n <= 65535")
+      .field(d->tokens >= 0 && d->heads >= 1 && d->dim >= 1, "tokens >= 0, heads >= 1, dim >= 1")
+      .field(d->axes >= 1 && d->axes <= PARLE_ROPE_MAX_AXES, "1 <= axes <= PARLE_ROPE_MAX_AXES");
+  if (c.status) return false;
+  long long pairs = 0;
+  for (int i = 0; i < d->axes; ++i) {
+    c.field(d->pairs[i] >= 0, "pairs of an axis are negative");
+    pairs += d->pairs[i];
+  }
+  c.field(2 * pairs <= d->dim, "pairs are more than half of dim");
+  c.that(d->tokens <= kMostRows && d->dim <= 4096 && (long long)d->heads * d->dim <= kMostRows, PARLE_ESIZE,
+         "tokens or heads * dim exceeds 2^22, or dim 4096");
+  if (c.status) return false;
+  const long long width = (long long)d->heads * d->dim;
+  return good_rows(c, d->n, d->tokens, width, d->ld, d->stride, "ld is less than heads * dim", "stride is less than a replica's rows") &&
+         good_rows(c, d->n, d->tokens, width, d->ld_out, d->out_stride, "ld_out is less than heads * dim",
+                   "out_stride is less than a replica's rows");
+}
+// What the attention calls share.
+bool good_heads(Check &c, int dtype, int heads, int kv_heads, int dim, int window, int sinks, float scale) {
+  c.field((dtype | 1) == 1, "dtype is 0 or 1")
+      .field(heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0, "heads is a multiple of kv_heads, both at least 1")
+      .field(dim >= 8 && dim % 8 == 0, "dim is a multiple of 8")
+      .field(window >= 0 && sinks >= 0, "window >= 0, sinks >= 0")
+      .field(scale > 0.f && scale < 3e38f, "scale is not positive and finite")
+      .that(dim <= PARLE_ATTENTION_MAX_DIM, PARLE_ESIZE, "dim exceeds PARLE_ATTENTION_MAX_DIM")
+      .that(sinks <= PARLE_ATTENTION_MAX_SINKS, PARLE_ESIZE, "sinks exceeds PARLE_ATTENTION_MAX_SINKS")
+      .that(heads <= 65535, PARLE_ESIZE, "heads exceeds 65535");
+  return c.status == PARLE_OK;
+}
+bool good(Check &c, const parle_attention_desc *d) {
+  c.field(d, "desc is NULL");
+  if (c.status || !good_heads(c, d->dtype, d->heads, d->kv_heads, d->dim, d->window, d->sinks, d->scale)) return false;
+  c.field(d->n >= 1 && d->n <= 65535, "1 <= n <= 65535")
+      .field(d->tokens >= 0 && d->sequences >= 1, "tokens >= 0, sequences >= 1")
+      .that(d->tokens <= kMostRows && d->sequences <= kMostRows, PARLE_ESIZE, "tokens or sequences exceeds 2^22")
+      .that((long long)d->tokens * d->heads < 1LL << 30, PARLE_ESIZE, "tokens * heads reaches 2^30");
+  return c.status == PARLE_OK &&
+         good_rows(c, d->n, d->tokens, (long long)d->heads * d->dim, d->ld_q, d->q_stride, "ld_q is less than heads * dim",
+                   "q_stride is less than a replica's rows") &&
+         good_rows(c, d->n, d->tokens, (long long)d->kv_heads * d->dim, d->ld_kv, d->kv_stride, "ld_kv is less than kv_heads * dim",
+                   "kv_stride is less than a replica's rows") &&
+         good_rows(c, d->n, d->tokens, (long long)d->heads * d->dim, d->ld_out, d->out_stride, "ld_out is less than heads * dim",
+                   "out_stride is less than a replica's rows");
+}
+bool good(Check &c, const parle_cache_desc *d) {
+  c.field(d, "desc is NULL");
+  if (c.status || !good_heads(c, d->dtype, d->heads, d->kv_heads, d->dim, d->window, d->sinks, d->scale)) return false;
+  c.field(d->sequences >= 0 && d->capacity > d->sinks, "sequences >= 0, capacity > sinks")
+      .field(d->ld_q >= (int64_t)d->heads * d->dim, "ld_q is less than heads * dim")
+      .field(d->ld_kv >= (int64_t)d->kv_heads * d->dim, "ld_kv is less than kv_heads * dim")
+      .field(d->ld_out >= (int64_t)d->heads * d->dim, "ld_out is less than heads * dim");
+  if (c.status) return false;
+  c.that(d->sequences <= 65535, PARLE_ESIZE, "sequences exceeds 65535")
+      .that((int64_t)d->capacity <= kMostElems / ((int64_t)d->kv_heads * d->dim * (d->sequences + 1)), PARLE_ESIZE, "a cache exceeds 2^40 elements")
+      .that(d->ld_q <= kMostElems / (d->sequences + 1) && d->ld_out <= kMostElems / (d->sequences + 1) && d->ld_kv <= kMostElems / kMostRows, PARLE_ESIZE,
+            "rows exceed 2^40 elements");
+  return c.status == PARLE_OK;
+}
+bool good(Check &c, const parle_sample_desc *d) {
+  c.field(d, "desc is NULL");
+  if (c.status) return false;
+  c.field((d->dtype | 1) == 1, "dtype is 0 or 1")
+      .field(d->n >= 1 && d->n <= 65535, "1 <= n <= 65535")
+      .field(d->rows >= 0 && d->classes >= 1, "rows >= 0, classes >= 1")
+      .field(d->ld >= d->classes, "ld is less than classes");
+  if (c.status) return false;
+  c.that(d->classes <= kMostRows, PARLE_ESIZE, "classes exceeds 2^22")
+      .that((long long)d->n * d->rows < kMostRows && d->ld <= kMostElems / ((long long)d->n * d->rows + 1), PARLE_ESIZE,
+            "n * rows reaches 2^22 or the logits 2^40 elements");
+  return c.status == PARLE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -231,6 +316,98 @@ parle_status parle_k_logprob_backward(void *hip_stream, const parle_logprob_desc
   c.given(dlogits, "dlogits is NULL").maybe(dentropy).maybe(entropy).field(!dentropy || entropy, "dentropy needs entropy");
   if (c.status) return c.status;
   return c.launched(launch_logprob_bwd((hipStream_t)hip_stream, *desc, logits, labels, lse, entropy, dlogp, dentropy, dlogits));
+}
+
+parle_status parle_k_rope(void *hip_stream, const parle_rope_desc *desc, const void *x, const int32_t *positions, const float *freqs, void *out) {
+  Check c{"parle_k_rope"};
+  if (!good(c, desc)) return c.status;
+  if (desc->tokens == 0) return PARLE_OK;
+  c.given(x, "x is NULL").given(positions, "positions is NULL").given(freqs, "freqs is NULL").given(out, "out is NULL");
+  c.field(x != out || (desc->ld == desc->ld_out && (desc->n == 1 || desc->stride == desc->out_stride)), "out is x in another layout");
+  if (c.status) return c.status;
+  return c.launched(launch_rope((hipStream_t)hip_stream, *desc, x, positions, freqs, out));
+}
+
+int64_t parle_k_attention_scratch_bytes(const parle_attention_desc *desc) {
+  Check c{"parle_k_attention_scratch_bytes"};
+  return good(c, desc) ? attention_scratch_bytes(*desc) : -1;
+}
+
+parle_status parle_k_attention_forward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
+                                       const int32_t *offsets, void *out, float *lse) {
+  Check c{"parle_k_attention_forward"};
+  if (!good(c, desc)) return c.status;
+  if (desc->tokens == 0) return PARLE_OK;
+  c.given(q, "q is NULL").given(k, "k is NULL").given(v, "v is NULL").given(out, "out is NULL").maybe(offsets).maybe(lse);
+  c.field(offsets || desc->sequences == 1, "offsets is NULL with more than one sequence");
+  c.field(out != q && out != k && out != v, "out is q, k or v");
+  if (c.status) return c.status;
+  return c.launched(launch_attention_fwd((hipStream_t)hip_stream, *desc, q, k, v, offsets, out, lse));
+}
+
+parle_status parle_k_attention_backward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
+                                        const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch,
+                                        int64_t scratch_bytes, void *dq, void *dk, void *dv) {
+  Check c{"parle_k_attention_backward"};
+  if (!good(c, desc)) return c.status;
+  if (desc->tokens == 0) return PARLE_OK;
+  c.given(q, "q is NULL").given(k, "k is NULL").given(v, "v is NULL").given(out, "out is NULL").given(lse, "lse is NULL").given(dout, "dout is NULL");
+  c.given(dq, "dq is NULL").given(dk, "dk is NULL").given(dv, "dv is NULL").maybe(offsets);
+  c.field(offsets || desc->sequences == 1, "offsets is NULL with more than one sequence");
+  const void *in[] = {q, k, v, out, dout};
+  for (const void *p : in) c.field(dq != p && dk != p && dv != p, "a gradient is written over an input");
+  c.field(dq != dk && dq != dv && dk != dv, "two gradients are one buffer");
+  c.scratch(scratch, scratch_bytes, attention_scratch_bytes(*desc));
+  if (c.status) return c.status;
+  return c.launched(launch_attention_bwd((hipStream_t)hip_stream, *desc, q, k, v, offsets, out, lse, dout, scratch, dq, dk, dv));
+}
+
+parle_status parle_k_attention_store(void *hip_stream, const parle_cache_desc *desc, int32_t tokens, const void *k, const void *v,
+                                     const int32_t *offsets, const int32_t *lengths, void *k_cache, void *v_cache) {
+  Check c{"parle_k_attention_store"};
+  if (!good(c, desc)) return c.status;
+  c.field(tokens >= 0, "tokens >= 0").that(tokens <= kMostRows, PARLE_ESIZE, "tokens exceeds 2^22");
+  if (c.status || tokens == 0 || desc->sequences == 0) return c.status;
+  c.given(k, "k is NULL").given(v, "v is NULL").given(offsets, "offsets is NULL").given(lengths, "lengths is NULL");
+  c.given(k_cache, "k_cache is NULL").given(v_cache, "v_cache is NULL").field(k_cache != v_cache, "the caches are one buffer");
+  if (c.status) return c.status;
+  return c.launched(launch_attention_store((hipStream_t)hip_stream, *desc, tokens, k, v, offsets, lengths, k_cache, v_cache));
+}
+
+int64_t parle_k_decode_scratch_bytes(const parle_cache_desc *desc) {
+  Check c{"parle_k_decode_scratch_bytes"};
+  return good(c, desc) ? decode_scratch_bytes(*desc) : -1;
+}
+
+parle_status parle_k_attention_decode(void *hip_stream, const parle_cache_desc *desc, const void *q, const void *k, const void *v,
+                                      const int32_t *lengths, void *scratch, int64_t scratch_bytes, void *k_cache, void *v_cache, void *out) {
+  Check c{"parle_k_attention_decode"};
+  if (!good(c, desc)) return c.status;
+  if (desc->sequences == 0) return PARLE_OK;
+  c.given(q, "q is NULL").given(lengths, "lengths is NULL").given(k_cache, "k_cache is NULL").given(v_cache, "v_cache is NULL");
+  c.given(out, "out is NULL").maybe(k).maybe(v).field(!k == !v, "k and v come together").field(k_cache != v_cache, "the caches are one buffer");
+  c.field(out != q && out != k && out != v, "out is q, k or v");
+  c.scratch(scratch, scratch_bytes, decode_scratch_bytes(*desc));
+  if (c.status) return c.status;
+  return c.launched(launch_attention_decode((hipStream_t)hip_stream, *desc, q, k, v, lengths, scratch, k_cache, v_cache, out));
+}
+
+int64_t parle_k_sample_scratch_bytes(const parle_sample_desc *desc) {
+  Check c{"parle_k_sample_scratch_bytes"};
+  return good(c, desc) ? sample_scratch_bytes(*desc) : -1;
+}
+
+parle_status parle_k_sample(void *hip_stream, const parle_sample_desc *desc, const void *logits, const float *uniform, const float *temperature,
+                            const int32_t *top_k, const float *top_p, const float *min_p, void *scratch, int64_t scratch_bytes, int32_t *tokens,
+                            int32_t *kept, float *logp) {
+  Check c{"parle_k_sample"};
+  if (!good(c, desc)) return c.status;
+  if (desc->rows == 0) return PARLE_OK;
+  c.given(logits, "logits is NULL").given(uniform, "uniform is NULL").given(tokens, "tokens is NULL");
+  c.maybe(temperature).maybe(top_k).maybe(top_p).maybe(min_p).maybe(kept).maybe(logp);
+  c.scratch(scratch, scratch_bytes, sample_scratch_bytes(*desc));
+  if (c.status) return c.status;
+  return c.launched(launch_sample((hipStream_t)hip_stream, *desc, logits, uniform, temperature, top_k, top_p, min_p, scratch, tokens, kept, logp));
 }
 
 }  // extern "C"

@@ -1,0 +1,112 @@
+// Rotary positions: pairs of a head's elements turned by position * frequency.  All memory: each element is read and written once.
+//
+// The sines and cosines of a token are the same for its heads, so a workgroup makes those of its tokens once, in LDS, and then streams the
+// heads.  An angle is formed and reduced to a turn in 64 bits, where position * frequency is exact; sine and cosine of the rest, half a turn at most
+// either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the rest's rounding and two steps of the function.
+#include "tok.h"
+
+namespace {
+
+using namespace tok;
+
+constexpr int kThreads = 256;
+constexpr int kPairs = 2048;  // sines and cosines of a workgroup, 16 KiB
+
+struct Args {
+  const void *x;
+  const int32_t *positions;
+  const float *freqs;
+  void *out;
+  int tokens, heads, dim, axes, pairs, at_once;
+  int ends[PARLE_ROPE_MAX_AXES];  // pairs up to and with each axis
+  int turned, per_head;           // pieces of eight pairs of a head; with the pieces of sixteen elements behind them
+  float sign;
+  long long ld, stride, ld_out, out_stride;
+};
+
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void k_rope(Args g) {
+  __shared__ __attribute__((aligned(16))) f2 turn[kPairs];
+  const int tid = threadIdx.x, rep = blockIdx.y, t0 = blockIdx.x * g.at_once, count = min(g.at_once, g.tokens - t0);
+  const T *x = (const T *)g.x + rep * g.stride + (long long)t0 * g.ld;
+  T *out = (T *)g.out + rep * g.out_stride + (long long)t0 * g.ld_out;
+  const int32_t *pos = g.positions + ((long long)rep * g.tokens + t0) * g.axes;
+
+  for (int i = tid; i < count * g.pairs; i += kThreads) {
+    const int t = i / g.pairs, p = i - t * g.pairs;
+    int axis = 0;
+    while (axis < g.axes - 1 && p >= g.ends[axis]) ++axis;
+    const double turns = (double)pos[t * g.axes + axis] * (double)g.freqs[p] * 0.15915494309189533577;
+    const float half = (float)(2.0 * (turns - rint(turns)));
+    float s, c;
+    sincospif(half, &s, &c);
+    turn[i] = f2{c, s * g.sign};
+  }
+  __syncthreads();
+
+  for (int it = tid; it < count * g.heads * g.per_head; it += kThreads) {
+    const int row = it / g.per_head, piece = it - row * g.per_head, t = row / g.heads, head = row - t * g.heads;
+    const T *src = x + (long long)t * g.ld + (long long)head * g.dim;
+    T *dst = out + (long long)t * g.ld_out + (long long)head * g.dim;
+    if (piece >= g.turned) {
+      const int at = 2 * g.pairs + (piece - g.turned) * 2 * kVec, n = g.dim - at;
+      float a[kVec], b[kVec];
+      load8(src + at, n, 0.f, a), load8(src + at + kVec, n - kVec, 0.f, b);
+      store8(dst + at, n, a), store8(dst + at + kVec, n - kVec, b);
+      continue;
+    }
+    const int p = piece * kVec, n = g.pairs - p;
+    const f2 *cs = turn + t * g.pairs + p;
+    if constexpr (INTERLEAVED) {
+      float a[2][kVec];
+      load8(src + 2 * p, 2 * n, 0.f, a[0]), load8(src + 2 * p + kVec, 2 * n - kVec, 0.f, a[1]);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const f2 w = i < n ? cs[i] : f2{0.f, 0.f};
+        float &u = a[i >> 2][2 * (i & 3)], &v = a[i >> 2][2 * (i & 3) + 1];
+        const float y = u * w.x - v * w.y, z = u * w.y + v * w.x;
+        u = y, v = z;
+      }
+      store8(dst + 2 * p, 2 * n, a[0]), store8(dst + 2 * p + kVec, 2 * n - kVec, a[1]);
+    } else {
+      float a[kVec], b[kVec];
+      load8(src + p, n, 0.f, a), load8(src + g.pairs + p, n, 0.f, b);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const f2 w = i < n ? cs[i] : f2{0.f, 0.f};
+        const float y = a[i] * w.x - b[i] * w.y, z = a[i] * w.y + b[i] * w.x;
+        a[i] = y, b[i] = z;
+      }
+      store8(dst + p, n, a), store8(dst + g.pairs + p, n, b);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope(hipStream_t st, const parle_rope_desc &d, const void *x, const int32_t *positions, const float *freqs, void *out) {
+  Args g{x, positions, freqs, out, d.tokens, d.heads, d.dim, d.axes};
+  for (int i = 0; i < d.axes; ++i) g.pairs += d.pairs[i], g.ends[i] = g.pairs;
+  g.turned = ceil_div(g.pairs, kVec);
+  // elements that do not turn stay where they are when written in place
+  const bool in_place = x == out;
+  g.per_head = g.turned + (in_place ? 0 : ceil_div(d.dim - 2 * g.pairs, 2 * kVec));
+  if (g.per_head == 0) return hipSuccess;
+  g.sign = d.inverse ? -1.f : 1.f;
+  g.ld = d.ld, g.stride = d.stride, g.ld_out = d.ld_out, g.out_stride = d.out_stride;
+  // Tokens of a workgroup: four pieces a thread, so that sines are shared and memory has work, but 1024 workgroups before that.
+  const long long items = (long long)d.heads * g.per_head;
+  long long n = 4 * kThreads / items;
+  const long long spread = (long long)d.tokens * d.n / 1024;
+  if (n > spread) n = spread;
+  if (g.pairs > 0 && n > kPairs / g.pairs) n = kPairs / g.pairs;
+  if (n < 1) n = 1;
+  g.at_once = (int)n;
+  const dim3 grid(ceil_div(d.tokens, n), d.n);
+  auto go = [&](auto *kernel) {
+    kernel<<<grid, kThreads, 0, st>>>(g);
+    return hipGetLastError();
+  };
+  if (d.dtype) return d.interleaved ? go(k_rope<bf16_t, true>) : go(k_rope<bf16_t, false>);
+  return d.interleaved ? go(k_rope<float, true>) : go(k_rope<float, false>);
+}
