@@ -5,6 +5,9 @@
 // register sums and one exchange between the halves of the wavefront, and P^T, as it leaves the accumulators, is the second operand of the
 // next product: its eight values of a lane stand for keys 16 t + 8 (j / 4) + 4 (l / 32) + j % 4, and the first operand is read in that order.
 #pragma once
+#include <type_traits>
+
+#include "igemm_dev.h"
 #include "tok.h"
 
 namespace attn {
@@ -89,57 +92,119 @@ struct Tile {
     return ((r & 3) << 2) | ((r >> 2) & 3);
   }
   static __device__ __forceinline__ int at(int r, int chunk) { return r * kRowBytes + ((chunk ^ turn(r)) << 4); }
-  // elements 8 c .. 8 c + 7 of row r
-  static __device__ __forceinline__ Frag<T> row(const char *tile, int r, int c) {
+  // A lane's places in a tile: of elements 16 i + 8 (lane / 32) .. of row lane % 32, and of column 32 d + lane % 32.
+  struct Places {
+    static constexpr int kRow = sizeof(T) / 2, kCol = sizeof(T) == 2 ? 2 : 4;
+    int row[DP / 16][kRow], col[DP / 32][kCol];
+    __device__ __forceinline__ void init(int lane) {
+      const int h = lane >> 5;
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < kRow; ++e) row[i][e] = at(lane & 31, (2 * i + h) * kRow + e);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        if constexpr (sizeof(T) == 4) {
+          const int c = 32 * d + (lane & 31);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) col[d][j] = at(4 * h + j, c >> 2) + 4 * (c & 3);
+        } else {
+          // a transposing read: lane l of sixteen addresses row l / 4, columns 4 (l % 4) .. + 3 of a 4 x 16 block and receives its column l
+          const int r = 4 * h + ((lane & 15) >> 2), c = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          col[d][0] = at(r, c >> 3) + 2 * (c & 7), col[d][1] = at(r + 8, c >> 3) + 2 * (c & 7);
+        }
+      }
+    }
+  };
+  // elements 16 i + 8 (lane / 32) .. + 7 of row r0 + lane % 32, r0 a multiple of 32
+  static __device__ __forceinline__ Frag<T> row(const char *tile, const Places &p, int r0, int i) {
     Frag<T> f;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) f.v[i] = *(const u4 *)(tile + at(r, c * ((int)sizeof(T) / 2) + i));
+    for (int e = 0; e < Places::kRow; ++e) f.v[e] = *(const u4 *)(tile + p.row[i][e] + r0 * kRowBytes);
     return f;
   }
-  // column 32 db + l % 32 of rows r0 + 8 (j / 4) + 4 (l / 32) + j % 4, j = 0 .. 7; r0 a multiple of 16
-  static __device__ __forceinline__ Frag<T> column(const char *tile, int r0, int db, int lane) {
+  // column 32 d + lane % 32 of rows r0 + 8 (j / 4) + 4 (lane / 32) + j % 4, j = 0 .. 7; r0 a multiple of 16
+  static __device__ __forceinline__ Frag<T> column(const char *tile, const Places &p, int r0, int d) {
     Frag<T> f;
-    const int h = lane >> 5;
     if constexpr (sizeof(T) == 4) {
-      const int d = 32 * db + (lane & 31);
+      // the place of a chunk in a row differs by bit 2 of its index between rows 8 apart
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        f.v[j >> 2][j & 3] = *(const uint32_t *)(tile + at(r0 + 8 * (j >> 2) + 4 * h + (j & 3), d >> 2) + 4 * (d & 3));
+      for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = *(const uint32_t *)(tile + (p.col[d][j & 3] ^ (j >> 2 ? 64 : 0)) + (r0 + 8 * (j >> 2)) * kRowBytes);
     } else {
-      // a transposing read: lane l of sixteen addresses row l / 4, columns 4 (l % 4) .. + 3 of a 4 x 16 block and receives its column l
-      const int r = r0 + 4 * h + ((lane & 15) >> 2), d = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-      const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + at(r, d >> 3) + 2 * (d & 7)));
-      const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + at(r + 8, d >> 3) + 2 * (d & 7)));
+      const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + p.col[d][0] + r0 * kRowBytes));
+      const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + p.col[d][1] + r0 * kRowBytes));
       f.v[0] = __builtin_bit_cast(u4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     return f;
   }
 };
 
-// Rows of a matrix on their way into a tile of ROWS rows by all threads of a workgroup; columns from `dim` on are zeros.
-template <typename T, int DP, int ROWS>
-struct Rows {
+// Rows of a matrix that go into tiles of ROWS rows, by all threads of a workgroup.  With DMA they go straight into LDS, arrive some time later
+// (kLoads loads of each wavefront a tile) and are zeros behind the last row; without, they have arrived in front of the next barrier, and the last row
+// stands for those behind it.  Columns from `dim` on are zeros.  DMA needs rows of whole 16 bytes and a matrix of less than 2^31 of them (`direct`).
+template <typename T, int DP, int ROWS, bool DMA>
+struct Loader {
   using Tl = Tile<T, DP>;
   static constexpr int kChunks = DP / Tl::kChunk, kTurns = (ROWS * kChunks + kThreads - 1) / kThreads;
-  u4 v[kTurns];
-  // rows first .. first + ROWS - 1, those behind `last` as `last`
-  __device__ __forceinline__ void load(const T *base, long long ld, int first, int last, int dim, int tid) {
+  static constexpr int kRowChunks = Tl::kPitch / Tl::kChunk, kLoads = ROWS * Tl::kRowBytes / (kWaves * PARLE_WAVE * 16);
+  static_assert(ROWS * Tl::kRowBytes == kLoads * kWaves * PARLE_WAVE * 16, "a tile is whole loads of all wavefronts");
+  static constexpr uint32_t kFar = 0x80000000u;  // beyond any buffer, also with a row's offset added
+  const T *base;
+  long long ld;
+  int last, dim;
+  u4 desc;
+  uint32_t off[DMA ? kLoads : 1];
+
+  __device__ __forceinline__ void init(long long ld_, int dim_) {
+    ld = ld_, dim = dim_;
+    if constexpr (DMA) {
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int at = tid + i * kThreads, r = at / kChunks, c = at % kChunks;
-      v[i] = u4{0u, 0u, 0u, 0u};
-      if ((ROWS * kChunks % kThreads == 0 || r < ROWS) && c * Tl::kChunk < dim)
-        v[i] = *(const u4_any *)(base + (long long)min(first + r, last) * ld + c * Tl::kChunk);
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = ((int)(threadIdx.x >> 6) * kLoads + i) * PARLE_WAVE + (threadIdx.x & 63), r = at / kRowChunks;
+        const int c = (at % kRowChunks) ^ Tl::turn(r);
+        off[i] = c * Tl::kChunk < dim ? (uint32_t)r * (uint32_t)(ld * sizeof(T)) + c * 16 : kFar;
+      }
     }
   }
-  __device__ __forceinline__ void store(char *tile, int tid) const {
+  // the matrix: rows up to `last` are there
+  __device__ __forceinline__ void from(const T *p, int last_) {
+    base = p, last = last_;
+    if constexpr (DMA) desc = igemm_dev::buffer_desc(p, (uint32_t)(last + 1) * (uint32_t)(ld * sizeof(T)));
+  }
+  __device__ __forceinline__ void load(char *tile, int first) const {
+    if constexpr (DMA) {
+      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile, row = (uint32_t)first * (uint32_t)(ld * sizeof(T));
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int at = tid + i * kThreads, r = at / kChunks, c = at % kChunks;
-      if (ROWS * kChunks % kThreads == 0 || r < ROWS) *(u4 *)(tile + Tl::at(r, c)) = v[i];
+      for (int i = 0; i < kLoads; ++i)
+        igemm_dev::dma16(__builtin_amdgcn_readfirstlane(lds + ((threadIdx.x >> 6) * kLoads + i) * 1024), desc, off[i] + row, 0);
+    } else {
+      u4 v[kTurns];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int at = (int)threadIdx.x + i * kThreads, r = at / kChunks, c = at % kChunks;
+        v[i] = u4{0u, 0u, 0u, 0u};
+        if ((ROWS * kChunks % kThreads == 0 || r < ROWS) && c * Tl::kChunk < dim)
+          v[i] = *(const u4_any *)(base + (long long)min(first + r, last) * ld + c * Tl::kChunk);
+      }
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int at = (int)threadIdx.x + i * kThreads, r = at / kChunks, c = at % kChunks;
+        if (ROWS * kChunks % kThreads == 0 || r < ROWS) *(u4 *)(tile + Tl::at(r, c)) = v[i];
+      }
     }
   }
 };
+// Whether a matrix can go straight into LDS.
+inline bool direct(int tokens, int64_t ld, int64_t stride, int n, int size) {
+  return ld * size % 16 == 0 && (n == 1 || stride * size % 16 == 0) && (long long)tokens * ld * size < 1LL << 31;
+}
+// All but the last N loads have arrived, and every wavefront is here.
+template <int N>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // The rows [start, end) of the sequence that row i of a replica belongs to; empty where there is none.  offsets NULL: one sequence of all rows.
 struct Span {

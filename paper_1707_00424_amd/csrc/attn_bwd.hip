@@ -4,33 +4,34 @@
 // Two kernels make the probabilities each for themselves: one owns rows of queries and walks over the keys they see (dQ, and delta on the
 // way), one owns keys and walks over the queries that see them (dK, dV), of all query heads that share the keys.  So no sum crosses
 // workgroups, nothing is added atomically, and results are the same every time; seven products instead of the five that one pass would take.
-// Sinks behind a window are seen by far more queries than other keys.  What chunks of kChunk queries beyond the reach of a sink's tile add to it is summed
-// by workgroups of their own, in front, into scratch.
+// Sinks behind a window are seen by far more queries than other keys.  What the queries beyond the reach of a sink's tile add to it is summed in chunks by
+// workgroups of their own, into scratch, and joined behind.
 #include "attn.h"
 
 namespace {
 
 using namespace attn;
 
-constexpr int kRows = 32 * kWaves;  // queries, or keys, of a workgroup
-constexpr int kChunk = 512;
+constexpr int kRows = 32 * kWaves;  // queries of a workgroup
 
 struct BwdArgs {
   Args a;
   const void *dout;
-  float *delta;    // [n][heads][tokens]
-  float *far;      // [n][kv_heads][chunks][sinks][2][dim]: dK / scale and dV of the sinks of the sequence that a chunk begins in
+  float *stats;  // [n][heads][2][tokens]: -lse log2(e), -delta
+  // dK / scale and dV of sinks, [2][dim] each: of the queries of a chunk, for the sequence that the chunk begins in; and of the queries in front of a
+  // sequence's first such chunk, by that chunk.  [n][kv_heads][chunks][sinks].
+  float *far, *near;
   void *dq, *dk, *dv;
-  int chunks;
+  int chunk, chunks;  // rows of a chunk, a multiple of kRows
 };
 
-// The first query that the workgroup of key tile `t` leaves to the chunks, for sinks.
-__host__ __device__ __forceinline__ int reach(int t, int window, int tokens) {
-  const long long e = ((long long)(t + 1) * kRows - 1 + window + kChunk - 1) / kChunk * kChunk;
+// The first query that the workgroup of a key leaves to the chunks, for sinks.
+__host__ __device__ __forceinline__ int reach(int key, int window, int chunk, int tokens) {
+  const long long e = ((long long)(key / kRows + 1) * kRows - 1 + window + chunk - 1) / chunk * chunk;
   return (int)(e < tokens ? e : tokens);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool DMA>
 __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
   const Args &g = b.a;
   using Tl = Tile<T, DP>;
@@ -81,26 +82,28 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
   delta = half_sum(delta);
   const long long stat = ((long long)rep * g.heads + head) * g.tokens + rowc;
   const float lse2 = g.lse[stat] * kLog2e;
-  if (row < g.tokens && h == 0) b.delta[stat] = delta;
+  if (row < g.tokens && h == 0) {
+    float *to = b.stats + 2 * (stat - rowc) + rowc;
+    to[0] = -lse2, to[g.tokens] = -delta;
+  }
+
+  Loader<T, DP, BN, DMA> kl, vl;
+  kl.init(g.ld_kv, g.dim), vl.init(g.ld_kv, g.dim);
+  kl.from(k, khi - 1), vl.from(v, khi - 1);
+  typename Tl::Places pl;
+  pl.init(lane);
 
   const float c = g.scale * kLog2e;
   f16v dq[ND];
-  for (int safe = 0;; ++safe) {  // as in the forward pass, for infinite and NaN keys
+  auto pass = [&](auto safe) {  // as in the forward pass, for infinite and NaN keys
+    constexpr bool SAFE = decltype(safe)::value;
 #pragma unroll
     for (int d = 0; d < ND; ++d) dq[d] = zero16();
-    Rows<T, DP, BN> kr, vr;
     auto base_of = [&](int t) { return t < nS ? s0 + t * BN : klo + (t - nS) * BN; };
-    auto fetch = [&](int t) {
-      const int at = base_of(t), last = (t < nS ? s1 : khi) - 1;
-      kr.load(k, g.ld_kv, at, last, g.dim, tid);
-      vr.load(v, g.ld_kv, at, last, g.dim, tid);
-    };
-    if (total > 0) {
-      fetch(0);
-      kr.store(lds[0][0], tid), vr.store(lds[0][1], tid);
-    }
-    __syncthreads();
+    auto fetch = [&](int t) { kl.load(lds[t & 1][0], base_of(t)), vl.load(lds[t & 1][1], base_of(t)); };
+    if (total > 0) fetch(0);
     for (int t = 0; t < total; ++t) {
+      arrive<0>();
       if (t + 1 < total) fetch(t + 1);
       const int kb = base_of(t);
       const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
@@ -112,8 +115,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
           f16v sc = zero16(), dp = zero16();
 #pragma unroll
           for (int i = 0; i < NS; ++i) {
-            mma(Tl::row(kt, 32 * n + (lane & 31), 2 * i + h), qf[i], sc);
-            mma(Tl::row(vt, 32 * n + (lane & 31), 2 * i + h), df[i], dp);
+            mma(Tl::row(kt, pl, 32 * n, i), qf[i], sc);
+            mma(Tl::row(vt, pl, 32 * n, i), df[i], dp);
           }
           float ds[16];
 #pragma unroll
@@ -124,7 +127,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const bool ok = now.sees(kb + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3));
-              seen |= (uint32_t)ok << i;
+              if (SAFE) seen |= (uint32_t)ok << i;
               ds[i] = ok ? ds[i] : 0.f;
             }
           }
@@ -134,9 +137,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) p[j] = ds[8 * u + j];
             const Frag<T> pf = make_frag<T>(p);
-            if (!(safe && !whole)) {
+            if (!SAFE || whole) {
 #pragma unroll
-              for (int d = 0; d < ND; ++d) mma(Tl::column(kt, 32 * n + 16 * u, d, lane), pf, dq[d]);
+              for (int d = 0; d < ND; ++d) mma(Tl::column(kt, pl, 32 * n + 16 * u, d), pf, dq[d]);
             } else {
               float ones[8];
 #pragma unroll
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
 #pragma unroll
               for (int d = 0; d < ND; ++d) {
                 Frag<T> fin, oth;
-                part_finite(Tl::column(kt, 32 * n + 16 * u, d, lane), fin, oth);
+                part_finite(Tl::column(kt, pl, 32 * n + 16 * u, d), fin, oth);
                 f16v bad = zero16();
                 mma(fin, pf, dq[d]);
                 mma(oth, see, bad);
@@ -157,16 +160,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
           }
         }
       }
-      if (t + 1 < total) kr.store(lds[(t + 1) & 1][0], tid), vr.store(lds[(t + 1) & 1][1], tid);
-      __syncthreads();
     }
     bool odd = false;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd |= non_finite(dq[d][i]);
-    if (safe || !__syncthreads_or(odd)) break;
-  }
+    return odd;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) pass(std::true_type{});
   if (row >= g.tokens) return;
   T *out = (T *)b.dq + rep * g.q_stride + (long long)row * g.ld_q + (long long)head * g.dim;
 #pragma unroll
@@ -179,60 +181,75 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
     }
 }
 
-// FAR: the keys are the sinks of the sequence that a chunk of queries begins in.
-template <typename T, int DP, bool FAR>
-__global__ __launch_bounds__(kThreads, 1) void k_attn_dkv(BwdArgs b) {
+// A wavefront owns 32 keys: K and V are fragments in registers, dK and dV accumulators, and 32 queries a step come through LDS, read as rows for
+// S = Q K^T and dP = dO V^T and as columns for dV and dK.  PARTS wavefronts share keys: they take the steps in turn and their sums meet in LDS, so
+// that a few keys, or few heads of keys, still make enough workgroups.  Behind the workgroups of keys come those of the sinks' chunks.
+template <typename T, int DP, int PARTS, bool DMA>
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) void k_attn_dkv(BwdArgs b) {
   const Args &g = b.a;
   using Tl = Tile<T, DP>;
-  constexpr int BQ = 32, ND = DP / 32, NS = DP / 16;
-  constexpr int kTileBytes = BQ * Tl::kRowBytes;
-  __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][BQ];
+  constexpr int BQ = 32, ND = DP / 32, NS = DP / 16, kKeys = kRows / PARTS;
+  // Stages in LDS, of a tile for each part: one that is multiplied and kAhead on their way.
+  constexpr int kTileBytes = BQ * Tl::kRowBytes, kStageBytes = PARTS * 2 * kTileBytes;
+  constexpr int kRoom = (sizeof(T) == 2 && DP == 64 ? 72 : 136) << 10;  // two workgroups to a compute unit, or one
+  constexpr int kBufs = !DMA || 3 * kStageBytes > kRoom ? 2 : 4 * kStageBytes > kRoom ? 3 : 4, kAhead = kBufs - 1;
+  __shared__ __attribute__((aligned(1024))) char lds[kBufs][PARTS][2][kTileBytes];
+  __shared__ __attribute__((aligned(16))) float stats[kBufs][kWaves][2][BQ];  // of each wavefront its own: -lse log2(e), -delta
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
-  const int kvh = blockIdx.x % g.kv_heads, tile = blockIdx.x / g.kv_heads, rep = blockIdx.y, group = g.heads / g.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, part = wave % PARTS;
+  const int kvh = blockIdx.x % g.kv_heads, rep = blockIdx.y, group = g.heads / g.kv_heads, key_tiles = g.tiles;
+  const bool far = (int)(blockIdx.x / g.kv_heads) >= key_tiles;
+  const int tile = blockIdx.x / g.kv_heads - (far ? key_tiles : 0);
   const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
   const T *k = (const T *)g.k + rep * g.kv_stride + (long long)kvh * g.dim;
   const T *v = (const T *)g.v + rep * g.kv_stride + (long long)kvh * g.dim;
   const Span cov = covered(offsets, g.sequences, g.tokens);
 
-  // This lane's key, and the queries that see it: key .. hi.  Queries of the workgroup: [qlo, qhi).
-  int key, hi = -1, qlo = 0, qhi = 0, sink = 0x7fffffff, end = 0;
+  // This lane's key, and the queries that see it: key .. hi.  Queries of the workgroup: [qlo, qhi).  slot: where sums of a sink go, or -1.
+  int key = wave / PARTS * 32 + (lane & 31), hi = -1, qlo = 0, qhi = 0;
+  long long slot = -1;
   bool all_in;
-  if constexpr (FAR) {
-    const int c0 = tile * kChunk;
+  if (far) {
+    // workgroups of a chunk, one for kKeys sinks each
+    const int blocks = (g.sinks + kKeys - 1) / kKeys, ch = tile / blocks, first = tile % blocks * kKeys, c0 = ch * b.chunk;
     const Span s = span_of(offsets, g.sequences, g.tokens, c0);
-    key = s.start + wave * 32 + (lane & 31);
-    if (key < s.start + g.sinks && key < s.end && c0 >= reach(key / kRows, g.window, g.tokens)) hi = s.end - 1;
-    // the first sink's tile has the least reach
-    if (s.end > s.start && c0 >= reach(s.start / kRows, g.window, g.tokens)) qlo = c0, qhi = min(c0 + kChunk, s.end);
+    const int sink = first + key;
+    key = s.start + sink;
+    if (sink < g.sinks && key < s.end && c0 >= reach(key, g.window, b.chunk, g.tokens)) {
+      hi = s.end - 1;
+      slot = (((long long)rep * g.kv_heads + kvh) * b.chunks + ch) * g.sinks + sink;
+    }
+    // the first sink has the least reach
+    if (s.end > s.start && c0 >= reach(s.start + first, g.window, b.chunk, g.tokens)) qlo = c0, qhi = min(c0 + b.chunk, s.end);
     all_in = __all(hi >= 0);
   } else {
-    const int k0 = tile * kRows;
-    key = k0 + wave * 32 + (lane & 31);
+    const int k0 = tile * kKeys;
+    key += k0;
     Span s = {0, 0};
     if (key < g.tokens) s = span_of(offsets, g.sequences, g.tokens, key);
     if (s.end > s.start) {
-      end = s.end;
       hi = g.window > 0 && key - s.start >= g.sinks ? (int)min((long long)s.end, (long long)key + g.window) - 1 : s.end - 1;
-      if (g.window > 0 && key - s.start < g.sinks) sink = key - s.start, hi = min(hi, max(reach(tile, g.window, g.tokens), key + 1) - 1);
+      if (g.window > 0 && key - s.start < g.sinks) {
+        const int r = reach(key, g.window, b.chunk, g.tokens), ch = (r + b.chunk - 1) / b.chunk;
+        hi = min(hi, r - 1);
+        if ((long long)ch * b.chunk < s.end) slot = (((long long)rep * g.kv_heads + kvh) * b.chunks + ch) * g.sinks + key - s.start;
+      }
     }
-    const int kv0 = max(k0, cov.start), kv1 = min(k0 + kRows, cov.end) - 1;
+    const int kv0 = max(k0, cov.start), kv1 = min(k0 + kKeys, cov.end) - 1;
     if (kv0 <= kv1) {
       const Span f = span_of(offsets, g.sequences, g.tokens, kv1);
       qlo = kv0;
       qhi = g.window > 0 ? (int)min((long long)f.end, (long long)kv1 + g.window) : f.end;
-      if (g.window > 0 && max(f.start, kv0) - f.start < g.sinks) qhi = max(qhi, min(f.end, reach(tile, g.window, g.tokens)));
+      if (g.window > 0 && max(f.start, kv0) - f.start < g.sinks) qhi = max(qhi, min(f.end, reach(kv1, g.window, b.chunk, g.tokens)));
     }
     all_in = key - (lane & 31) >= cov.start && key - (lane & 31) + 31 < cov.end;
   }
   qlo = __builtin_amdgcn_readfirstlane(qlo), qhi = __builtin_amdgcn_readfirstlane(qhi);
-  int hi_least = hi, hi_most = hi, key_last = key;
+  int hi_least = hi, hi_most = hi;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) hi_least = min(hi_least, __shfl_xor(hi_least, o)), hi_most = max(hi_most, __shfl_xor(hi_most, o));
   hi_least = __builtin_amdgcn_readfirstlane(hi_least), hi_most = __builtin_amdgcn_readfirstlane(hi_most);
-  key_last = __builtin_amdgcn_readlane(key, 31);
-  const int key_first = __builtin_amdgcn_readfirstlane(key);
+  const int key_first = __builtin_amdgcn_readfirstlane(key), key_last = key_first + 31;
 
   const int keyc = min(key, g.tokens - 1);
   Frag<T> kf[NS], vf[NS];
@@ -246,173 +263,242 @@ __global__ __launch_bounds__(kThreads, 1) void k_attn_dkv(BwdArgs b) {
   const float c = g.scale * kLog2e;
   const int each = (max(qhi - qlo, 0) + BQ - 1) / BQ, total = each * group;
   f16v dk[ND], dv[ND];
-  for (int safe = 0;; ++safe) {  // as in the forward pass, for infinite and NaN rows of q and dout
+  Loader<T, DP, BQ, DMA> ql, dl;
+  ql.init(g.ld_q, g.dim), dl.init(g.ld_out, g.dim);
+  constexpr int kLoads = PARTS * 2 * Loader<T, DP, BQ, DMA>::kLoads + 1;
+  typename Tl::Places pl;
+  pl.init(lane);
+
+  // One step: 32 queries from `qb` on.  SAFE: infinite and NaN values of q and dout are taken out of masked tiles, as in the forward pass.
+  auto add = [&](auto masked, auto safe, const char *qt, const char *dt, const float *st, int qb) {
+    constexpr bool MASKED = decltype(masked)::value, SAFE = decltype(safe)::value;
+    f16v sc = zero16(), dp;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const f4 de = *(const f4 *)&st[BQ + 8 * n + 4 * h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dp[4 * n + i] = de[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      mma(Tl::row(qt, pl, 0, i), kf[i], sc);
+      mma(Tl::row(dt, pl, 0, i), vf[i], dp);
+    }
+    uint32_t seen = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float x[8], y[8];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const f4 ls = *(const f4 *)&st[8 * (2 * u + n) + 4 * h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 4 * n + i, r = 8 * u + j;
+          float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, ls[i])), ds = p * dp[r];
+          if constexpr (MASKED) {
+            const int row = qb + 8 * (r >> 2) + 4 * h + (r & 3);
+            const bool ok = (row >= key) & (row <= hi);
+            if (SAFE) seen |= (uint32_t)ok << r;
+            p = ok ? p : 0.f, ds = ok ? ds : 0.f;
+          }
+          x[j] = p, y[j] = ds;
+        }
+      }
+      const Frag<T> pf = make_frag<T>(x), sf = make_frag<T>(y);
+      if constexpr (!(SAFE && MASKED)) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          mma(Tl::column(dt, pl, 16 * u, d), pf, dv[d]);
+          mma(Tl::column(qt, pl, 16 * u, d), sf, dk[d]);
+        }
+      } else {
+        float ones[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ones[j] = (seen >> (8 * u + j)) & 1u ? 1.f : 0.f;
+        const Frag<T> see = make_frag<T>(ones);
+        auto finite = [&](const char *tl, const Frag<T> &f, f16v &acc, int d) {
+          Frag<T> fin, oth;
+          part_finite(Tl::column(tl, pl, 16 * u, d), fin, oth);
+          f16v bad = zero16();
+          mma(fin, f, acc);
+          mma(oth, see, bad);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[i] = bad[i] > 0.f ? NAN : acc[i];
+        };
+#pragma unroll
+        for (int d = 0; d < ND; ++d) finite(dt, pf, dv[d], d), finite(qt, sf, dk[d], d);
+      }
+    }
+  };
+  auto pass = [&](auto safe) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) dk[d] = zero16(), dv[d] = zero16();
-    Rows<T, DP, BQ> qr, dr;
-    float st = 0.f;
-    auto fetch = [&](int t) {
-      const int head = kvh * group + t / each, at = qlo + t % each * BQ;
-      qr.load((const T *)g.q + rep * g.q_stride + (long long)head * g.dim, g.ld_q, at, qhi - 1, g.dim, tid);
-      dr.load((const T *)b.dout + rep * g.out_stride + (long long)head * g.dim, g.ld_out, at, qhi - 1, g.dim, tid);
-      if (tid < 2 * BQ) {
-        const long long i = ((long long)rep * g.heads + head) * g.tokens + min(at + (tid & (BQ - 1)), qhi - 1);
-        st = tid < BQ ? g.lse[i] * kLog2e : b.delta[i];
+    // the tile that is fetched next: query head of the group, first query; and this part's that is added next
+    int fetch_head = -1, fetch_at = qhi, at = qlo + part * BQ;
+    const float *sp = nullptr;
+    auto fetch = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        if (fetch_at >= qhi) {
+          if (fetch_head + 1 < group) ++fetch_head;  // behind the last tile, the last head's again, so that loads keep their count
+          const int head = kvh * group + fetch_head;
+          ql.from((const T *)g.q + rep * g.q_stride + (long long)head * g.dim, qhi - 1);
+          dl.from((const T *)b.dout + rep * g.out_stride + (long long)head * g.dim, qhi - 1);
+          sp = b.stats + ((long long)rep * g.heads + head) * 2 * g.tokens;
+          fetch_at = qlo;
+        }
+        ql.load(lds[buf][i][0], fetch_at), dl.load(lds[buf][i][1], fetch_at);
+        if (i == part) {
+          if constexpr (DMA)
+            igemm_dev::dma4(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&stats[buf][wave][0][0]),
+                            igemm_dev::buffer_desc(sp, (uint32_t)g.tokens * 8u), (uint32_t)((lane >> 5) * g.tokens + fetch_at + (lane & 31)) * 4u);
+          else
+            stats[buf][wave][lane >> 5][lane & 31] = sp[(long long)(lane >> 5) * g.tokens + min(fetch_at + (lane & 31), qhi - 1)];
+        }
+        fetch_at += BQ;
       }
     };
-    auto put = [&](int buf) {
-      qr.store(lds[buf][0], tid), dr.store(lds[buf][1], tid);
-      if (tid < 2 * BQ) stats[buf][tid / BQ][tid & (BQ - 1)] = st;
-    };
-    if (total > 0) fetch(0), put(0);
-    __syncthreads();
-    for (int t = 0; t < total; ++t) {
-      if (t + 1 < total) fetch(t + 1);
-      const int qb = qlo + t % each * BQ;
-      const char *qt = lds[t & 1][0], *dt = lds[t & 1][1];
-      if (qb + BQ > key_first && qb <= hi_most) {
-        f16v sc = zero16(), dp = zero16();
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          mma(Tl::row(qt, lane & 31, 2 * i + h), kf[i], sc);
-          mma(Tl::row(dt, lane & 31, 2 * i + h), vf[i], dp);
-        }
-        float p[16], ds[16];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const f4 ls = *(const f4 *)&stats[t & 1][0][8 * n + 4 * h], de = *(const f4 *)&stats[t & 1][1][8 * n + 4 * h];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[4 * n + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * n + i], c, -ls[i]));
-            ds[4 * n + i] = p[4 * n + i] * (dp[4 * n + i] - de[i]);
-          }
-        }
-        const bool whole = all_in && qb >= key_last && qb + BQ - 1 <= hi_least;
-        uint32_t seen = 0;
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int row = qb + 8 * (i >> 2) + 4 * h + (i & 3);
-            const bool ok = (row >= key) & (row <= hi);
-            seen |= (uint32_t)ok << i;
-            p[i] = ok ? p[i] : 0.f, ds[i] = ok ? ds[i] : 0.f;
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float x[8], y[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = p[8 * u + j], y[j] = ds[8 * u + j];
-          const Frag<T> pf = make_frag<T>(x), sf = make_frag<T>(y);
-          if (!(safe && !whole)) {
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              mma(Tl::column(dt, 16 * u, d, lane), pf, dv[d]);
-              mma(Tl::column(qt, 16 * u, d, lane), sf, dk[d]);
-            }
-          } else {
-            float ones[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) ones[j] = (seen >> (8 * u + j)) & 1u ? 1.f : 0.f;
-            const Frag<T> see = make_frag<T>(ones);
-            auto add = [&](const char *tile, const Frag<T> &f, f16v &acc, int d) {
-              Frag<T> fin, oth;
-              part_finite(Tl::column(tile, 16 * u, d, lane), fin, oth);
-              f16v bad = zero16();
-              mma(fin, f, acc);
-              mma(oth, see, bad);
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                acc[i] = bad[i] > 0.f ? NAN : acc[i];
-            };
-#pragma unroll
-            for (int d = 0; d < ND; ++d) add(dt, pf, dv[d], d), add(qt, sf, dk[d], d);
-          }
-        }
+    if (total > 0)
+      for (int i = 0; i < kAhead; ++i) fetch(i);
+    int buf = 0;
+    // a part's tiles of a head follow on those of the head before without a gap, so it steps over heads' ends by itself
+    for (int t = part; t < total + part; t += PARTS) {
+      while (at >= qhi) at -= each * BQ;
+      arrive<DMA ? (kAhead - 1) * kLoads : 0>();
+      fetch(buf == 0 ? kBufs - 1 : buf - 1);
+      if ((t < total) & (at + BQ > key_first) & (at <= hi_most)) {
+        const char *qt = lds[buf][part][0], *dt = lds[buf][part][1];
+        const float *st = &stats[buf][wave][0][0];
+        if (all_in & (at >= key_last) & (at + BQ - 1 <= hi_least))
+          add(std::false_type{}, safe, qt, dt, st, at);
+        else
+          add(std::true_type{}, safe, qt, dt, st, at);
       }
-      if (t + 1 < total) put((t + 1) & 1);
-      __syncthreads();
+      at += PARTS * BQ;
+      buf = buf + 1 < kBufs ? buf + 1 : 0;
     }
+    arrive<0>();  // nothing lands in LDS later
     bool odd = false;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd |= non_finite(dk[d][i]) | non_finite(dv[d][i]);
-    if (safe || !__syncthreads_or(odd)) break;
-  }
+    return odd;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) pass(std::true_type{});
 
-  // [2][dim] of a sink, of chunk 0
-  float *far = b.far ? b.far + ((long long)rep * g.kv_heads + kvh) * b.chunks * g.sinks * 2 * g.dim : nullptr;
-  const long long far_chunk = (long long)g.sinks * 2 * g.dim;
-  if constexpr (FAR) {
-    if (hi < 0) return;
-    far += tile * far_chunk + (long long)(wave * 32 + (lane & 31)) * 2 * g.dim;
+  // the parts' sums meet in the first part's registers, in order, a block of 32 elements at a time
+  if constexpr (PARTS > 1) {
+    float *red = (float *)&lds[0][0][0][0] + wave / PARTS * (2 * 16 * PARLE_WAVE);
+    static_assert(kWaves / PARTS * 2 * 16 * PARLE_WAVE * 4 <= (int)sizeof(lds), "");
 #pragma unroll
     for (int d = 0; d < ND; ++d)
+      for (int from = 1; from < PARTS; ++from) {
+        __syncthreads();
+        if (part == from) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int at = 32 * d + 8 * n + 4 * h;
-        if (at < g.dim) {
-          *(f4 *)(far + at) = f4{dk[d][4 * n], dk[d][4 * n + 1], dk[d][4 * n + 2], dk[d][4 * n + 3]};
-          *(f4 *)(far + g.dim + at) = f4{dv[d][4 * n], dv[d][4 * n + 1], dv[d][4 * n + 2], dv[d][4 * n + 3]};
+          for (int i = 0; i < 16; ++i) red[i * PARLE_WAVE + lane] = dk[d][i], red[(16 + i) * PARLE_WAVE + lane] = dv[d][i];
+        }
+        __syncthreads();
+        if (part == 0) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dk[d][i] += red[i * PARLE_WAVE + lane], dv[d][i] += red[(16 + i) * PARLE_WAVE + lane];
         }
       }
-  } else {
-    if (key >= g.tokens) return;
-    const int first = sink < g.sinks ? (reach(tile, g.window, g.tokens) + kChunk - 1) / kChunk : 0x7fffffff;
-    T *dkr = (T *)b.dk + rep * g.kv_stride + (long long)key * g.ld_kv + (long long)kvh * g.dim;
-    T *dvr = (T *)b.dv + rep * g.kv_stride + (long long)key * g.ld_kv + (long long)kvh * g.dim;
+    if (part) return;
+  }
+  if (far ? slot < 0 : key >= g.tokens) return;
+  T *dkr = (T *)b.dk + rep * g.kv_stride + (long long)key * g.ld_kv + (long long)kvh * g.dim;
+  T *dvr = (T *)b.dv + rep * g.kv_stride + (long long)key * g.ld_kv + (long long)kvh * g.dim;
+  float *to = (far ? b.far : b.near) + (slot < 0 ? 0 : slot) * 2 * g.dim;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+  for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int at = 32 * d + 8 * n + 4 * h;
-        if (at < g.dim) {
-          f4 x = {dk[d][4 * n], dk[d][4 * n + 1], dk[d][4 * n + 2], dk[d][4 * n + 3]};
-          f4 y = {dv[d][4 * n], dv[d][4 * n + 1], dv[d][4 * n + 2], dv[d][4 * n + 3]};
-          for (long long ch = first; ch * kChunk < end; ++ch) {
-            x += *(const f4 *)(far + ch * far_chunk + (long long)sink * 2 * g.dim + at);
-            y += *(const f4 *)(far + ch * far_chunk + (long long)sink * 2 * g.dim + g.dim + at);
-          }
-          store4(dkr + at, x[0] * g.scale, x[1] * g.scale, x[2] * g.scale, x[3] * g.scale);
-          store4(dvr + at, y[0], y[1], y[2], y[3]);
-        }
+    for (int n = 0; n < 4; ++n) {
+      const int at = 32 * d + 8 * n + 4 * h;
+      if (at >= g.dim) continue;
+      const f4 x = {dk[d][4 * n], dk[d][4 * n + 1], dk[d][4 * n + 2], dk[d][4 * n + 3]};
+      const f4 y = {dv[d][4 * n], dv[d][4 * n + 1], dv[d][4 * n + 2], dv[d][4 * n + 3]};
+      if (slot >= 0) {
+        *(f4 *)(to + at) = x, *(f4 *)(to + g.dim + at) = y;
+      } else {
+        store4(dkr + at, x[0] * g.scale, x[1] * g.scale, x[2] * g.scale, x[3] * g.scale);
+        store4(dvr + at, y[0], y[1], y[2], y[3]);
       }
+    }
+}
+
+// The sinks of a sequence: what their own workgroup and the chunks behind its reach have summed, in order.  The workgroup of a chunk sees to the sinks
+// whose first chunk it is; a thread takes four elements of dK or of dV.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_sinks(BwdArgs b) {
+  const Args &g = b.a;
+  const int kvh = blockIdx.x % g.kv_heads, ch = blockIdx.x / g.kv_heads, rep = blockIdx.y;
+  const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
+  const Span s = span_of(offsets, g.sequences, g.tokens, ch * b.chunk);
+  const long long first = (((long long)rep * g.kv_heads + kvh) * b.chunks + ch) * g.sinks, step = (long long)g.sinks * 2 * g.dim;
+  const int per = g.dim / 2;  // pieces of four of a sink's dK and dV
+  for (int it = threadIdx.x; it < g.sinks * per; it += 256) {
+    const int sink = it / per, e = (it - sink * per) * 4, key = s.start + sink;
+    if (key >= s.end || (reach(key, g.window, b.chunk, g.tokens) + b.chunk - 1) / b.chunk != ch) continue;
+    const float *p = b.far + (first + sink) * 2 * g.dim + e;
+    f4 x = *(const f4 *)(b.near + (first + sink) * 2 * g.dim + e);
+    for (long long i = ch; i * b.chunk < s.end; ++i, p += step) x += *(const f4 *)p;
+    const bool is_v = e >= g.dim;
+    T *to = (T *)(is_v ? b.dv : b.dk) + rep * g.kv_stride + (long long)key * g.ld_kv + (long long)kvh * g.dim + (is_v ? e - g.dim : e);
+    const float f = is_v ? 1.f : g.scale;
+    store4(to, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
   }
 }
 
-bool has_far(const parle_attention_desc &d) { return d.window > 0 && d.sinks > 0 && reach(0, d.window, d.tokens) < d.tokens; }
-int64_t delta_bytes(const parle_attention_desc &d) { return tok::round_up((long long)d.n * d.heads * d.tokens * 4, 256); }
+// Chunks of 128 queries, longer where there were more than 64 of them: what a chunk sums is written and read again.
+int chunk_of(const parle_attention_desc &d) { return kRows * tok::ceil_div(tok::ceil_div(d.tokens, kRows), 64); }
+bool has_far(const parle_attention_desc &d) { return d.window > 0 && d.sinks > 0 && reach(0, d.window, chunk_of(d), d.tokens) < d.tokens; }
+int64_t stats_bytes(const parle_attention_desc &d) { return tok::round_up((long long)d.n * d.heads * d.tokens * 8, 256); }
+int64_t far_elems(const parle_attention_desc &d) {
+  return has_far(d) ? (int64_t)d.n * d.kv_heads * tok::ceil_div(d.tokens, chunk_of(d)) * d.sinks * 2 * d.dim : 0;
+}
+// Wavefronts that share keys: one, two or four (two where four would need more LDS than there is), whichever first makes two workgroups for each place
+// that the chip has.
+int parts_of(const parle_attention_desc &d) {
+  const long long tiles = (long long)d.n * d.kv_heads * tok::ceil_div(d.tokens, kRows), places = d.dtype && d.dim <= 64 ? 512 : 256;
+  return tiles >= 2 * places ? 1 : 2 * tiles >= 2 * places || (!d.dtype && d.dim > 64) ? 2 : 4;
+}
 
 }  // namespace
 
-int64_t attention_scratch_bytes(const parle_attention_desc &d) {
-  if (d.tokens == 0) return 0;
-  const int64_t far = has_far(d) ? (int64_t)d.n * d.kv_heads * tok::ceil_div(d.tokens, kChunk) * d.sinks * 2 * d.dim * 4 : 0;
-  return delta_bytes(d) + far;
-}
+int64_t attention_scratch_bytes(const parle_attention_desc &d) { return d.tokens == 0 ? 0 : stats_bytes(d) + 2 * far_elems(d) * 4; }
 
 hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
                                 const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch, void *dq, void *dk,
                                 void *dv) {
-  const int tiles = tok::ceil_div(d.tokens, kRows), chunks = tok::ceil_div(d.tokens, kChunk);
+  const int tiles = tok::ceil_div(d.tokens, kRows), chunk = chunk_of(d), chunks = tok::ceil_div(d.tokens, chunk), parts = parts_of(d);
   const bool far = has_far(d);
+  float *fp = far ? (float *)((char *)scratch + stats_bytes(d)) : nullptr;
   BwdArgs b{{q, k, v, offsets, (void *)out, (float *)lse, d.n, d.tokens, d.sequences, d.heads, d.kv_heads, d.dim, d.window, d.sinks, tiles, d.scale,
              d.ld_q, d.q_stride, d.ld_kv, d.kv_stride, d.ld_out, d.out_stride},
-            dout, (float *)scratch, far ? (float *)((char *)scratch + delta_bytes(d)) : nullptr, dq, dk, dv, chunks};
-  auto go = [&](auto *of_queries, auto *of_sinks, auto *of_keys) {
+            dout, (float *)scratch, fp, far ? fp + far_elems(d) : nullptr, dq, dk, dv, chunk, chunks};
+  auto go = [&](auto *of_queries, auto *of_keys, auto *of_sinks) {
     of_queries<<<dim3(tiles * d.heads, d.n), kThreads, 0, st>>>(b);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && far) {
-      of_sinks<<<dim3(chunks * d.kv_heads, d.n), kThreads, 0, st>>>(b);
-      e = hipGetLastError();
-    }
     if (e != hipSuccess) return e;
-    of_keys<<<dim3(tiles * d.kv_heads, d.n), kThreads, 0, st>>>(b);
+    const int keys = kRows / parts;
+    b.a.tiles = tok::ceil_div(d.tokens, keys);
+    of_keys<<<dim3((b.a.tiles + (far ? chunks * tok::ceil_div(d.sinks, keys) : 0)) * d.kv_heads, d.n), kThreads, 0, st>>>(b);
+    e = hipGetLastError();
+    if (e != hipSuccess || !far) return e;
+    of_sinks<<<dim3(chunks * d.kv_heads, d.n), 256, 0, st>>>(b);
     return hipGetLastError();
   };
-#define PARLE_GO(T, DP) go(k_attn_dq<T, DP>, k_attn_dkv<T, DP, true>, k_attn_dkv<T, DP, false>)
-  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64) : d.dim <= 96 ? PARLE_GO(bf16_t, 96) : PARLE_GO(bf16_t, 128);
-  return d.dim <= 64 ? PARLE_GO(float, 64) : PARLE_GO(float, 128);
+  const int size = d.dtype ? 2 : 4;
+  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, size) && direct(d.tokens, d.ld_q, d.q_stride, d.n, size) &&
+                   direct(d.tokens, d.ld_out, d.out_stride, d.n, size);
+#define PARLE_KEYS(T, DP, MOST, DMA) (parts == 1 ? k_attn_dkv<T, DP, 1, DMA> : parts == 2 ? k_attn_dkv<T, DP, 2, DMA> : k_attn_dkv<T, DP, MOST, DMA>)
+#define PARLE_GO(T, DP, MOST)                                                                  \
+  (dma ? go(k_attn_dq<T, DP, true>, PARLE_KEYS(T, DP, MOST, true), k_attn_sinks<T>) \
+       : go(k_attn_dq<T, DP, false>, PARLE_KEYS(T, DP, MOST, false), k_attn_sinks<T>))
+  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64, 4) : d.dim <= 96 ? PARLE_GO(bf16_t, 96, 4) : PARLE_GO(bf16_t, 128, 4);
+  return d.dim <= 64 ? PARLE_GO(float, 64, 4) : PARLE_GO(float, 128, 2);
+#undef PARLE_KEYS
 #undef PARLE_GO
 }

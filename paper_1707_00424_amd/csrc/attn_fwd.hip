@@ -11,7 +11,7 @@ constexpr int kRows = 32 * kWaves;  // queries of a workgroup, 32 to a wavefront
 template <typename T>
 constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 
-template <typename T, int DP>
+template <typename T, int DP, bool DMA>
 __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
   using Tl = Tile<T, DP>;
   constexpr int BN = kKeys<T>, NB = BN / 32, ND = DP / 32, NS = DP / 16;
@@ -54,28 +54,27 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
     if (16 * i + 8 * h < g.dim) qf[i] = load_frag(q + (long long)min(row, g.tokens - 1) * g.ld_q + 16 * i + 8 * h);
   }
 
+  Loader<T, DP, BN, DMA> kl, vl;
+  kl.init(g.ld_kv, g.dim), vl.init(g.ld_kv, g.dim);
+  kl.from(k, khi - 1), vl.from(v, khi - 1);
+  typename Tl::Places at;
+  at.init(lane);
+
   const float c = g.scale * kLog2e;
   f16v o[ND];
   float m, l;
   // Masked tiles multiply the values of keys that a row does not see by zero, which is no zero where they are infinite or NaN.  That is looked
   // for in the result, and only then is all done again with such values taken out of those tiles and their rows noted.
-  for (int safe = 0;; ++safe) {
+  auto pass = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] = zero16();
     m = -INFINITY, l = 0.f;
-    Rows<T, DP, BN> kr, vr;
     auto base_of = [&](int t) { return t < nS ? s0 + t * BN : klo + (t - nS) * BN; };
-    auto fetch = [&](int t) {
-      const int b = base_of(t), last = (t < nS ? s1 : khi) - 1;
-      kr.load(k, g.ld_kv, b, last, g.dim, tid);
-      vr.load(v, g.ld_kv, b, last, g.dim, tid);
-    };
-    if (total > 0) {
-      fetch(0);
-      kr.store(lds[0][0], tid), vr.store(lds[0][1], tid);
-    }
-    __syncthreads();
+    auto fetch = [&](int t) { kl.load(lds[t & 1][0], base_of(t)), vl.load(lds[t & 1][1], base_of(t)); };
+    if (total > 0) fetch(0);
     for (int t = 0; t < total; ++t) {
+      arrive<0>();
       if (t + 1 < total) fetch(t + 1);
       const int kb = base_of(t);
       const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
@@ -86,7 +85,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
         for (int b = 0; b < NB; ++b) {
           sc[b] = zero16();
 #pragma unroll
-          for (int i = 0; i < NS; ++i) mma(Tl::row(kt, 32 * b + (lane & 31), 2 * i + h), qf[i], sc[b]);
+          for (int i = 0; i < NS; ++i) mma(Tl::row(kt, at, 32 * b, i), qf[i], sc[b]);
         }
         const bool whole = all_in && t >= nS && kb + BN - 1 <= w0 && kb >= lo_last;
         uint32_t seen[NB];
@@ -94,11 +93,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
           const Sight now = t < nS ? only_sinks(s, s1) : s;
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
-            seen[b] = 0;
+            if (SAFE) seen[b] = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const bool ok = now.sees(kb + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3));
-              seen[b] |= (uint32_t)ok << i;
+              if (SAFE) seen[b] |= (uint32_t)ok << i;
               sc[b][i] = ok ? sc[b][i] : -INFINITY;
             }
           }
@@ -131,11 +130,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
             l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
             pf[2 * b + u] = make_frag<T>(p);
           }
-        if (!(safe && !whole)) {
+        if (!SAFE || whole) {
 #pragma unroll
           for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int u = 0; u < 2 * NB; ++u) mma(Tl::column(vt, 16 * u, d, lane), pf[u], o[d]);
+            for (int u = 0; u < 2 * NB; ++u) mma(Tl::column(vt, at, 16 * u, d), pf[u], o[d]);
         } else {
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
@@ -143,7 +142,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
 #pragma unroll
             for (int u = 0; u < 2 * NB; ++u) {
               Frag<T> fin, oth;
-              part_finite(Tl::column(vt, 16 * u, d, lane), fin, oth);
+              part_finite(Tl::column(vt, at, 16 * u, d), fin, oth);
               float ones[8];
 #pragma unroll
               for (int j = 0; j < 8; ++j) ones[j] = (seen[u >> 1] >> (8 * (u & 1) + j)) & 1u ? 1.f : 0.f;
@@ -156,16 +155,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
           }
         }
       }
-      if (t + 1 < total) kr.store(lds[(t + 1) & 1][0], tid), vr.store(lds[(t + 1) & 1][1], tid);
-      __syncthreads();
     }
     bool odd = false;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd |= non_finite(o[d][i]);
-    if (safe || !__syncthreads_or(odd)) break;
-  }
+    return odd;
+  };
+  if (__syncthreads_or(pass(std::false_type{}))) pass(std::true_type{});
 
   l = half_sum(l);
   if (row >= g.tokens) return;
@@ -175,8 +173,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      const int at = 32 * d + 8 * b + 4 * h;
-      if (at < g.dim) store4(out + at, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv);
+      const int e = 32 * d + 8 * b + 4 * h;
+      if (e < g.dim) store4(out + e, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv);
     }
   if (g.lse && h == 0) g.lse[((long long)rep * g.heads + head) * g.tokens + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
@@ -192,6 +190,9 @@ hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, c
     kernel<<<grid, kThreads, 0, st>>>(g);
     return hipGetLastError();
   };
-  if (d.dtype) return d.dim <= 64 ? go(k_attn_fwd<bf16_t, 64>) : d.dim <= 96 ? go(k_attn_fwd<bf16_t, 96>) : go(k_attn_fwd<bf16_t, 128>);
-  return d.dim <= 64 ? go(k_attn_fwd<float, 64>) : go(k_attn_fwd<float, 128>);
+  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, d.dtype ? 2 : 4);
+#define PARLE_GO(T, DP) (dma ? go(k_attn_fwd<T, DP, true>) : go(k_attn_fwd<T, DP, false>))
+  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64) : d.dim <= 96 ? PARLE_GO(bf16_t, 96) : PARLE_GO(bf16_t, 128);
+  return d.dim <= 64 ? PARLE_GO(float, 64) : PARLE_GO(float, 128);
+#undef PARLE_GO
 }
