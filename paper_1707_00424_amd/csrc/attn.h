@@ -198,6 +198,9 @@ struct Loader {
 inline bool direct(int tokens, int64_t ld, int64_t stride, int n, int size) {
   return ld * size % 16 == 0 && (n == 1 || stride * size % 16 == 0) && (long long)tokens * ld * size < 1LL << 31;
 }
+// What was loaded into registers is there.  In front of a loop whose loads go to LDS: the compiler, which does not count those, would wait for registers
+// loaded before the loop at their first use in it, and so for all that is on its way.
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0); }
 // All but the last N loads have arrived, and every wavefront is here.
 template <int N>
 __device__ __forceinline__ void arrive() {

@@ -32,14 +32,14 @@ __host__ __device__ __forceinline__ int reach(int key, int window, int chunk, in
 }
 
 template <typename T, int DP, bool DMA>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attn_dq(BwdArgs b) {
   const Args &g = b.a;
   using Tl = Tile<T, DP>;
   constexpr int BN = sizeof(T) == 2 ? 64 : 32, NB = BN / 32, ND = DP / 32, NS = DP / 16;
   constexpr int kTileBytes = BN * Tl::kRowBytes;
   __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   const int hx = blockIdx.x % g.heads, kvh = hx % g.kv_heads, head = kvh * (g.heads / g.kv_heads) + hx / g.kv_heads;
   const int tile = g.tiles - 1 - blockIdx.x / g.heads, rep = blockIdx.y;
   const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_dq(BwdArgs b) {
   typename Tl::Places pl;
   pl.init(lane);
 
+  settle();
   const float c = g.scale * kLog2e;
   f16v dq[ND];
   auto pass = [&](auto safe) {  // as in the forward pass, for infinite and NaN keys
@@ -260,6 +261,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
     if (at < g.dim) kf[i] = load_frag(k + (long long)keyc * g.ld_kv + at), vf[i] = load_frag(v + (long long)keyc * g.ld_kv + at);
   }
 
+  settle();
   const float c = g.scale * kLog2e;
   const int each = (max(qhi - qlo, 0) + BQ - 1) / BQ, total = each * group;
   f16v dk[ND], dv[ND];
@@ -272,6 +274,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
   // One step: 32 queries from `qb` on.  SAFE: infinite and NaN values of q and dout are taken out of masked tiles, as in the forward pass.
   auto add = [&](auto masked, auto safe, const char *qt, const char *dt, const float *st, int qb) {
     constexpr bool MASKED = decltype(masked)::value, SAFE = decltype(safe)::value;
+    // Loads from LDS are put in front of what hides them: fragments of rows first, those of the first half's columns beside the products of rows,
+    // those of the second half's beside the first half's products.
     f16v sc = zero16(), dp;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
@@ -279,11 +283,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
 #pragma unroll
       for (int i = 0; i < 4; ++i) dp[4 * n + i] = de[i];
     }
+    Frag<T> qr[NS], dr[NS], qc[2][ND], dc[2][ND];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) qr[i] = Tl::row(qt, pl, 0, i), dr[i] = Tl::row(dt, pl, 0, i);
+    __builtin_amdgcn_sched_barrier(0);
+    auto columns = [&](int u) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) dc[u][d] = Tl::column(dt, pl, 16 * u, d), qc[u][d] = Tl::column(qt, pl, 16 * u, d);
+    };
+    columns(0);
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      mma(Tl::row(qt, pl, 0, i), kf[i], sc);
-      mma(Tl::row(dt, pl, 0, i), vf[i], dp);
+      mma(qr[i], kf[i], sc);
+      mma(dr[i], vf[i], dp);
     }
+    __builtin_amdgcn_sched_barrier(0);
     uint32_t seen = 0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -305,20 +319,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
         }
       }
       const Frag<T> pf = make_frag<T>(x), sf = make_frag<T>(y);
+      if (u == 0) columns(1);
       if constexpr (!(SAFE && MASKED)) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          mma(Tl::column(dt, pl, 16 * u, d), pf, dv[d]);
-          mma(Tl::column(qt, pl, 16 * u, d), sf, dk[d]);
+          mma(dc[u][d], pf, dv[d]);
+          mma(qc[u][d], sf, dk[d]);
         }
       } else {
         float ones[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) ones[j] = (seen >> (8 * u + j)) & 1u ? 1.f : 0.f;
         const Frag<T> see = make_frag<T>(ones);
-        auto finite = [&](const char *tl, const Frag<T> &f, f16v &acc, int d) {
+        auto finite = [&](const Frag<T> &column, const Frag<T> &f, f16v &acc) {
           Frag<T> fin, oth;
-          part_finite(Tl::column(tl, pl, 16 * u, d), fin, oth);
+          part_finite(column, fin, oth);
           f16v bad = zero16();
           mma(fin, f, acc);
           mma(oth, see, bad);
@@ -326,7 +341,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
           for (int i = 0; i < 16; ++i) acc[i] = bad[i] > 0.f ? NAN : acc[i];
         };
 #pragma unroll
-        for (int d = 0; d < ND; ++d) finite(dt, pf, dv[d], d), finite(qt, sf, dk[d], d);
+        for (int d = 0; d < ND; ++d) finite(dc[u][d], pf, dv[d]), finite(qc[u][d], sf, dk[d]);
       }
     }
   };
@@ -458,11 +473,11 @@ int64_t stats_bytes(const parle_attention_desc &d) { return tok::round_up((long 
 int64_t far_elems(const parle_attention_desc &d) {
   return has_far(d) ? (int64_t)d.n * d.kv_heads * tok::ceil_div(d.tokens, chunk_of(d)) * d.sinks * 2 * d.dim : 0;
 }
-// Wavefronts that share keys: one, two or four (two where four would need more LDS than there is), whichever first makes two workgroups for each place
-// that the chip has.
+// Wavefronts that share keys: two, or four where two make fewer workgroups than the chip has places (and LDS holds the tiles of four).  Eight heads of
+// 8192 tokens, 64 elements each, take 331 us with two and 363 with four, 1000 tokens of eight heads that share one, 128 elements each, 81 and 67.
 int parts_of(const parle_attention_desc &d) {
-  const long long tiles = (long long)d.n * d.kv_heads * tok::ceil_div(d.tokens, kRows), places = d.dtype && d.dim <= 64 ? 512 : 256;
-  return tiles >= 2 * places ? 1 : 2 * tiles >= 2 * places || (!d.dtype && d.dim > 64) ? 2 : 4;
+  const long long wgs = (long long)d.n * d.kv_heads * tok::ceil_div(d.tokens, kRows / 2), places = d.dtype && d.dim <= 64 ? 512 : 256;
+  return wgs >= places || (!d.dtype && d.dim > 64) ? 2 : 4;
 }
 
 }  // namespace
@@ -493,7 +508,7 @@ hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, c
   const int size = d.dtype ? 2 : 4;
   const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, size) && direct(d.tokens, d.ld_q, d.q_stride, d.n, size) &&
                    direct(d.tokens, d.ld_out, d.out_stride, d.n, size);
-#define PARLE_KEYS(T, DP, MOST, DMA) (parts == 1 ? k_attn_dkv<T, DP, 1, DMA> : parts == 2 ? k_attn_dkv<T, DP, 2, DMA> : k_attn_dkv<T, DP, MOST, DMA>)
+#define PARLE_KEYS(T, DP, MOST, DMA) (parts == 2 ? k_attn_dkv<T, DP, 2, DMA> : k_attn_dkv<T, DP, MOST, DMA>)
 #define PARLE_GO(T, DP, MOST)                                                                  \
   (dma ? go(k_attn_dq<T, DP, true>, PARLE_KEYS(T, DP, MOST, true), k_attn_sinks<T>) \
        : go(k_attn_dq<T, DP, false>, PARLE_KEYS(T, DP, MOST, false), k_attn_sinks<T>))

@@ -12,13 +12,13 @@ template <typename T>
 constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 
 template <typename T, int DP, bool DMA>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attn_fwd(Args g) {
   using Tl = Tile<T, DP>;
   constexpr int BN = kKeys<T>, NB = BN / 32, ND = DP / 32, NS = DP / 16;
   constexpr int kTileBytes = BN * Tl::kRowBytes;
   __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   const int hx = blockIdx.x % g.heads, kvh = hx % g.kv_heads, head = kvh * (g.heads / g.kv_heads) + hx / g.kv_heads;
   const int tile = g.tiles - 1 - blockIdx.x / g.heads, rep = blockIdx.y;
   const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
@@ -60,6 +60,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
   typename Tl::Places at;
   at.init(lane);
 
+  settle();
   const float c = g.scale * kLog2e;
   f16v o[ND];
   float m, l;
@@ -81,11 +82,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
       const bool none = kb > w0 + 31 || (all_in && t >= nS && kb + BN - 1 < lo_first && kb >= sink_first);
       if (!none) {
         f16v sc[NB];
+        Frag<T> kf[NB][NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) kf[0][i] = Tl::row(kt, at, 0, i);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
+          if (b + 1 < NB) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) kf[b + 1][i] = Tl::row(kt, at, 32 * (b + 1), i);
+          }
           sc[b] = zero16();
 #pragma unroll
-          for (int i = 0; i < NS; ++i) mma(Tl::row(kt, at, 32 * b, i), qf[i], sc[b]);
+          for (int i = 0; i < NS; ++i) mma(kf[b][i], qf[i], sc[b]);
         }
         const bool whole = all_in && t >= nS && kb + BN - 1 <= w0 && kb >= lo_last;
         uint32_t seen[NB];
@@ -132,9 +140,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_fwd(Args g) {
           }
         if (!SAFE || whole) {
 #pragma unroll
-          for (int d = 0; d < ND; ++d)
+          for (int u = 0; u < 2 * NB; ++u)
 #pragma unroll
-            for (int u = 0; u < 2 * NB; ++u) mma(Tl::column(vt, at, 16 * u, d), pf[u], o[d]);
+            for (int d = 0; d < ND; ++d) mma(Tl::column(vt, at, 16 * u, d), pf[u], o[d]);
         } else {
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
