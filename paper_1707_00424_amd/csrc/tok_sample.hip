@@ -4,8 +4,11 @@
 // the count, or the sum of the weights e^((x - max) / T), reach a number?  Weights are whole multiples of 2^-s of the largest, so sums are
 // exact in 64-bit integers, in any order, and the answers the same every time; they are formed in 64 bits, as a number next to a border is on one
 // side of it or the other.
-// Nothing is sorted but a few: counts and sums over kBuckets steps of the weight's logarithm say in which step an answer lies, the row is read again
-// for the classes of that step, and up to kList of those are sorted.  More of them (many equal logits) are counted again in finer steps of value and class.
+//
+// A workgroup has a row.  Where few classes can stay, they are listed and sorted, and the list has all answers: a row of up to kList classes; the classes at
+// or above the k-th largest of the threads' largest logits, which the k largest of all are among; or, without top-k, those that min-p leaves, with the
+// sum of all the others' weights.  Else counts and sums over steps of 1/32 power of two say in which step an answer lies, and the row is read again
+// for the classes of that step, up to kList of which are sorted.  More of them (many equal logits) are counted again in finer steps of value and class.
 #include "tok.h"
 
 namespace {
@@ -16,6 +19,10 @@ typedef unsigned long long u64;
 constexpr int kThreads = 1024, kWaves = kThreads / PARLE_WAVE;
 constexpr int kBuckets = 2048, kPer = kBuckets / kThreads;
 constexpr int kList = kThreads;
+constexpr int kPick = 600;    // largest top-k by the threads' largest: that many of 1024 threads hold about 900 classes
+constexpr int kSteps = 32;    // steps of a power of two
+constexpr int kNear = 12 * kSteps;
+constexpr int kBatch = 4;     // 16-byte loads of a thread on their way
 constexpr int kIdBits = 22;  // classes <= 2^22
 
 struct Args {
@@ -42,22 +49,42 @@ __device__ __forceinline__ float value_of(u64 rank) {
 
 // The weights of a row.
 struct Scale {
-  double most, per;  // the largest logit; log2(e) / temperature
+  static constexpr double kMagic = 6755399441055744.0 / kSteps;  // 1.5 * 2^52 / kSteps: a sum with it is rounded to steps, their number in its low bits
+  static constexpr double kWhole = 4503599627370496.0;           // 2^52: a sum with it is rounded to whole numbers, in its low bits
+  double most, per;     // the largest logit; log2(e) / temperature
+  bool infinite;        // the largest logit is: it counts as 0, and all others as next to nothing
   int bits;
-  // the weight's logarithm, base 2, <= 0
-  __device__ __forceinline__ double log_of(float x) const { return (double)x == most ? 0.0 : ((double)x - most) * per; }
-  __device__ __forceinline__ u64 units(double t) const {
-    if (!(t > -(double)(bits + 1))) return 0;
-    const double v = exp2(t + bits) + 4503599627370496.0;  // 2^52: the whole part is in the low bits, rounded to nearest
-    return (u64)__double_as_longlong(v) & ((1ull << 52) - 1);
+  const __attribute__((address_space(3))) double *table;  // 2^(j / kSteps)
+  __device__ __forceinline__ Scale(float largest, float temperature, int bits_, const double *t)
+      : most(largest), per(1.4426950408889634074 / (double)temperature), infinite(largest == INFINITY), bits(bits_),
+        table((const __attribute__((address_space(3))) double *)t) {
+    if (infinite) most = 0.0, per = 1.0;
   }
-  // the last step holds what has no weight
+  // the weight's logarithm, base 2, <= 0; what has no weight, -inf too, is somewhere below
+  __device__ __forceinline__ double log_of(float x) const {
+    const float y = infinite ? (x == INFINITY ? 0.f : -1e30f) : x;
+    return fmax(((double)y - most) * per, -(double)(bits + 2));
+  }
+  // the nearest step to t, counted downwards from the largest weight's; the last one holds what has no weight
   __device__ __forceinline__ int bucket(double t) const {
-    const double range = bits + 1;
-    if (!(t > -range)) return kBuckets - 1;
-    const int b = (int)(-t * ((kBuckets - 1) / range));
-    return b < kBuckets - 2 ? b : kBuckets - 2;
+    if (!(t > -(double)(bits + 1))) return kBuckets - 1;
+    return -(int)(uint32_t)__double_as_longlong(t + kMagic);
   }
+  // 2^(t + bits) for t >= -(bits + 2), as kWhole and that.  t = step / 32 + r, |r| <= 1/64: 2^t = 2^(step / 32) e^(r ln 2), by five terms of the
+  // series, the next of which is below 3e-15
+  __device__ __forceinline__ u64 raw_units(double t) const {
+    const double z = t + kMagic, r = t - (z - kMagic);
+    const int step = (int)(uint32_t)__double_as_longlong(z);
+    constexpr double c = 0.69314718055994530942;
+    double p = __builtin_fma(r, c * c * c * c * c / 120, c * c * c * c / 24);
+    p = __builtin_fma(r, p, c * c * c / 6);
+    p = __builtin_fma(r, p, c * c / 2);
+    p = __builtin_fma(r, p, c);
+    p *= r;
+    const double base = table[step & (kSteps - 1)];
+    return (u64)__double_as_longlong(ldexp(__builtin_fma(base, p, base), (step >> 5) + bits) + kWhole);
+  }
+  __device__ __forceinline__ u64 units(double t) const { return t > -(double)(bits + 1) ? raw_units(t) - (u64)__double_as_longlong(kWhole) : 0; }
 };
 
 struct Shared {
@@ -67,22 +94,50 @@ struct Shared {
   u64 wave_sum[kWaves];
   uint32_t wave_count[kWaves];
   float wave_max[kWaves];
-  u64 low, high;
+  double table[kSteps];
+  u64 low, high, total;
   // an answer: classes before its last one and with it, their sum, and the last one
   u64 found_mass, found_rank;
   uint32_t found_count, found_bucket, listed;
 };
 
-// f(x, class) for all classes of a row, in no order
+// f(x, class) for all classes of a row, eight neighbours x at a time, in no order; -inf where eight begin with classes that others have, and behind the
+// last.  kBatch of a thread's loads are on their way.  The loop is not unrolled: a row takes few turns, and long code is fetched from memory for each.
+template <typename T, typename F>
+__device__ __forceinline__ void for_eights(const T *row, int classes, F &&f) {
+  constexpr int kTurn = kThreads * kVec;
+  const int last = max(classes - kVec, 0);
+  Raw8<T> r[kBatch];
+  int at = threadIdx.x * kVec;
+  if (classes >= kVec) {
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) r[j].load(row + min(at + j * kTurn, last), kVec);
+  } else {
+    r[0].load(row, classes);
+  }
+#pragma unroll 1
+  for (; at < classes; at += kTurn) {
+    float x[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = r[0].at(i);
+#pragma unroll
+    for (int j = 0; j + 1 < kBatch; ++j) r[j] = r[j + 1];
+    if (classes >= kVec) r[kBatch - 1].load(row + min(at + kBatch * kTurn, last), kVec);
+    const int first = min(at, last);
+    if (at != first || classes < kVec) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) x[i] = first + i >= at && first + i < classes ? x[i] : -INFINITY;
+    }
+    f(x, first);
+  }
+}
+// f(x, class) one by one
 template <typename T, typename F>
 __device__ __forceinline__ void for_row(const T *row, int classes, F &&f) {
-  for (int at = threadIdx.x * kVec; at < classes; at += kThreads * kVec) {
-    float x[kVec];
-    load8(row + at, classes - at, -INFINITY, x);
+  for_eights(row, classes, [&](const float(&x)[kVec], int id) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (x[i] > -INFINITY) f(x[i], at + i);
-  }
+    for (int i = 0; i < kVec; ++i) f(x[i], id + i);
+  });
 }
 
 __device__ __forceinline__ u64 wave_scan(u64 v) {
@@ -150,6 +205,29 @@ __device__ __forceinline__ int find_bucket(Shared &sh, const uint32_t *count, co
   return b;
 }
 
+// The list of `size` ranks in ascending order, one to a thread, ~0 behind them: by exchanges in a network, between lanes where they are near.
+__device__ __forceinline__ u64 sorted(Shared &sh, uint32_t size) {
+  const int tid = threadIdx.x;
+  u64 x = tid < (int)size ? sh.list[tid] : ~0ull;
+  int span = 64;
+  while (span < (int)size) span <<= 1;
+  for (int k = 2; k <= span; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      u64 y;
+      if (j < 64) {
+        y = __shfl_xor(x, j);
+      } else {
+        __syncthreads();
+        sh.list[tid] = x;
+        __syncthreads();
+        y = sh.list[tid ^ j];
+      }
+      const bool low = ((tid & j) == 0) == ((tid & k) == 0);  // this one keeps the lower
+      x = low == (x < y) ? x : y;
+    }
+  return x;
+}
+
 // The answer inside step `b` of the row, with found_count, found_mass (from the row's first class on) and found_rank set.
 template <typename T>
 __device__ void resolve(Shared &sh, const T *row, const Scale &sc, int classes, int b, Ask ask, uint32_t n, double target) {
@@ -157,16 +235,30 @@ __device__ void resolve(Shared &sh, const T *row, const Scale &sc, int classes, 
   uint32_t c0 = b ? sh.count[b - 1] : 0, size = sh.count[b] - c0;
   u64 m0 = b ? sh.mass[b - 1] : 0;
   u64 lo = 0, hi = ~0ull;
+  // f(x, class, rank) for the classes of the step whose rank is within lo .. hi.  Logits that are not near it are told apart in fp32, eight at once: its
+  // middle, and half its width and a little more.
+  const double middle = sc.most - (double)b / kSteps / sc.per, half = 0.5 / kSteps / sc.per;
+  const float mid = (float)middle, reach = (float)(half * 1.001 + 1e-6 * fabs(middle)) + 1e-37f;
+  auto of_step = [&](auto f) {
+    for_eights(row, classes, [&](const float(&x)[kVec], int id) {
+      float near = fabsf(x[0] - mid);
+#pragma unroll
+      for (int i = 1; i < kVec; ++i) near = fminf(near, fabsf(x[i] - mid));
+      if (near <= reach || sc.infinite || !(reach < 3e38f)) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (x[i] > -INFINITY && sc.bucket(sc.log_of(x[i])) == b) {
+            const u64 r = rank_of(x[i], id + i);
+            if (r >= lo && r <= hi) f(x[i], r);
+          }
+      }
+    });
+  };
   if (size > kList) {
     if (tid == 0) sh.low = ~0ull, sh.high = 0;
     __syncthreads();
     u64 least = ~0ull, most = 0;
-    for_row(row, classes, [&](float x, int id) {
-      if (sc.bucket(sc.log_of(x)) == b) {
-        const u64 r = rank_of(x, id);
-        least = r < least ? r : least, most = r > most ? r : most;
-      }
-    });
+    of_step([&](float, u64 r) { least = r < least ? r : least, most = r > most ? r : most; });
     atomicMin(&sh.low, least), atomicMax(&sh.high, most);
     __syncthreads();
     lo = sh.low, hi = sh.high;
@@ -175,13 +267,10 @@ __device__ void resolve(Shared &sh, const T *row, const Scale &sc, int classes, 
       const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > 11 ? bits - 11 : 0;
       for (int i = tid; i < kBuckets; i += kThreads) sh.sub_count[i] = 0, sh.sub_mass[i] = 0;
       __syncthreads();
-      for_row(row, classes, [&](float x, int id) {
-        const u64 r = rank_of(x, id);
-        if (r >= lo && r <= hi) {
-          const int at = (int)((r - lo) >> shift);
-          atomicAdd(&sh.sub_count[at], 1u);
-          atomicAdd(&sh.sub_mass[at], sc.units(sc.log_of(x)));
-        }
+      of_step([&](float x, u64 r) {
+        const int at = (int)((r - lo) >> shift);
+        atomicAdd(&sh.sub_count[at], 1u);
+        atomicAdd(&sh.sub_mass[at], sc.units(sc.log_of(x)));
       });
       __syncthreads();
       scan_buckets(sh, sh.sub_count, sh.sub_mass);
@@ -196,28 +285,9 @@ __device__ void resolve(Shared &sh, const T *row, const Scale &sc, int classes, 
   }
   if (tid == 0) sh.listed = 0;
   __syncthreads();
-  for_row(row, classes, [&](float x, int id) {
-    if (sc.bucket(sc.log_of(x)) == b) {
-      const u64 r = rank_of(x, id);
-      if (r >= lo && r <= hi) sh.list[atomicAdd(&sh.listed, 1u)] = r;
-    }
-  });
+  of_step([&](float, u64 r) { sh.list[atomicAdd(&sh.listed, 1u)] = r; });
   __syncthreads();
-  // sorted by exchanges in a network; what the list does not fill stays behind
-  if (tid >= (int)size) sh.list[tid] = ~0ull;
-  int span = 2;
-  while (span < (int)size) span <<= 1;
-  __syncthreads();
-  for (int k = 2; k <= span; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const int other = tid ^ j;
-      if (tid < span && other > tid) {
-        const u64 x = sh.list[tid], y = sh.list[other];
-        if ((x > y) == ((tid & k) == 0)) sh.list[tid] = y, sh.list[other] = x;
-      }
-      __syncthreads();
-    }
-  const u64 r = sh.list[tid];
+  const u64 r = sorted(sh, size);
   const u64 w = tid < (int)size ? sc.units(sc.log_of(value_of(r))) : 0;
   u64 m = w;
   uint32_t c = tid < (int)size;
@@ -227,23 +297,55 @@ __device__ void resolve(Shared &sh, const T *row, const Scale &sc, int classes, 
   __syncthreads();
 }
 
+// A bound that at least `k` threads' values reach, or all threads' least: the upper sixteen bits of the k-th largest value's order, by two counts of
+// eight bits.
+__device__ float bound_of(Shared &sh, float value, uint32_t k) {
+  const int tid = threadIdx.x;
+  const uint32_t up = (uint32_t)(~(rank_of(value, 0) >> kIdBits));  // ascends with the value
+  uint32_t prefix = 0, left = k;
+#pragma unroll
+  for (int round = 0; round < 2; ++round) {
+    const int shift = 24 - 8 * round;
+    if (tid < 256) sh.sub_count[tid] = 0;
+    __syncthreads();
+    if (round == 0 || (up >> 24) == prefix >> 24) atomicAdd(&sh.sub_count[255 - ((up >> shift) & 255)], 1u);
+    __syncthreads();
+    if (tid < 64) {
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = sh.sub_count[4 * tid + i], sum += c[i];
+      uint32_t before = wave_scan(sum) - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (before < left && before + c[i] >= left) sh.found_bucket = 255 - (4 * tid + i), sh.found_count = before;
+        before += c[i];
+      }
+    }
+    __syncthreads();
+    prefix |= sh.found_bucket << shift, left -= sh.found_count;
+    __syncthreads();
+  }
+  const float bound = __uint_as_float(prefix ^ ((prefix >> 31) ? 0x80000000u : 0xffffffffu));
+  return bound == bound ? bound : -INFINITY;  // the order of -inf, cut to sixteen bits, is that of a NaN
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const long long at = blockIdx.x;
   const T *row = (const T *)g.logits + at * g.ld;
+  const float temperature = g.temperature ? g.temperature[at] : 1.f, p = g.top_p ? g.top_p[at] : 1.f, least = g.min_p ? g.min_p[at] : 0.f;
+  const float u = fminf(fmaxf(g.uniform[at], 0.f), 0.99999994f);
+  const int wanted = g.top_k ? g.top_k[at] : 0;
 
-  float most = -INFINITY;
+  float mine = -INFINITY, most;
   bool nan = false;
-  for (int i = tid * kVec; i < g.classes; i += kThreads * kVec) {
-    float x[kVec];
-    load8(row + i, g.classes - i, -INFINITY, x);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) most = fmaxf(most, x[j]), nan |= x[j] != x[j];
-  }
-  most = wave_max_all(most);
+  for_row(row, g.classes, [&](float x, int) { mine = fmaxf(mine, x), nan |= x != x; });
+  most = wave_max_all(mine);
   if (lane == 0) sh.wave_max[wave] = most;
+  if (tid < kSteps) sh.table[tid] = exp2((double)tid / kSteps);
+  if (tid == 0) sh.listed = 0, sh.total = 0;
   nan = __syncthreads_or(nan);
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) most = fmaxf(most, sh.wave_max[w]);
@@ -256,14 +358,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
     return;
   }
 
-  const float temperature = g.temperature ? g.temperature[at] : 1.f;
   if (!(temperature > 0.f)) {
     if (tid == 0) sh.listed = 0xffffffffu;
     __syncthreads();
     uint32_t first = 0xffffffffu;
-    for_row(row, g.classes, [&](float x, int id) {
-      if (x == most) first = min(first, (uint32_t)id);
-    });
+    if (mine == most)
+      for_row(row, g.classes, [&](float x, int id) { first = x == most ? min(first, (uint32_t)id) : first; });
     if (first != 0xffffffffu) atomicMin(&sh.listed, first);
     __syncthreads();
     if (tid == 0) {
@@ -274,69 +374,160 @@ __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
     return;
   }
 
-  const Scale sc{(double)most, 1.4426950408889634074 / (double)temperature, g.bits};
-  for (int i = tid; i < kBuckets; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
-  __syncthreads();
-  uint32_t none = 0;  // without weight: no sum to add, and often most of a row
-  for_row(row, g.classes, [&](float x, int) {
-    const double t = sc.log_of(x);
-    const int b = sc.bucket(t);
-    if (b == kBuckets - 1) {
-      ++none;
-    } else {
-      atomicAdd(&sh.count[b], 1u);
-      atomicAdd(&sh.mass[b], sc.units(t));
-    }
-  });
-  if (none) atomicAdd(&sh.count[kBuckets - 1], none);
-  __syncthreads();
-  scan_buckets(sh, sh.count, sh.mass);
-
-  uint32_t kept = sh.count[kBuckets - 1];
-  u64 mass = sh.mass[kBuckets - 1];
-  const uint32_t k = g.top_k && g.top_k[at] > 0 ? (uint32_t)g.top_k[at] : kept;
-  if (k < kept) {
-    const int b = find_bucket(sh, sh.count, sh.mass, 0, 0, kCount, k, 0.0);
-    kept = k, mass = sh.mass[b];
-    if (b < kBuckets - 1 && sh.count[b] != k) {
-      resolve(sh, row, sc, g.classes, b, kCount, k, 0.0);
-      mass = sh.found_mass;
-      __syncthreads();
-    }
-  }
-  const float p = g.top_p ? g.top_p[at] : 1.f;
-  if (p < 1.f) {
-    const double target = (double)p * (double)mass;
-    resolve(sh, row, sc, g.classes, find_bucket(sh, sh.count, sh.mass, 0, 0, kAtLeast, 0, target), kAtLeast, 0, target);
-    kept = sh.found_count, mass = sh.found_mass;
-    __syncthreads();
-  }
-  const float least = g.min_p ? g.min_p[at] : 0.f;
-  if (least > 0.f) {
-    const int b = sc.bucket(log2((double)least));
-    const uint32_t c0 = b ? sh.count[b - 1] : 0;
-    if (c0 < kept) {
-      uint32_t c = 0;
-      u64 m = 0;
-      for_row(row, g.classes, [&](float x, int) {
-        const double t = sc.log_of(x);
-        if (sc.bucket(t) == b && exp2(t) >= (double)least) ++c, m += sc.units(t);
+  const Scale sc(most, temperature, g.bits, sh.table);
+  uint32_t kept;
+  u64 mass, rank = 0;
+  auto list = [&](float x, int id) {
+    const uint32_t i = atomicAdd(&sh.listed, 1u);
+    if (i < kList) sh.list[i] = rank_of(x, id);
+  };
+  const bool picks = wanted > 0 && wanted <= kPick, cuts = wanted <= 0 && least > 0.f && most < INFINITY;
+  uint32_t size = kList + 1;
+  if (g.classes <= kList || picks) {
+    const float bound = g.classes <= kList ? -INFINITY : bound_of(sh, mine, wanted);
+    if (g.classes <= kList || mine >= bound)
+      for_row(row, g.classes, [&](float x, int id) {
+        if (x >= bound && x > -INFINITY) list(x, id);
       });
-      block_scan(sh, m, c);
-      if (tid == kThreads - 1) sh.found_count = c0 + c, sh.found_mass = (b ? sh.mass[b - 1] : 0) + m;
-      __syncthreads();
-      if (sh.found_count < kept) kept = sh.found_count, mass = sh.found_mass;
-      if (kept == 0) kept = 1, mass = sc.units(0.0);
-      __syncthreads();
-    }
+    __syncthreads();
+    size = sh.listed;
+  } else if (cuts) {
+    // what reaches min-p is at or above this logit, and a little more is
+    const float from = most + (float)(log((double)least) * (double)temperature) * 1.00001f - 1e-5f * fabsf(most);
+    u64 m = 0;
+    uint32_t n = 0;
+    for_eights(row, g.classes, [&](const float(&x)[kVec], int id) {
+      float top = x[0];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        m += sc.raw_units(sc.log_of(x[i])), top = fmaxf(top, x[i]);
+        if (i % 4 == 3) asm volatile("" : "+v"(m));  // now: left for later, all of a turn's weights would wait in registers
+      }
+      n += kVec;
+      if (top >= from) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (x[i] >= from) list(x[i], id + i);
+      }
+    });
+    atomicAdd(&sh.total, m - n * (u64)__double_as_longlong(Scale::kWhole));
+    __syncthreads();
+    size = sh.listed;
+    if (size == 0) size = kList + 1;  // min-p leaves none: the first stays
   }
-  const float u = fminf(fmaxf(g.uniform[at], 0.f), 0.99999994f);
-  const double target = (double)u * (double)mass;
-  resolve(sh, row, sc, g.classes, find_bucket(sh, sh.count, sh.mass, 0, 0, kMore, 0, target), kMore, 0, target);
+  if (size <= kList) {
+    const u64 r = sorted(sh, size);
+    const double t = tid < (int)size ? sc.log_of(value_of(r)) : 0.0;
+    const u64 w = tid < (int)size ? sc.units(t) : 0;
+    u64 m = w;
+    uint32_t c = tid < (int)size;
+    __syncthreads();
+    block_scan(sh, m, c);
+    // the sum after top-k; then each rule's count
+    kept = wanted > 0 ? min((uint32_t)wanted, size) : size;
+    if (tid == (int)kept - 1) sh.found_mass = m;
+    if (tid == 0) sh.found_count = 0xffffffffu;
+    __syncthreads();
+    mass = cuts && g.classes > kList ? sh.total : sh.found_mass;
+    const double target = (double)p * (double)mass;
+    if (p < 1.f && tid < (int)size && (double)m >= target && (tid == 0 || (double)(m - w) < target)) sh.found_count = tid + 1;
+    __syncthreads();
+    kept = min(kept, sh.found_count);
+    if (least > 0.f) {
+      const int stay = __syncthreads_count(tid < (int)size && exp2(t) >= (double)least);
+      kept = min(kept, (uint32_t)max(stay, 1));
+    }
+    if (tid == (int)kept - 1) sh.found_mass = m;
+    __syncthreads();
+    mass = sh.found_mass;
+    const double goal = (double)u * (double)mass;
+    if ((double)m > goal && (double)(m - w) <= goal) sh.found_rank = r;
+    __syncthreads();
+    rank = sh.found_rank;
+  } else {
+    // Steps of the largest weights first: most answers lie there, few classes do, and the sums of the others need no atomics.  All steps where an
+    // answer lies behind them.
+    bool done = false;
+    for (int last = kNear; !done; last = kBuckets - 1) {
+      done = true;
+      const bool all = last == kBuckets - 1;
+      for (int i = tid; i < kBuckets; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
+      __syncthreads();
+      uint32_t others = 0;
+      u64 other_mass = 0;
+      for_eights(row, g.classes, [&](const float(&x)[kVec], int) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const double t = sc.log_of(x[i]);
+          const int b = sc.bucket(t);
+          const u64 w = sc.raw_units(t) - (u64)__double_as_longlong(Scale::kWhole);
+          const bool near = b < last;
+          if (near) atomicAdd(&sh.count[b], 1u), atomicAdd(&sh.mass[b], w);
+          others += !near & (x[i] > -INFINITY), other_mass += near ? 0 : w;
+          if (i % 4 == 3) asm volatile("" : "+v"(other_mass));
+        }
+      });
+      if (others) atomicAdd(&sh.count[kBuckets - 1], others), atomicAdd(&sh.mass[kBuckets - 1], other_mass);
+      __syncthreads();
+      scan_buckets(sh, sh.count, sh.mass);
+
+      kept = sh.count[kBuckets - 1], mass = sh.mass[kBuckets - 1];
+#pragma unroll 1
+      for (int rule = 0; rule < 3 && done; ++rule) {
+        Ask ask = kMore;
+        uint32_t n = 0;
+        double target = 0.0;
+        if (rule == 0) {
+          if (wanted <= 0 || (uint32_t)wanted >= kept) continue;
+          ask = kCount, n = (uint32_t)wanted;
+        } else if (rule == 1) {
+          if (!(p < 1.f)) continue;
+          ask = kAtLeast, target = (double)p * (double)mass;
+        } else {
+          if (least > 0.f) {
+            const int b = sc.bucket(fmin(log2((double)least), 0.0));
+            const uint32_t c0 = b ? sh.count[b - 1] : 0;
+            if (c0 < kept && !all && b >= last) {
+              done = false;
+              break;
+            }
+            if (c0 < kept) {
+              uint32_t c = 0;
+              u64 m = 0;
+              for_row(row, g.classes, [&](float x, int) {
+                const double t = sc.log_of(x);
+                if (x > -INFINITY && sc.bucket(t) == b && exp2(t) >= (double)least) ++c, m += sc.units(t);
+              });
+              block_scan(sh, m, c);
+              if (tid == kThreads - 1) sh.found_count = c0 + c, sh.found_mass = (b ? sh.mass[b - 1] : 0) + m;
+              __syncthreads();
+              if (sh.found_count < kept) kept = sh.found_count, mass = sh.found_mass;
+              if (kept == 0) kept = 1, mass = sc.units(0.0);
+              __syncthreads();
+            }
+          }
+          target = (double)u * (double)mass;
+        }
+        const int b = find_bucket(sh, sh.count, sh.mass, 0, 0, ask, n, target);
+        if (!all && b >= last) {
+          done = false;
+          break;
+        }
+        if (rule == 0 && (b == kBuckets - 1 || sh.count[b] == n)) {  // the whole step, or classes without weight
+          kept = n, mass = sh.mass[b];
+          continue;
+        }
+        resolve(sh, row, sc, g.classes, b, ask, n, target);
+        if (rule < 2) kept = sh.found_count, mass = sh.found_mass;
+        __syncthreads();
+      }
+    }
+    rank = sh.found_rank;
+  }
   if (tid == 0) {
-    g.tokens[at] = (int32_t)(sh.found_rank & ((1u << kIdBits) - 1));
+    g.tokens[at] = (int32_t)(rank & ((1u << kIdBits) - 1));
     if (g.kept) g.kept[at] = (int32_t)kept;
-    if (g.logp) g.logp[at] = (float)((sc.log_of(value_of(sh.found_rank)) + g.bits - log2((double)mass)) * 0.69314718055994530942);
+    if (g.logp) g.logp[at] = (float)((sc.log_of(value_of(rank)) + g.bits - log2((double)mass)) * 0.69314718055994530942);
   }
 }
 
