@@ -22,6 +22,7 @@ constexpr int kList = kThreads;
 constexpr int kPick = 600;    // largest top-k by the threads' largest: that many of 1024 threads hold about 900 classes
 constexpr int kSteps = 32;    // steps of a power of two
 constexpr int kNear = 12 * kSteps;
+constexpr int kValues = 4096;  // values of a bf16 row that are counted: 32 octaves of 128
 constexpr int kBatch = 4;     // 16-byte loads of a thread on their way
 constexpr int kIdBits = 22;  // classes <= 2^22
 
@@ -99,6 +100,11 @@ struct Shared {
   // an answer: classes before its last one and with it, their sum, and the last one
   u64 found_mass, found_rank;
   uint32_t found_count, found_bucket, listed;
+  // of a row of bf16: how often each value occurs, and the answer that lies among the occurrences of one
+  uint32_t times[kValues + PARLE_WAVE];
+  u64 found_before, found_weight;
+  uint32_t found_first;
+  float found_value;
 };
 
 // f(x, class) for all classes of a row, eight neighbours x at a time, in no order; -inf where eight begin with classes that others have, and behind the
@@ -329,6 +335,239 @@ __device__ float bound_of(Shared &sh, float value, uint32_t k) {
   return bound == bound ? bound : -INFINITY;  // the order of -inf, cut to sixteen bits, is that of a NaN
 }
 
+// A row of bf16 by the values that occur in it: 128 to an octave, of which kValues hold the largest ones down to what has no weight, but for a band around zero,
+// whose few classes are listed.  So only values have weights formed, and a rule's answer is how many occurrences of one stay.  False where the band
+// has too many classes.
+struct Rules {
+  float u, p, least;
+  int wanted;
+};
+__device__ __forceinline__ bool by_values(Shared &sh, const bf16_t *row, const Scale &sc, int classes, float largest, const Rules &rules, uint32_t &kept, u64 &mass,
+                                          u64 &rank) {
+  constexpr int kEach = kValues / kThreads;
+  const int tid = threadIdx.x;
+  // magnitudes as bf16 codes: those of positive values go from the largest logit's down to c0, of negative ones from c0 up to what has no weight
+  const float none = (float)(sc.most - (double)(sc.bits + 2) / sc.per);
+  const int top_p = largest > 0.f ? (int)(__float_as_uint(largest) >> 16) : -1, top_n = none < 0.f ? (int)min(__float_as_uint(-none) >> 16, 0x7f7fu) : -1;
+  // octaves of both sides, 32 together; a whole number of them below the larger side where the other has none
+  const int op = top_p >> 7, on = top_n >> 7;
+  const int c0 = max(top_n < 0 ? (op - 31) << 7 : top_p < 0 ? (on - 31) << 7 : ((op + on - 30 + 1) >> 1) << 7, 0);
+  const int count_p = top_p >= c0 ? top_p - c0 + 1 : 0, count_n = top_n >= c0 ? top_n - c0 + 1 : 0, shift_n = count_p - c0;
+  for (int i = tid; i < kValues; i += kThreads) sh.times[i] = 0;
+  if (tid == 0) sh.listed = 0, sh.found_count = 0;
+  __syncthreads();
+  uint32_t behind = 0;  // classes without weight
+  for_eights(row, classes, [&](const float(&x)[kVec], int id) {
+    bool others = false;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int bits = (int)(__float_as_uint(x[i]) >> 16), c = bits & 0x7fff;
+      const bool negative = bits >> 15, held = (uint32_t)(c - c0) < (uint32_t)(negative ? count_n : count_p);
+      // without a branch: what is not held counts where nobody looks, each lane in a place of its own
+      atomicAdd(&sh.times[held ? (negative ? c + shift_n : top_p - c) : kValues + (tid & 63)], 1u);
+      others |= !held;
+    }
+    if (others) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int bits = (int)(__float_as_uint(x[i]) >> 16), c = bits & 0x7fff;
+        const bool negative = bits >> 15;
+        if ((uint32_t)(c - c0) < (uint32_t)(negative ? count_n : count_p) || x[i] == -INFINITY) continue;
+        if (x[i] >= none) {
+          const uint32_t n = atomicAdd(&sh.listed, 1u);
+          if (n < kList) sh.list[n] = rank_of(x[i], id + i);
+        } else {
+          ++behind;
+        }
+      }
+    }
+  });
+  if (behind) atomicAdd(&sh.found_count, behind);
+  __syncthreads();
+  const uint32_t in_band = sh.listed;
+  if (in_band > kList) return false;
+  behind = sh.found_count;
+  // the band, sorted, and its sums
+  const u64 band_rank = sorted(sh, in_band);
+  const float band_value = value_of(band_rank);
+  const bool banded = tid < (int)in_band;
+  const double band_t = banded ? sc.log_of(band_value) : 0.0;
+  const u64 band_w = banded ? sc.units(band_t) : 0;
+  u64 band_m = band_w;
+  uint32_t band_c = banded;
+  __syncthreads();
+  block_scan(sh, band_m, band_c);
+  if (tid == kThreads - 1) sh.total = band_m;
+  __syncthreads();
+  const u64 band_mass = sh.total;
+  // a thread's values: their weights, and counts and masses in front of them
+  float value[kEach];
+  u64 weight[kEach], before_m = 0;
+  uint32_t times[kEach], before_c = 0;
+  bool stays[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = tid * kEach + i, c = at < count_p ? top_p - at : at - shift_n;
+    times[i] = sh.times[at];
+    value[i] = __uint_as_float((uint32_t)(at < count_p ? c : c | 0x8000) << 16);
+    const double t = times[i] ? sc.log_of(value[i]) : 0.0;
+    weight[i] = times[i] ? sc.units(t) : 0;
+    stays[i] = times[i] && rules.least > 0.f && exp2(t) >= (double)rules.least;
+    before_m += times[i] * weight[i], before_c += times[i];
+  }
+  {
+    u64 m = before_m;
+    uint32_t c = before_c;
+    block_scan(sh, m, c);
+    before_m = m - before_m, before_c = c - before_c;
+  }
+  // the band lies behind the positive values
+  auto in_front = [&](int i, uint32_t &c, u64 &m) {
+    c = before_c, m = before_m;
+    for (int j = 0; j < i; ++j) c += times[j], m += times[j] * weight[j];
+    if (tid * kEach + i >= count_p) c += in_band, m += band_mass;
+  };
+  u64 positive_m = 0;
+  uint32_t positive_c = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (tid * kEach + i == (count_p ? count_p - 1 : 0)) {
+      uint32_t c;
+      u64 m;
+      in_front(i, c, m);
+      sh.found_count = count_p ? c + times[i] : 0, sh.found_mass = count_p ? m + times[i] * weight[i] : 0;
+    }
+  if (tid == kThreads - 1) sh.found_first = before_c, sh.found_before = before_m;
+  __syncthreads();
+  positive_c = sh.found_count, positive_m = sh.found_mass;
+  __syncthreads();
+  if (tid == kThreads - 1) {
+    uint32_t c = before_c + in_band;
+    u64 m = before_m + band_mass;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) c += times[i], m += times[i] * weight[i];
+    sh.found_count = c, sh.found_mass = m;
+  }
+  __syncthreads();
+  kept = sh.found_count + behind, mass = sh.found_mass;
+  const uint32_t weighted = sh.found_count;
+  __syncthreads();
+  // the value, or the class of the band, that an answer lies in: sums in front of it and its weight
+  auto ask_for = [&](Ask ask, uint32_t n, double target) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      uint32_t c;
+      u64 m;
+      in_front(i, c, m);
+      if (times[i] && reached(ask, n, target, c + times[i], m + times[i] * weight[i]) && !(c && reached(ask, n, target, c, m)))
+        sh.found_first = c, sh.found_before = m, sh.found_weight = weight[i], sh.found_value = value[i], sh.found_rank = ~0ull;
+    }
+    const uint32_t c = positive_c + band_c - 1;
+    const u64 m = positive_m + band_m - band_w;
+    if (banded && reached(ask, n, target, c + 1, m + band_w) && !(c && reached(ask, n, target, c, m)))
+      sh.found_first = c, sh.found_before = m, sh.found_weight = band_w, sh.found_rank = band_rank;
+    __syncthreads();
+  };
+  // the fewest occurrences, one at least, that reach the target
+  auto occurrences = [&](Ask ask, double target) {
+    const u64 w = sh.found_weight, m = sh.found_before;
+    uint32_t r = w ? (uint32_t)fmin(fmax((target - (double)m) / (double)w, 1.0), 4.2e6) : 1;
+    while (r > 1 && reached(ask, 0, target, 0, m + (r - 1) * w)) --r;
+    while (w && !reached(ask, 0, target, 0, m + r * w)) ++r;
+    return r;
+  };
+  if (rules.wanted > 0 && (uint32_t)rules.wanted < kept) {
+    kept = (uint32_t)rules.wanted;
+    if (kept < weighted) {
+      ask_for(kCount, kept, 0.0);
+      mass = sh.found_before + (kept - sh.found_first) * sh.found_weight;
+      __syncthreads();
+    }
+  }
+  if (rules.p < 1.f) {
+    const double target = (double)rules.p * (double)mass;
+    ask_for(kAtLeast, 0, target);
+    const uint32_t r = occurrences(kAtLeast, target);
+    kept = sh.found_first + r, mass = sh.found_before + r * sh.found_weight;
+    __syncthreads();
+  }
+  if (rules.least > 0.f) {
+    if (tid == 0) sh.found_count = 1, sh.found_mass = sc.units(0.0);
+    __syncthreads();
+    uint32_t most_c = 0;
+    u64 most_m = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (stays[i]) {
+        in_front(i, most_c, most_m);
+        most_c += times[i], most_m += times[i] * weight[i];
+      }
+    if (banded && exp2(band_t) >= (double)rules.least && positive_c + band_c > most_c) most_c = positive_c + band_c, most_m = positive_m + band_m;
+    atomicMax(&sh.found_count, most_c);
+    __syncthreads();
+    if (most_c == sh.found_count && most_c > 1) sh.found_mass = most_m;
+    __syncthreads();
+    if (sh.found_count < kept) kept = sh.found_count, mass = sh.found_mass;
+    __syncthreads();
+  }
+  const double target = (double)rules.u * (double)mass;
+  ask_for(kMore, 0, target);
+  rank = sh.found_rank;
+  if (rank != ~0ull) return true;
+  // the class of that occurrence, in the order of classes: counted by ranges of them where there are many
+  uint32_t r = occurrences(kMore, target);
+  const float v = sh.found_value;
+  int from = 0, to = classes;
+  __syncthreads();
+  for (int again = 0; again < 2; ++again) {
+    if (tid == 0) sh.listed = 0;
+    __syncthreads();
+    for_eights(row, classes, [&](const float(&x)[kVec], int id) {
+      bool some = false;
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) some |= x[i] == v;
+      if (some) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (x[i] == v && id + i >= from && id + i < to) {
+            const uint32_t n = atomicAdd(&sh.listed, 1u);
+            if (n < kList) sh.list[n] = rank_of(v, id + i);
+          }
+      }
+    });
+    __syncthreads();
+    if (sh.listed <= kList) break;
+    for (int i = tid; i < kValues; i += kThreads) sh.times[i] = 0;
+    __syncthreads();
+    const int range = (classes + kValues - 1) / kValues;  // 1024 at most
+    for_row(row, classes, [&](float x, int id) {
+      if (x == v) atomicAdd(&sh.times[id / range], 1u);
+    });
+    __syncthreads();
+    uint32_t c = 0, each[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) each[i] = sh.times[tid * kEach + i], c += each[i];
+    u64 m = 0;
+    uint32_t upto = c;
+    block_scan(sh, m, upto);
+    upto -= c;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (upto < r && upto + each[i] >= r) sh.found_first = upto, sh.found_bucket = tid * kEach + i;
+      upto += each[i];
+    }
+    __syncthreads();
+    from = sh.found_bucket * range, to = min(from + range, classes), r -= sh.found_first;
+    __syncthreads();
+  }
+  const u64 x = sorted(sh, sh.listed);
+  __syncthreads();
+  if (tid == (int)r - 1) sh.found_rank = x;
+  __syncthreads();
+  rank = sh.found_rank;
+  return true;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
   __shared__ Shared sh;
@@ -381,9 +620,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
     const uint32_t i = atomicAdd(&sh.listed, 1u);
     if (i < kList) sh.list[i] = rank_of(x, id);
   };
+  bool done = false;
+  if constexpr (sizeof(T) == 2)
+    if (g.classes > kList && most < INFINITY && !(wanted > 0 && wanted <= kPick)) done = by_values(sh, row, sc, g.classes, most, Rules{u, p, least, wanted}, kept, mass, rank);
   const bool picks = wanted > 0 && wanted <= kPick, cuts = wanted <= 0 && least > 0.f && most < INFINITY;
   uint32_t size = kList + 1;
-  if (g.classes <= kList || picks) {
+  if (done) {
+  } else if (g.classes <= kList || picks) {
     const float bound = g.classes <= kList ? -INFINITY : bound_of(sh, mine, wanted);
     if (g.classes <= kList || mine >= bound)
       for_row(row, g.classes, [&](float x, int id) {
@@ -415,7 +658,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
     size = sh.listed;
     if (size == 0) size = kList + 1;  // min-p leaves none: the first stays
   }
-  if (size <= kList) {
+  if (done) {
+  } else if (size <= kList) {
     const u64 r = sorted(sh, size);
     const double t = tid < (int)size ? sc.log_of(value_of(r)) : 0.0;
     const u64 w = tid < (int)size ? sc.units(t) : 0;
@@ -447,7 +691,6 @@ __global__ __launch_bounds__(kThreads) void k_sample(Args g) {
   } else {
     // Steps of the largest weights first: most answers lie there, few classes do, and the sums of the others need no atomics.  All steps where an
     // answer lies behind them.
-    bool done = false;
     for (int last = kNear; !done; last = kBuckets - 1) {
       done = true;
       const bool all = last == kBuckets - 1;
