@@ -18,7 +18,7 @@ struct DecodeArgs {
   const void *q, *k, *v;
   const int32_t *lengths;
   void *k_cache, *v_cache, *out;
-  float *part;  // [sequences][heads][splits][dim + 2]: o, m, l
+  float *part, *stats;  // of a share: o [sequences][heads][splits][dim]; m and l [sequences][heads][splits][2]
   int sequences, capacity, heads, kv_heads, dim, window, sinks, splits, groups;
   float scale;
   long long ld_q, ld_kv, ld_out;
@@ -54,9 +54,10 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return half_sum(v);
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
+template <typename T, int DP, int WAVES>
+__global__ __launch_bounds__(WAVES *PARLE_WAVE) void k_decode(DecodeArgs g) {
   using Tl = Tile<T, DP>;
+  constexpr int kWaves = WAVES, kThreads = WAVES * PARLE_WAVE;
   constexpr int NS = DP / 32, ND = DP / 16;
   constexpr int kChunks = DP / Tl::kChunk, kTurns = kStep * kChunks / PARLE_WAVE;  // 16-byte pieces of a step's values, of a lane
   constexpr int kTileBytes = kStep * Tl::kRowBytes;
@@ -68,15 +69,14 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
   const int share = g.heads / g.kv_heads, g0 = group * kCols, cols = min(kCols, share - g0), head0 = kvh * share + g0;
   const int length = g.lengths[seq];
   T *out = (T *)g.out + (long long)seq * g.ld_out + (long long)head0 * g.dim;
-  float *part = g.part + ((long long)seq * g.heads + head0) * g.splits * (g.dim + 2);
+  float *part = g.part + ((long long)seq * g.heads + head0) * g.splits * g.dim;
+  float *stats = g.stats + ((long long)seq * g.heads + head0) * g.splits * 2;
   T *kc = (T *)g.k_cache + ((long long)seq * g.kv_heads + kvh) * g.capacity * g.dim;
   T *vc = (T *)g.v_cache + ((long long)seq * g.kv_heads + kvh) * g.capacity * g.dim;
 
   if (length <= 0) {
     if (split == 0)
       for (int i = tid; i < cols * g.dim; i += kThreads) out[i] = 0;
-    if (g.splits > 1)
-      for (int i = tid; i < cols; i += kThreads) part[((long long)i * g.splits + split) * (g.dim + 2) + g.dim + 1] = 0.f;
     return;
   }
   const Seen s = seen_of(length, g.window, g.sinks, g.capacity);
@@ -90,8 +90,8 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
     const T *kn = (const T *)g.k + (long long)seq * g.ld_kv + (long long)kvh * g.dim, *vn = (const T *)g.v + (long long)seq * g.ld_kv + (long long)kvh * g.dim;
     if (tid < g.dim) kc[(long long)slot * g.dim + tid] = kn[tid];
     if (tid >= 128 && tid - 128 < g.dim) vc[(long long)slot * g.dim + tid - 128] = vn[tid - 128];
+    __syncthreads();
   }
-  __syncthreads();
 
   Frag<T> qf[NS];
 #pragma unroll
@@ -205,12 +205,13 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
   for (int w = 0; w < kWaves; ++w) sum += stat[w][1][col] * (stat[w][0][col] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[w][0][col] - most));
   const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
   constexpr int kPitch = DP + 4;
-  float *red = (float *)&lds[0][0];                // [wave][column][d], over the tiles of values
-  constexpr int kAtOnce = sizeof(T) == 2 ? 2 : 4;  // wavefronts that find room there
+  float *red = (float *)&lds[0][0];                         // [wave][column][d], over the tiles of values
+  constexpr int kAtOnce = sizeof(T) == 2 ? kWaves / 2 : kWaves;  // wavefronts that find room there
   static_assert(kAtOnce * kCols * kPitch * 4 <= kWaves * kTileBytes, "");
-  float total[(kCols * DP + kThreads - 1) / kThreads];
+  constexpr int kSums = (kCols * DP + kThreads - 1) / kThreads;
+  float total[kSums];
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(total) / 4); ++i) total[i] = 0.f;
+  for (int i = 0; i < kSums; ++i) total[i] = 0.f;
 #pragma unroll
   for (int w0 = 0; w0 < kWaves; w0 += kAtOnce) {
     if (wave >= w0 && wave < w0 + kAtOnce) {
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(total) / 4); ++i) {
+    for (int i = 0; i < kSums; ++i) {
       const int at = tid + i * kThreads;
       for (int w = 0; w < kAtOnce; ++w) total[i] += red[(w * kCols + at / DP) * kPitch + at % DP];
     }
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
   if (wave == 0 && lane < kCols) stat[0][0][col] = most, stat[0][1][col] = sum;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(total) / 4); ++i) {
+  for (int i = 0; i < kSums; ++i) {
     const int at = tid + i * kThreads, cl = at / DP, d = at % DP;
     if (cl >= cols || d >= g.dim) continue;
     if (g.splits == 1) {
@@ -240,79 +241,113 @@ __global__ __launch_bounds__(kThreads) void k_decode(DecodeArgs g) {
       else
         out[(long long)cl * g.dim + d] = f32_to_bf16(v);
     } else {
-      float *p = part + ((long long)cl * g.splits + split) * (g.dim + 2);
-      p[d] = total[i];
-      if (d == 0) p[g.dim] = stat[0][0][cl], p[g.dim + 1] = stat[0][1][cl];
+      part[((long long)cl * g.splits + split) * g.dim + d] = total[i];
+      if (d == 0) *(f2 *)(stats + ((long long)cl * g.splits + split) * 2) = f2{stat[0][0][cl], stat[0][1][cl]};
     }
   }
 }
 
-// The shares of a head joined: one workgroup for a head, a thread for a column.
+// The shares of a head joined: a workgroup for a head, a wavefront for every fourth share, four columns to a lane.  All loads are on their way at once.
 template <typename T>
-__global__ __launch_bounds__(128) void k_decode_join(DecodeArgs g) {
-  const int head = blockIdx.x, seq = blockIdx.y, d = threadIdx.x;
-  if (g.lengths[seq] <= 0 || d >= g.dim) return;
-  const float *p = g.part + ((long long)seq * g.heads + head) * g.splits * (g.dim + 2);
-  float most = -INFINITY;
-  for (int i = 0; i < g.splits; ++i) most = fmaxf(most, p[(long long)i * (g.dim + 2) + g.dim]);
-  float sum = 0.f, o = 0.f;
-  for (int i = 0; i < g.splits; ++i) {
-    const float *x = p + (long long)i * (g.dim + 2);
-    const float f = x[g.dim] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[g.dim] - most);
-    sum += f * x[g.dim + 1], o += f * x[d];
+__global__ __launch_bounds__(kThreads) void k_decode_join(DecodeArgs g) {
+  constexpr int kMost = 256 / PARLE_WAVE;  // shares of a lane
+  __shared__ float factor[256];
+  __shared__ f4 sums[kWaves][32];
+  const int head = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (g.lengths[seq] <= 0) return;
+  const float *stats = g.stats + ((long long)seq * g.heads + head) * g.splits * 2;
+  const float *part = g.part + ((long long)seq * g.heads + head) * g.splits * g.dim;
+  float m[kMost], l[kMost], most = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int at = lane + i * PARLE_WAVE;
+    const f2 v = at < g.splits ? *(const f2 *)(stats + 2 * at) : f2{-INFINITY, 0.f};
+    m[i] = v.x, l[i] = v.y, most = fmaxf(most, v.x);
   }
-  T *out = (T *)g.out + (long long)seq * g.ld_out + (long long)head * g.dim;
-  if constexpr (sizeof(T) == 4)
-    out[d] = o / sum;
-  else
-    out[d] = f32_to_bf16(o / sum);
+  most = tok::wave_max_all(most);
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - most);
+    sum += f * l[i];
+    if (wave == 0) factor[lane + i * PARLE_WAVE] = f;
+  }
+  sum = tok::wave_sum_all(sum);
+  __syncthreads();
+  const int at = (lane & 31) * 4, half = lane >> 5;
+  f4 o = {0.f, 0.f, 0.f, 0.f};
+  if (at < g.dim) {
+#pragma unroll 4
+    for (int i = 2 * wave + half; i < g.splits; i += 2 * kWaves) o += factor[i] * *(const f4 *)(part + (long long)i * g.dim + at);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
+  if (half == 0) sums[wave][lane] = o;
+  __syncthreads();
+  if (threadIdx.x < 32 && at < g.dim) {
+    o = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+    const float inv = 1.f / sum;
+    store4((T *)g.out + (long long)seq * g.ld_out + (long long)head * g.dim + at, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  }
 }
 
 int visible(const parle_cache_desc &d) {
   const long long ring = (long long)d.capacity - d.sinks;
   return (int)(d.sinks + (d.window > 0 && d.window < ring ? d.window : ring));
 }
-// Shares of a cache: as many as fill the chip four workgroups to a compute unit, of kLeast tokens at least.
+// Few tokens of many sequences, or so few that there is nothing to share, go through one workgroup of eight wavefronts for a key head: a share for each of
+// several workgroups costs a second launch to join them.  1028 tokens, 8 key heads: 4 sequences take 15 us in one and 11.5 in shares, 32 sequences
+// 28 and 34.
+bool in_one(const parle_cache_desc &d) {
+  const long long wgs = (long long)d.sequences * d.kv_heads * tok::ceil_div(d.heads / d.kv_heads, kCols);
+  return visible(d) <= (wgs >= 128 ? 1536 : 512);
+}
+// Shares of a cache: as many as make two workgroups for a compute unit, of kLeast tokens at least; 16384 tokens of one sequence, 8 key heads, take
+// 17.7 us in 64 shares, 21.4 in 128.
 int splits_of(const parle_cache_desc &d) {
-  if (d.sequences == 0) return 1;
-  const long long groups = tok::ceil_div(d.heads / d.kv_heads, kCols), wgs = (long long)d.sequences * d.kv_heads * groups;
-  long long n = (1024 + wgs - 1) / wgs;
+  if (d.sequences == 0 || in_one(d)) return 1;
+  const long long wgs = (long long)d.sequences * d.kv_heads * tok::ceil_div(d.heads / d.kv_heads, kCols);
+  long long n = (512 + wgs - 1) / wgs;
   const long long most = tok::ceil_div(visible(d), kLeast);
   n = n < most ? n : most;
   return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
 }
 
-// ---- a prompt's rows into the caches: a thread takes eight elements of a token's head, of k or of v ----
+// ---- a prompt's rows into the caches: a wavefront takes a row, whose sequence and slot it looks up once, and a lane eight elements of a head ----
 struct StoreArgs {
   const void *k, *v;
   const int32_t *offsets, *lengths;
   void *k_cache, *v_cache;
   int tokens, sequences, capacity, kv_heads, dim, sinks;
-  long long ld_kv, items;
+  long long ld_kv;
 };
 template <typename T>
-__global__ __launch_bounds__(256) void k_store(StoreArgs g) {
-  const int per = g.dim / 8, row_items = 2 * g.kv_heads * per;
-  for (long long it = (long long)blockIdx.x * 256 + threadIdx.x; it < g.items; it += (long long)gridDim.x * 256) {
-    const int row = (int)(it / row_items), rest = (int)(it - (long long)row * row_items);
-    const int which = rest / (g.kv_heads * per), head = rest / per - which * g.kv_heads, e = (rest % per) * 8;
-    int lo = 0, hi = g.sequences;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (g.offsets[mid] <= row)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    const int begin = g.offsets[lo], end = g.offsets[lo + 1], length = g.lengths[lo];
-    const long long p = (long long)length - end + row;
-    if (row < begin || row >= end || p < 0 || !(p < g.sinks || p >= (long long)length - (g.capacity - g.sinks))) continue;
-    const int slot = slot_of((int)p, g.sinks, g.capacity);
-    const T *src = (const T *)(which ? g.v : g.k) + (long long)row * g.ld_kv + (long long)head * g.dim + e;
-    T *dst = (T *)(which ? g.v_cache : g.k_cache) + (((long long)lo * g.kv_heads + head) * g.capacity + slot) * g.dim + e;
-    const Frag<T> f = load_frag(src);
+__global__ __launch_bounds__(kThreads) void k_store(StoreArgs g) {
+  const int lane = threadIdx.x & 63, row = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+  if (row >= g.tokens) return;
+  int lo = 0, hi = g.sequences;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (g.offsets[mid] <= row)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const int begin = g.offsets[lo], end = g.offsets[lo + 1], length = g.lengths[lo];
+  const long long p = (long long)length - end + row;
+  if (row < begin || row >= end || p < 0 || !(p < g.sinks || p >= (long long)length - (g.capacity - g.sinks))) return;
+  const int slot = slot_of((int)p, g.sinks, g.capacity);
+  const long long head_step = (long long)g.capacity * g.dim, first = ((long long)lo * g.kv_heads * g.capacity + slot) * g.dim;
+  const int per = g.dim / 8, items = g.kv_heads * per;
+  const T *k = (const T *)g.k + row * g.ld_kv, *v = (const T *)g.v + row * g.ld_kv;
+  for (int it = lane; it < items; it += PARLE_WAVE) {
+    const int head = it / per, e = (it - head * per) * 8;
+    const Frag<T> fk = load_frag(k + it * 8), fv = load_frag(v + it * 8);  // a row's heads lie one behind the other
+    const long long at = first + head * head_step + e;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) *(u4 *)((char *)dst + 16 * i) = f.v[i];
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      *(u4 *)((char *)((T *)g.k_cache + at) + 16 * i) = fk.v[i];
+      *(u4 *)((char *)((T *)g.v_cache + at) + 16 * i) = fv.v[i];
+    }
   }
 }
 
@@ -320,34 +355,34 @@ __global__ __launch_bounds__(256) void k_store(StoreArgs g) {
 
 int64_t decode_scratch_bytes(const parle_cache_desc &d) {
   const int s = splits_of(d);
-  return s == 1 ? 0 : (int64_t)d.sequences * d.heads * s * (d.dim + 2) * 4;
+  return s == 1 ? 0 : (int64_t)d.sequences * d.heads * s * (d.dim + 2) * 4;  // dim is a multiple of 8, so both parts are aligned
 }
 
 hipError_t launch_attention_decode(hipStream_t st, const parle_cache_desc &d, const void *q, const void *k, const void *v, const int32_t *lengths,
                                    void *scratch, void *k_cache, void *v_cache, void *out) {
   const int groups = tok::ceil_div(d.heads / d.kv_heads, kCols), splits = splits_of(d);
-  DecodeArgs g{q,         k,       v,       lengths, k_cache, v_cache, out,    (float *)scratch, d.sequences, d.capacity, d.heads, d.kv_heads, d.dim,
+  DecodeArgs g{q,         k,       v,       lengths, k_cache, v_cache, out,    (float *)scratch, (float *)scratch + (int64_t)d.sequences * d.heads * splits * d.dim, d.sequences, d.capacity, d.heads, d.kv_heads, d.dim,
                d.window, d.sinks, splits, groups,  d.scale, d.ld_q,  d.ld_kv, d.ld_out};
   auto go = [&](auto *kernel, auto *join) {
-    kernel<<<dim3(splits, d.kv_heads * groups, d.sequences), kThreads, 0, st>>>(g);
+    kernel<<<dim3(splits, d.kv_heads * groups, d.sequences), in_one(d) ? 8 * PARLE_WAVE : 4 * PARLE_WAVE, 0, st>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    join<<<dim3(d.heads, d.sequences), 128, 0, st>>>(g);
+    join<<<dim3(d.heads, d.sequences), kThreads, 0, st>>>(g);
     return hipGetLastError();
   };
-  if (d.dtype) return d.dim <= 64 ? go(k_decode<bf16_t, 64>, k_decode_join<bf16_t>) : go(k_decode<bf16_t, 128>, k_decode_join<bf16_t>);
-  return d.dim <= 64 ? go(k_decode<float, 64>, k_decode_join<float>) : go(k_decode<float, 128>, k_decode_join<float>);
+#define PARLE_GO(T, DP) (in_one(d) ? go(k_decode<T, DP, 8>, k_decode_join<T>) : go(k_decode<T, DP, 4>, k_decode_join<T>))
+  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64) : PARLE_GO(bf16_t, 128);
+  return d.dim <= 64 ? PARLE_GO(float, 64) : PARLE_GO(float, 128);
+#undef PARLE_GO
 }
 
 hipError_t launch_attention_store(hipStream_t st, const parle_cache_desc &d, int tokens, const void *k, const void *v, const int32_t *offsets,
                                   const int32_t *lengths, void *k_cache, void *v_cache) {
-  const long long items = (long long)tokens * d.kv_heads * (d.dim / 8) * 2;
-  StoreArgs g{k, v, offsets, lengths, k_cache, v_cache, tokens, d.sequences, d.capacity, d.kv_heads, d.dim, d.sinks, d.ld_kv, items};
-  const long long wgs = (items + 255) / 256;
-  const int grid = (int)(wgs < 16384 ? wgs : 16384);
+  StoreArgs g{k, v, offsets, lengths, k_cache, v_cache, tokens, d.sequences, d.capacity, d.kv_heads, d.dim, d.sinks, d.ld_kv};
+  const int grid = tok::ceil_div(tokens, kWaves);
   if (d.dtype)
-    k_store<bf16_t><<<grid, 256, 0, st>>>(g);
+    k_store<bf16_t><<<grid, kThreads, 0, st>>>(g);
   else
-    k_store<float><<<grid, 256, 0, st>>>(g);
+    k_store<float><<<grid, kThreads, 0, st>>>(g);
   return hipGetLastError();
 }

@@ -32,6 +32,34 @@ __global__ __launch_bounds__(kThreads) void k_rope(Args g) {
   T *out = (T *)g.out + rep * g.out_stride + (long long)t0 * g.ld_out;
   const int32_t *pos = g.positions + ((long long)rep * g.tokens + t0) * g.axes;
 
+  // A piece: eight pairs as a and b, or sixteen elements that do not turn.  The first is on its way while sines are made.
+  float a[kVec], b[kVec];
+  auto place = [&](int it, int &piece, long long &from, long long &to) {
+    const int row = it / g.per_head, t = row / g.heads, head = row - t * g.heads;
+    piece = it - row * g.per_head;
+    from = t * g.ld + (long long)head * g.dim, to = t * g.ld_out + (long long)head * g.dim;
+    return t;
+  };
+  auto parts = [&](int piece, int &first, int &second, int &n, int &m) {
+    if (piece >= g.turned) {
+      first = 2 * g.pairs + (piece - g.turned) * 2 * kVec, second = first + kVec, n = g.dim - first, m = n - kVec;
+    } else if (INTERLEAVED) {
+      first = 2 * piece * kVec, second = first + kVec, n = 2 * g.pairs - first, m = n - kVec;
+    } else {
+      first = piece * kVec, second = first + g.pairs, n = m = g.pairs - first;
+    }
+  };
+  auto load = [&](int it) {
+    int piece, first, second, n, m;
+    long long from, to;
+    place(it, piece, from, to);
+    parts(piece, first, second, n, m);
+    load8(x + from + first, n, 0.f, a), load8(x + from + second, m, 0.f, b);
+  };
+  const int items = count * g.heads * g.per_head;
+  int it = tid;
+  if (it < items) load(it);
+
   for (int i = tid; i < count * g.pairs; i += kThreads) {
     const int t = i / g.pairs, p = i - t * g.pairs;
     int axis = 0;
@@ -44,41 +72,25 @@ __global__ __launch_bounds__(kThreads) void k_rope(Args g) {
   }
   __syncthreads();
 
-  for (int it = tid; it < count * g.heads * g.per_head; it += kThreads) {
-    const int row = it / g.per_head, piece = it - row * g.per_head, t = row / g.heads, head = row - t * g.heads;
-    const T *src = x + (long long)t * g.ld + (long long)head * g.dim;
-    T *dst = out + (long long)t * g.ld_out + (long long)head * g.dim;
-    if (piece >= g.turned) {
-      const int at = 2 * g.pairs + (piece - g.turned) * 2 * kVec, n = g.dim - at;
-      float a[kVec], b[kVec];
-      load8(src + at, n, 0.f, a), load8(src + at + kVec, n - kVec, 0.f, b);
-      store8(dst + at, n, a), store8(dst + at + kVec, n - kVec, b);
-      continue;
-    }
-    const int p = piece * kVec, n = g.pairs - p;
-    const f2 *cs = turn + t * g.pairs + p;
-    if constexpr (INTERLEAVED) {
-      float a[2][kVec];
-      load8(src + 2 * p, 2 * n, 0.f, a[0]), load8(src + 2 * p + kVec, 2 * n - kVec, 0.f, a[1]);
+  while (it < items) {
+    int piece, first, second, n, m;
+    long long from, to;
+    const int t = place(it, piece, from, to);
+    parts(piece, first, second, n, m);
+    if (piece < g.turned) {
+      const f2 *cs = turn + t * g.pairs + piece * kVec;
+      const int pairs = g.pairs - piece * kVec;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        const f2 w = i < n ? cs[i] : f2{0.f, 0.f};
-        float &u = a[i >> 2][2 * (i & 3)], &v = a[i >> 2][2 * (i & 3) + 1];
+        const f2 w = i < pairs ? cs[i] : f2{0.f, 0.f};
+        float &u = !INTERLEAVED ? a[i] : i < 4 ? a[2 * (i & 3)] : b[2 * (i & 3)], &v = !INTERLEAVED ? b[i] : i < 4 ? a[2 * (i & 3) + 1] : b[2 * (i & 3) + 1];
         const float y = u * w.x - v * w.y, z = u * w.y + v * w.x;
         u = y, v = z;
       }
-      store8(dst + 2 * p, 2 * n, a[0]), store8(dst + 2 * p + kVec, 2 * n - kVec, a[1]);
-    } else {
-      float a[kVec], b[kVec];
-      load8(src + p, n, 0.f, a), load8(src + g.pairs + p, n, 0.f, b);
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const f2 w = i < n ? cs[i] : f2{0.f, 0.f};
-        const float y = a[i] * w.x - b[i] * w.y, z = a[i] * w.y + b[i] * w.x;
-        a[i] = y, b[i] = z;
-      }
-      store8(dst + p, n, a), store8(dst + g.pairs + p, n, b);
     }
+    store8(out + to + first, n, a), store8(out + to + second, m, b);
+    it += kThreads;
+    if (it < items) load(it);
   }
 }
 
@@ -94,9 +106,10 @@ hipError_t launch_rope(hipStream_t st, const parle_rope_desc &d, const void *x, 
   if (g.per_head == 0) return hipSuccess;
   g.sign = d.inverse ? -1.f : 1.f;
   g.ld = d.ld, g.stride = d.stride, g.ld_out = d.ld_out, g.out_stride = d.out_stride;
-  // Tokens of a workgroup: four pieces a thread, so that sines are shared and memory has work, but 1024 workgroups before that.
+  // Tokens of a workgroup: about a piece for a thread, and 1024 workgroups before that.  Three times 4099 tokens of 20 heads take 55 us, 61 with four
+  // pieces a thread, where all workgroups make their sines at once and then all wait for memory.
   const long long items = (long long)d.heads * g.per_head;
-  long long n = 4 * kThreads / items;
+  long long n = kThreads / items;
   const long long spread = (long long)d.tokens * d.n / 1024;
   if (n > spread) n = spread;
   if (g.pairs > 0 && n > kPairs / g.pairs) n = kPairs / g.pairs;
