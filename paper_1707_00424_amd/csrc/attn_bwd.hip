@@ -31,26 +31,27 @@ __host__ __device__ __forceinline__ int reach(int key, int window, int chunk, in
   return (int)(e < tokens ? e : tokens);
 }
 
-template <typename T, int DP, bool DMA>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attn_dq(BwdArgs b) {
+// PARTS: as in the forward pass.
+template <typename T, int DP, int PARTS, bool DMA>
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 4 && DP == 128) || (PARTS > 1 && (sizeof(T) == 4 || DP > 64)) ? 1 : 2) void k_attn_dq(BwdArgs b) {
   const Args &g = b.a;
   using Tl = Tile<T, DP>;
-  constexpr int BN = sizeof(T) == 2 ? 64 : 32, NB = BN / 32, ND = DP / 32, NS = DP / 16;
+  constexpr int BN = sizeof(T) == 2 && PARTS == 1 ? 64 : 32, NB = BN / 32, ND = DP / 32, NS = DP / 16, kQueries = kRows / PARTS;
   constexpr int kTileBytes = BN * Tl::kRowBytes;
-  __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[2][PARTS][2][kTileBytes];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, part = wave % PARTS;
   const int hx = blockIdx.x % g.heads, kvh = hx % g.kv_heads, head = kvh * (g.heads / g.kv_heads) + hx / g.kv_heads;
   const int tile = g.tiles - 1 - blockIdx.x / g.heads, rep = blockIdx.y;
   const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
   const T *k = (const T *)g.k + rep * g.kv_stride + (long long)kvh * g.dim;
   const T *v = (const T *)g.v + rep * g.kv_stride + (long long)kvh * g.dim;
 
-  const int r0 = tile * kRows, w0 = r0 + wave * 32, row = w0 + (lane & 31), rowc = min(row, g.tokens - 1);
+  const int r0 = tile * kQueries, w0 = r0 + wave / PARTS * 32, row = w0 + (lane & 31), rowc = min(row, g.tokens - 1);
   const Span cov = covered(offsets, g.sequences, g.tokens);
   Sight s = sight_of({0, 0}, 0, 0, 0);
   if (row < g.tokens) s = sight_of(span_of(offsets, g.sequences, g.tokens, row), row, g.window, g.sinks);
-  const int rv0 = max(r0, cov.start), rv1 = min(r0 + kRows, cov.end) - 1;
+  const int rv0 = max(r0, cov.start), rv1 = min(r0 + kQueries, cov.end) - 1;
   int klo = 0, khi = 0, s0 = 0, s1 = 0;  // as in the forward pass
   if (rv0 <= rv1) {
     const Sight f = sight_of(span_of(offsets, g.sequences, g.tokens, rv0), rv0, g.window, g.sinks);
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
   delta = half_sum(delta);
   const long long stat = ((long long)rep * g.heads + head) * g.tokens + rowc;
   const float lse2 = g.lse[stat] * kLog2e;
-  if (row < g.tokens && h == 0) {
+  if (row < g.tokens && h == 0 && part == 0) {
     float *to = b.stats + 2 * (stat - rowc) + rowc;
     to[0] = -lse2, to[g.tokens] = -delta;
   }
@@ -101,13 +102,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
 #pragma unroll
     for (int d = 0; d < ND; ++d) dq[d] = zero16();
     auto base_of = [&](int t) { return t < nS ? s0 + t * BN : klo + (t - nS) * BN; };
-    auto fetch = [&](int t) { kl.load(lds[t & 1][0], base_of(t)), vl.load(lds[t & 1][1], base_of(t)); };
-    if (total > 0) fetch(0);
-    for (int t = 0; t < total; ++t) {
+    auto fetch = [&](int step) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        const int at = base_of(step * PARTS + i);
+        kl.load(lds[step & 1][i][0], at), vl.load(lds[step & 1][i][1], at);
+      }
+    };
+    const int steps = (total + PARTS - 1) / PARTS;
+    if (steps > 0) fetch(0);
+    for (int step = 0; step < steps; ++step) {
       arrive<0>();
-      if (t + 1 < total) fetch(t + 1);
-      const int kb = base_of(t);
-      const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+      if (step + 1 < steps) fetch(step + 1);
+      const int t = step * PARTS + part, kb = base_of(t);
+      const char *kt = lds[step & 1][part][0], *vt = lds[step & 1][part][1];
       const bool none = kb > w0 + 31 || (all_in && t >= nS && kb + BN - 1 < lo_first && kb >= sink_first);
       if (!none) {
         const bool whole = all_in && t >= nS && kb + BN - 1 <= w0 && kb >= lo_last;
@@ -170,6 +178,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
     return odd;
   };
   if (__syncthreads_or(pass(std::false_type{}))) pass(std::true_type{});
+  if constexpr (PARTS > 1) {  // the parts' sums meet, in order
+    float *red = (float *)&lds[0][0][0][0];
+    static_assert(kWaves * 16 * PARLE_WAVE * 4 <= (int)sizeof(lds), "");
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) red[(wave * 16 + i) * PARLE_WAVE + lane] = dq[d][i];
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int j = 1; j < PARTS; ++j) dq[d][i] += red[((wave + j) * 16 + i) * PARLE_WAVE + lane];
+      }
+    }
+    if (part) return;
+  }
   if (row >= g.tokens) return;
   T *out = (T *)b.dq + rep * g.q_stride + (long long)row * g.ld_q + (long long)head * g.dim;
 #pragma unroll
@@ -493,8 +519,14 @@ hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, c
   BwdArgs b{{q, k, v, offsets, (void *)out, (float *)lse, d.n, d.tokens, d.sequences, d.heads, d.kv_heads, d.dim, d.window, d.sinks, tiles, d.scale,
              d.ld_q, d.q_stride, d.ld_kv, d.kv_stride, d.ld_out, d.out_stride},
             dout, (float *)scratch, fp, far ? fp + far_elems(d) : nullptr, dq, dk, dv, chunk, chunks};
+  const int size = d.dtype ? 2 : 4;
+  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, size) && direct(d.tokens, d.ld_q, d.q_stride, d.n, size) &&
+                   direct(d.tokens, d.ld_out, d.out_stride, d.n, size);
+  const bool few = (long long)tiles * d.heads * d.n < 256;  // as in the forward pass
+  const int most = d.dtype || d.dim <= 64 ? 4 : 2;
   auto go = [&](auto *of_queries, auto *of_keys, auto *of_sinks) {
-    of_queries<<<dim3(tiles * d.heads, d.n), kThreads, 0, st>>>(b);
+    b.a.tiles = tok::ceil_div(d.tokens, few ? kRows / most : kRows);
+    of_queries<<<dim3(b.a.tiles * d.heads, d.n), kThreads, 0, st>>>(b);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int keys = kRows / parts;
@@ -505,15 +537,14 @@ hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, c
     of_sinks<<<dim3(chunks * d.kv_heads, d.n), 256, 0, st>>>(b);
     return hipGetLastError();
   };
-  const int size = d.dtype ? 2 : 4;
-  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, size) && direct(d.tokens, d.ld_q, d.q_stride, d.n, size) &&
-                   direct(d.tokens, d.ld_out, d.out_stride, d.n, size);
+#define PARLE_QUERIES(T, DP, MOST, DMA) (few ? k_attn_dq<T, DP, MOST, DMA> : k_attn_dq<T, DP, 1, DMA>)
 #define PARLE_KEYS(T, DP, MOST, DMA) (parts == 2 ? k_attn_dkv<T, DP, 2, DMA> : k_attn_dkv<T, DP, MOST, DMA>)
 #define PARLE_GO(T, DP, MOST)                                                                  \
-  (dma ? go(k_attn_dq<T, DP, true>, PARLE_KEYS(T, DP, MOST, true), k_attn_sinks<T>) \
-       : go(k_attn_dq<T, DP, false>, PARLE_KEYS(T, DP, MOST, false), k_attn_sinks<T>))
+  (dma ? go(PARLE_QUERIES(T, DP, MOST, true), PARLE_KEYS(T, DP, MOST, true), k_attn_sinks<T>) \
+       : go(PARLE_QUERIES(T, DP, MOST, false), PARLE_KEYS(T, DP, MOST, false), k_attn_sinks<T>))
   if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64, 4) : d.dim <= 96 ? PARLE_GO(bf16_t, 96, 4) : PARLE_GO(bf16_t, 128, 4);
   return d.dim <= 64 ? PARLE_GO(float, 64, 4) : PARLE_GO(float, 128, 2);
 #undef PARLE_KEYS
+#undef PARLE_QUERIES
 #undef PARLE_GO
 }

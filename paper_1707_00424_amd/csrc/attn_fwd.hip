@@ -7,18 +7,16 @@ using namespace attn;
 
 constexpr int kRows = 32 * kWaves;  // queries of a workgroup, 32 to a wavefront
 
-// Keys of a tile: two of them, of K and of V, are in LDS at a time.
-template <typename T>
-constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
-
-template <typename T, int DP, bool DMA>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void k_attn_fwd(Args g) {
+// PARTS wavefronts share queries: they take the tiles of keys in turn, and their maxima, sums and results meet in LDS, so that few queries still
+// make enough workgroups.
+template <typename T, int DP, int PARTS, bool DMA>
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 4 && DP == 128) || (PARTS > 1 && (sizeof(T) == 4 || DP > 64)) ? 1 : 2) void k_attn_fwd(Args g) {
   using Tl = Tile<T, DP>;
-  constexpr int BN = kKeys<T>, NB = BN / 32, ND = DP / 32, NS = DP / 16;
+  constexpr int BN = sizeof(T) == 2 && PARTS == 1 ? 64 : 32, NB = BN / 32, ND = DP / 32, NS = DP / 16, kQueries = kRows / PARTS;
   constexpr int kTileBytes = BN * Tl::kRowBytes;
-  __shared__ __attribute__((aligned(1024))) char lds[2][2][kTileBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[2][PARTS][2][kTileBytes];  // of keys and values, for each part, of two steps
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, part = wave % PARTS;
   const int hx = blockIdx.x % g.heads, kvh = hx % g.kv_heads, head = kvh * (g.heads / g.kv_heads) + hx / g.kv_heads;
   const int tile = g.tiles - 1 - blockIdx.x / g.heads, rep = blockIdx.y;
   const int32_t *offsets = g.offsets ? g.offsets + (long long)rep * (g.sequences + 1) : nullptr;
@@ -26,11 +24,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
   const T *k = (const T *)g.k + rep * g.kv_stride + (long long)kvh * g.dim;
   const T *v = (const T *)g.v + rep * g.kv_stride + (long long)kvh * g.dim;
 
-  const int r0 = tile * kRows, w0 = r0 + wave * 32, row = w0 + (lane & 31);
+  const int r0 = tile * kQueries, w0 = r0 + wave / PARTS * 32, row = w0 + (lane & 31);
   const Span cov = covered(offsets, g.sequences, g.tokens);
   Sight s = sight_of({0, 0}, 0, 0, 0);
   if (row < g.tokens) s = sight_of(span_of(offsets, g.sequences, g.tokens, row), row, g.window, g.sinks);
-  const int rv0 = max(r0, cov.start), rv1 = min(r0 + kRows, cov.end) - 1;
+  const int rv0 = max(r0, cov.start), rv1 = min(r0 + kQueries, cov.end) - 1;
 
   // Keys: [s0, s1) of the sinks in front of the window of the first row, then [klo, khi).  A sequence that begins inside the tile has its
   // sinks in the second part.
@@ -72,13 +70,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
     for (int d = 0; d < ND; ++d) o[d] = zero16();
     m = -INFINITY, l = 0.f;
     auto base_of = [&](int t) { return t < nS ? s0 + t * BN : klo + (t - nS) * BN; };
-    auto fetch = [&](int t) { kl.load(lds[t & 1][0], base_of(t)), vl.load(lds[t & 1][1], base_of(t)); };
-    if (total > 0) fetch(0);
-    for (int t = 0; t < total; ++t) {
+    auto fetch = [&](int step) {  // tiles behind the last have no rows that are seen
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        const int at = base_of(step * PARTS + i);
+        kl.load(lds[step & 1][i][0], at), vl.load(lds[step & 1][i][1], at);
+      }
+    };
+    const int steps = (total + PARTS - 1) / PARTS;
+    if (steps > 0) fetch(0);
+    for (int step = 0; step < steps; ++step) {
       arrive<0>();
-      if (t + 1 < total) fetch(t + 1);
-      const int kb = base_of(t);
-      const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+      if (step + 1 < steps) fetch(step + 1);
+      const int t = step * PARTS + part, kb = base_of(t);
+      const char *kt = lds[step & 1][part][0], *vt = lds[step & 1][part][1];
       const bool none = kb > w0 + 31 || (all_in && t >= nS && kb + BN - 1 < lo_first && kb >= sink_first);
       if (!none) {
         f16v sc[NB];
@@ -174,6 +179,41 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && DP == 128 ? 1 : 2) void
   if (__syncthreads_or(pass(std::false_type{}))) pass(std::true_type{});
 
   l = half_sum(l);
+  if constexpr (PARTS > 1) {
+    // at the largest of the parts' maxima; the first part sums, in order, a block of 32 elements at a time
+    float *red = (float *)&lds[0][0][0][0];
+    static_assert(kWaves * 16 * PARLE_WAVE * 4 <= (int)sizeof(lds), "");
+    __syncthreads();
+    red[wave * PARLE_WAVE + lane] = m;
+    __syncthreads();
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) most = fmaxf(most, red[(wave - part + i) * PARLE_WAVE + lane]);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
+    l *= f, m = most;
+    __syncthreads();
+    red[wave * PARLE_WAVE + lane] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) l += red[(wave - part + i) * PARLE_WAVE + lane];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) red[(wave * 16 + i) * PARLE_WAVE + lane] = o[d][i] * f;
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          o[d][i] *= f;
+#pragma unroll
+          for (int j = 1; j < PARTS; ++j) o[d][i] += red[((wave + j) * 16 + i) * PARLE_WAVE + lane];
+        }
+      }
+    }
+    if (part) return;
+  }
   if (row >= g.tokens) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T *out = (T *)g.out + rep * g.out_stride + (long long)row * g.ld_out + (long long)head * g.dim;
@@ -193,14 +233,18 @@ hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, c
                                 const int32_t *offsets, void *out, float *lse) {
   Args g{q,       k,      v,          offsets, out,        lse,     d.n,     d.tokens, d.sequences, d.heads, d.kv_heads,
          d.dim,   d.window, d.sinks, tok::ceil_div(d.tokens, kRows), d.scale, d.ld_q,  d.q_stride, d.ld_kv, d.kv_stride, d.ld_out, d.out_stride};
-  const dim3 grid(g.tiles * d.heads, d.n);
+  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, d.dtype ? 2 : 4);
+  // fewer workgroups of 128 queries than compute units: 32 queries each, four wavefronts to their keys
+  const bool few = (long long)g.tiles * d.heads * d.n < 256;
+  const int parts = d.dtype || d.dim <= 64 ? 4 : 2;  // of fp32 tiles of 128 elements LDS holds those of two
+  if (few) g.tiles = tok::ceil_div(d.tokens, kRows / parts);
   auto go = [&](auto *kernel) {
-    kernel<<<grid, kThreads, 0, st>>>(g);
+    kernel<<<dim3(g.tiles * d.heads, d.n), kThreads, 0, st>>>(g);
     return hipGetLastError();
   };
-  const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, d.dtype ? 2 : 4);
-#define PARLE_GO(T, DP) (dma ? go(k_attn_fwd<T, DP, true>) : go(k_attn_fwd<T, DP, false>))
-  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64) : d.dim <= 96 ? PARLE_GO(bf16_t, 96) : PARLE_GO(bf16_t, 128);
-  return d.dim <= 64 ? PARLE_GO(float, 64) : PARLE_GO(float, 128);
+#define PARLE_GO(T, DP, MOST) \
+  (dma ? (few ? go(k_attn_fwd<T, DP, MOST, true>) : go(k_attn_fwd<T, DP, 1, true>)) : (few ? go(k_attn_fwd<T, DP, MOST, false>) : go(k_attn_fwd<T, DP, 1, false>)))
+  if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64, 4) : d.dim <= 96 ? PARLE_GO(bf16_t, 96, 4) : PARLE_GO(bf16_t, 128, 4);
+  return d.dim <= 64 ? PARLE_GO(float, 64, 4) : PARLE_GO(float, 128, 2);
 #undef PARLE_GO
 }
