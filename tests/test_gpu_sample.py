@@ -111,6 +111,41 @@ def test_many_equal(gpu, dtype, classes):
     check(torch, pb, x, u, k=[classes // 2 + 1] * 24, p=[0.5] * 24, m=[0.9] * 24, t=[2.0, 0.25, 1.0, 1.0] * 6)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("classes", [40, 513, 1500, 9000])
+def test_more_rows_than_compute_units(gpu, dtype, classes):
+    """They go through smaller workgroups."""
+    torch, pb = gpu
+    R = 260
+    g = torch.Generator().manual_seed(classes + 1)
+    x = (3 * torch.randn(1, R, classes, generator=g)).to(torch.bfloat16 if dtype else torch.float32)
+    x[:, ::3, : classes // 3] = -math.inf
+    x[:, 1::7] = (x[:, 1::7] > 1).to(x.dtype)                                 # two values, one of them zero
+    x[:, 2::7] = 0.5
+    rand = lambda: torch.rand(R, generator=g).tolist()  # noqa: E731
+    pick = lambda v: [v[int(i)] for i in torch.randint(0, len(v), (R,), generator=g)]  # noqa: E731
+    check(torch, pb, x, rand(), pick([1.0, 0.7, 0.1, 3.0, 0.0]), pick([0, 1, 50, 299, 300, 301, 600, classes]), pick([1.0, 0.9, 0.5]), pick([0.0, 0.05, 0.5]))
+    check(torch, pb, x, rand())
+    check(torch, pb, x, rand(), k=pick([3, 400]))
+    check(torch, pb, x, rand(), p=pick([0.3, 0.95]))
+    check(torch, pb, x, rand(), m=pick([0.1, 1e-3, 1e-25]))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_zeros_of_both_signs_among_tiny_logits(gpu, dtype):
+    """A temperature as small as the logits: weights of all classes near zero differ, those of 0 and -0 do not."""
+    torch, pb = gpu
+    C = 2000
+    g = torch.Generator().manual_seed(8)
+    x = (torch.randn(8, C, generator=g) * 1e-37).to(torch.bfloat16 if dtype else torch.float32)
+    zero = torch.rand(8, C, generator=g) < 0.2
+    x = torch.where(zero, torch.where(torch.rand(8, C, generator=g) < 0.5, 0.0, -0.0).to(x.dtype), x)
+    x[4:] = x[4:].abs() * -1.0                                               # nothing above zero
+    for u in (0.0, 0.2, 0.5, 0.8, 0.99):
+        check(torch, pb, x[None], [u] * 8, t=[1e-37] * 8)
+        check(torch, pb, x[None], [u] * 8, t=[3e-37] * 8, p=[0.7] * 8, k=[1500] * 8)
+
+
 def test_special_rows(gpu):
     torch, pb = gpu
     inf, nan = math.inf, math.nan
