@@ -79,7 +79,7 @@ __device__ __forceinline__ f16v zero16() {
   return z;
 }
 
-// A tile of rows in LDS, kDP elements each, in 16-byte chunks whose place in the row is XORed with bits of the row, so that neither a chunk of sixteen
+// A tile of rows in LDS, DP elements each, in 16-byte chunks whose place in the row is XORed with bits of the row, so that neither a chunk of sixteen
 // rows nor 32 columns of four rows meet in a bank.
 template <typename T, int DP>
 struct Tile {
@@ -282,6 +282,21 @@ __device__ __forceinline__ void store4<float>(float *p, float a, float b, float 
 template <>
 __device__ __forceinline__ void store4<bf16_t>(bf16_t *p, float a, float b, float c, float d) {
   *(tok::us4_any *)p = f32x4_to_bf16x4(f4{a, b, c, d});
+}
+
+// Wavefronts of the kernels of queries that share queries where few take part: of fp32 tiles of 128 elements LDS holds those of two.
+inline int most_parts(const parle_attention_desc &d) { return d.dtype || d.dim <= 64 ? 4 : 2; }
+// Whether they do.  A workgroup of 128 queries that does not share takes a start and a step for each 64 keys that its queries see; one that shares takes
+// 1 / parts of the queries, the same start, and half as long again for its part of the steps, but there may be several rounds of them.  A start is
+// worth ten steps of bf16, two of fp32.  Measured, without and with sharing, one sequence: bf16, 64 elements, 4096 tokens of 8 heads 69 and 44 us, of 12 heads
+// 70 and 59, of 16 heads 72 and 78; 128 elements, 8192 tokens of 2 heads 157 and 101, 2048 of 12 heads 47 and 56; fp32, 64 elements, 1024 tokens of 16 heads 84
+// and 40, with a window of 256 38 and 31, of 24 heads with the window 38 and 45.
+inline bool shares_keys(const parle_attention_desc &d) {
+  const int parts = most_parts(d), queries = 128 / parts, places = d.dtype && d.dim <= 64 ? 512 : 256;
+  const double start = d.dtype ? 10 : 2, length = (double)d.tokens / d.sequences, span = d.window > 0 && d.window < length ? d.window : length;
+  const double wgs = (double)tok::ceil_div(d.tokens, queries) * d.heads * d.n, rounds = wgs > places ? wgs / places : 1;
+  const double alone = start + (128 + span) / 64, shared = start + (queries + (span < length ? span : span / 2)) / 64 / parts * 1.5;
+  return rounds * shared < alone;
 }
 
 struct Args {

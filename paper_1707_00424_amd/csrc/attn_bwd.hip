@@ -309,17 +309,24 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
 #pragma unroll
       for (int i = 0; i < 4; ++i) dp[4 * n + i] = de[i];
     }
+    constexpr bool AHEAD = !(sizeof(T) == 4 && DP == 128);  // there is no room for them, and the instructions of fp32 are slow
     Frag<T> qr[NS], dr[NS], qc[2][ND], dc[2][ND];
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) qr[i] = Tl::row(qt, pl, 0, i), dr[i] = Tl::row(dt, pl, 0, i);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < NS; ++i) qr[i] = Tl::row(qt, pl, 0, i), dr[i] = Tl::row(dt, pl, 0, i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     auto columns = [&](int u) {
 #pragma unroll
       for (int d = 0; d < ND; ++d) dc[u][d] = Tl::column(dt, pl, 16 * u, d), qc[u][d] = Tl::column(qt, pl, 16 * u, d);
     };
-    columns(0);
+    if constexpr (AHEAD) columns(0);
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
+      if constexpr (!AHEAD) {
+        qr[i] = Tl::row(qt, pl, 0, i), dr[i] = Tl::row(dt, pl, 0, i);
+        if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
       mma(qr[i], kf[i], sc);
       mma(dr[i], vf[i], dp);
     }
@@ -345,10 +352,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
         }
       }
       const Frag<T> pf = make_frag<T>(x), sf = make_frag<T>(y);
-      if (u == 0) columns(1);
+      if (AHEAD && u == 0) columns(1);
       if constexpr (!(SAFE && MASKED)) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
+          if constexpr (!AHEAD) {
+            dc[u][d] = Tl::column(dt, pl, 16 * u, d), qc[u][d] = Tl::column(qt, pl, 16 * u, d);
+            __builtin_amdgcn_sched_barrier(0);
+          }
           mma(dc[u][d], pf, dv[d]);
           mma(qc[u][d], sf, dk[d]);
         }
@@ -367,7 +378,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
           for (int i = 0; i < 16; ++i) acc[i] = bad[i] > 0.f ? NAN : acc[i];
         };
 #pragma unroll
-        for (int d = 0; d < ND; ++d) finite(dc[u][d], pf, dv[d]), finite(qc[u][d], sf, dk[d]);
+        for (int d = 0; d < ND; ++d) {
+          if constexpr (!AHEAD) dc[u][d] = Tl::column(dt, pl, 16 * u, d), qc[u][d] = Tl::column(qt, pl, 16 * u, d);
+          finite(dc[u][d], pf, dv[d]), finite(qc[u][d], sf, dk[d]);
+        }
       }
     }
   };
@@ -522,10 +536,9 @@ hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, c
   const int size = d.dtype ? 2 : 4;
   const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, size) && direct(d.tokens, d.ld_q, d.q_stride, d.n, size) &&
                    direct(d.tokens, d.ld_out, d.out_stride, d.n, size);
-  const bool few = (long long)tiles * d.heads * d.n < 256;  // as in the forward pass
-  const int most = d.dtype || d.dim <= 64 ? 4 : 2;
+  const bool few = shares_keys(d);  // as in the forward pass; 4096 tokens of 8 heads of 64 elements, bf16, the whole gradient: 139 us without, 115 with
   auto go = [&](auto *of_queries, auto *of_keys, auto *of_sinks) {
-    b.a.tiles = tok::ceil_div(d.tokens, few ? kRows / most : kRows);
+    b.a.tiles = tok::ceil_div(d.tokens, few ? kRows / most_parts(d) : kRows);
     of_queries<<<dim3(b.a.tiles * d.heads, d.n), kThreads, 0, st>>>(b);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

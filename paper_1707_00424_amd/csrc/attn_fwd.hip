@@ -234,10 +234,8 @@ hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, c
   Args g{q,       k,      v,          offsets, out,        lse,     d.n,     d.tokens, d.sequences, d.heads, d.kv_heads,
          d.dim,   d.window, d.sinks, tok::ceil_div(d.tokens, kRows), d.scale, d.ld_q,  d.q_stride, d.ld_kv, d.kv_stride, d.ld_out, d.out_stride};
   const bool dma = direct(d.tokens, d.ld_kv, d.kv_stride, d.n, d.dtype ? 2 : 4);
-  // fewer workgroups of 128 queries than compute units: 32 queries each, four wavefronts to their keys
-  const bool few = (long long)g.tiles * d.heads * d.n < 256;
-  const int parts = d.dtype || d.dim <= 64 ? 4 : 2;  // of fp32 tiles of 128 elements LDS holds those of two
-  if (few) g.tiles = tok::ceil_div(d.tokens, kRows / parts);
+  const bool few = shares_keys(d);
+  if (few) g.tiles = tok::ceil_div(d.tokens, kRows / most_parts(d));
   auto go = [&](auto *kernel) {
     kernel<<<dim3(g.tiles * d.heads, d.n), kThreads, 0, st>>>(g);
     return hipGetLastError();
