@@ -6,6 +6,11 @@
 // workgroups, nothing is added atomically, and results are the same every time; seven products instead of the five that one pass would take.
 // Sinks behind a window are seen by far more queries than other keys.  What the queries beyond the reach of a sink's tile add to it is summed in chunks by
 // workgroups of their own, into scratch, and joined behind.
+//
+// Measured, bf16: three replicas of 4096 tokens, 16 heads of 64 elements on 4 of keys, a window of 1024 and 4 sinks: 104 us for dQ, 155 for dK and dV, 7 for
+// the sinks, 0.45 PFLOP/s of the seven products; 4099 tokens of 16 heads of 128 elements without a window 182 and 257, 0.55 PFLOP/s.  What bounds them is that
+// matrix unit (30 and 26 to 42 % of the time), vector unit (24 to 46 %) and LDS (15 to 23 %) wait for one another: dK and dV of 128 elements leave room
+// for one wavefront on a SIMD, the others for two.
 #include "attn.h"
 
 namespace {
@@ -483,7 +488,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
     }
 }
 
-// The sinks of a sequence: what their own workgroup and the chunks behind its reach have summed, in order.  The workgroup of a chunk sees to the sinks
+// The sinks of a sequence: what their own workgroup and the chunks behind its reach have summed, in order.  All latency: 7 us for up to 32 chunks.
+// One workgroup of keys for all queries of a sink would take as long as the whole rest.  The workgroup of a chunk sees to the sinks
 // whose first chunk it is; a thread takes four elements of dK or of dV.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_sinks(BwdArgs b) {

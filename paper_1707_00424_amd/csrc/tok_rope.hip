@@ -3,6 +3,9 @@
 // The sines and cosines of a token are the same for its heads, so a workgroup makes those of its tokens once, in LDS, and then streams the
 // heads.  An angle is formed and reduced to a turn in 64 bits, where position * frequency is exact; sine and cosine of the rest, half a turn at most
 // either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the rest's rounding and two steps of the function.
+//
+// Three replicas of 4099 tokens, 20 heads of 80 elements of which 64 turn, fp32: 40 us, 3.9 TB/s for reads and writes; 8192 tokens of 40 heads of 128 elements in bf16
+// 36 us, 4.7 TB/s; 16 tokens 6 us, a start, sines and a load.
 #include "tok.h"
 
 namespace {
@@ -106,12 +109,10 @@ hipError_t launch_rope(hipStream_t st, const parle_rope_desc &d, const void *x, 
   if (g.per_head == 0) return hipSuccess;
   g.sign = d.inverse ? -1.f : 1.f;
   g.ld = d.ld, g.stride = d.stride, g.ld_out = d.ld_out, g.out_stride = d.out_stride;
-  // Tokens of a workgroup: about a piece for a thread, and 1024 workgroups before that.  Three times 4099 tokens of 20 heads take 55 us, 61 with four
-  // pieces a thread, where all workgroups make their sines at once and then all wait for memory.
+  // Tokens of a workgroup: a piece for a thread.  Three times 4099 tokens of 20 heads take 40 us, 47 with four pieces a thread, where all workgroups make their
+  // sines at once and then all wait for memory.
   const long long items = (long long)d.heads * g.per_head;
   long long n = kThreads / items;
-  const long long spread = (long long)d.tokens * d.n / 1024;
-  if (n > spread) n = spread;
   if (g.pairs > 0 && n > kPairs / g.pairs) n = kPairs / g.pairs;
   if (n < 1) n = 1;
   g.at_once = (int)n;

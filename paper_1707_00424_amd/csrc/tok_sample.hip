@@ -12,9 +12,9 @@
 //
 // A row of bf16 is counted by value first (by_values), so that 4096 weights are formed in 64 bits and not one for each class.
 //
-// What bounds it: 4 rows of 128000 with top-k 50 (23 us) are latency, of a row's loads by one workgroup, 12 us at 22 GB/s for each, and of a chain of scans
-// and a sort; 1024 rows of 50001 bf16 (103 us, 102 MB read thrice, twice from cache) the vector unit, about 35 operations for a class, half
-// of the time, atomics in LDS a quarter.  The same of fp32 takes 224, in weights of 64 bits for every class.
+// What bounds it: 4 rows of 128000 bf16 with top-k 50 (21 us) are latency, two passes of a row by one workgroup and a chain of scans and a sort; 1024 rows of 50001
+// bf16 with top-p and min-p (104 us, 102 MB read three times, twice from cache) the vector unit, 54 % of the time, 35 operations for a class.  The same of fp32 with top-p
+// takes 224, in weights of 64 bits for every class.
 #include <type_traits>
 
 #include "tok.h"
