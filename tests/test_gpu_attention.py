@@ -112,9 +112,23 @@ CASES = [
     (1, 1, 1600, [[0, 500, 1600]], 3, 1, 48, 64, 100, 0, 0),  # sinks over two tiles
     (1, 2, 700, [[0, 699], [100, 600]], 2, 1, 112, 0, 0, 0, 0),
 ]
+# so many workgroups that wavefronts share no queries, and two share keys
+MANY = [
+    (1, 4, 200, [[0, 90, 200]] * 4, 40, 40, 64, 30, 3, 0, 0),
+    (1, 4, 200, None, 40, 8, 40, 0, 0, 3, 5),
+    (1, 4, 140, [[0, 50, 139]] * 4, 24, 24, 128, 33, 5, 0, 0),
+    (1, 4, 140, None, 24, 24, 96, 0, 0, 1, 1),
+    (1, 4, 140, [[3, 70, 140]] * 4, 24, 6, 88, 20, 2, 0, 0),
+    (1, 4, 140, None, 24, 24, 104, 0, 0, 1, 0),
+    (0, 4, 140, [[0, 50, 139]] * 4, 40, 40, 64, 33, 5, 0, 0),
+    (0, 4, 140, None, 40, 10, 48, 0, 0, 1, 1),
+    (0, 4, 140, [[0, 50, 139]] * 4, 40, 20, 128, 33, 5, 0, 0),
+    (0, 4, 140, None, 40, 8, 72, 0, 0, 1, 0),
+    (1, 1, 700, [[0, 300, 690]], 48, 48, 64, 64, 4, 0, 0),      # the same with sinks that leave queries to chunks
+]
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(v) for i, v in enumerate(c) if i != 3))
+@pytest.mark.parametrize("case", CASES + MANY, ids=lambda c: "-".join(str(v) for i, v in enumerate(c) if i != 3))
 def test_forward_and_backward(gpu, case):
     torch, pb = gpu
     P = Problem(torch, pb, *case)
@@ -210,6 +224,44 @@ def test_what_is_not_seen_has_no_influence(gpu, dtype, bad):
     assert torch.equal(d0[rows][:, :H], d2[rows][:, :H])
     assert torch.equal(d0[~keys][:, H:], d2[~keys][:, H:])
     assert not torch.isfinite(d2[keys][:, H:].float()).all()
+
+
+@pytest.mark.parametrize("dtype,H,K,D", [(1, 40, 20, 64), (1, 24, 24, 128), (0, 40, 20, 64), (0, 40, 40, 128)])
+def test_what_is_not_seen_among_many_heads(gpu, dtype, H, K, D):
+    """The same where wavefronts share no queries: a NaN or an infinity in a replica's head changes nothing but what sees it."""
+    torch, pb = gpu
+    n, T, at, offsets = 4, 140, 100, [[0, 50, 139]] * 4
+    clean, dirty = (Problem(torch, pb, dtype, n, T, offsets, H, K, D, 33, 5) for _ in range(2))
+    heads = H + 2 * K
+    view = dirty.view(dirty.rows, dirty.stride, dirty.ld, heads)
+    see, keys, group = visible(T, offsets[0], 33, 5)[:, at], visible(T, offsets[0], 33, 5)[at], slice(0, H // K)
+    out, lse = clean.forward()
+    dout = torch.randn(out.numel(), generator=torch.Generator().manual_seed(1)).to(out.dtype).cuda()
+    a, grad = clean.view(out, clean.out_stride, clean.ld_out, H).cpu(), clean.view(clean.backward(out, lse, dout), clean.stride, clean.ld, heads).cpu()
+
+    def others(x, rows, first, count):
+        """x [n, T, heads, D] without the given rows of the heads first .. first + count - 1 of replica 0."""
+        x = x.clone()
+        x[0, rows, first:first + count] = 0
+        return x
+
+    for part, bad in ((H + K, math.inf), (H + K, math.nan), (H, math.nan)):
+        view[0, at, part, 5] = bad
+        got, _ = dirty.forward()
+        b = dirty.view(got, dirty.out_stride, dirty.ld_out, H).cpu()
+        assert torch.equal(others(a, see, 0, H // K), others(b, see, 0, H // K)) and not torch.isfinite(b[0, see][:, group, 5].float()).any()
+        d = dirty.view(dirty.backward(out, lse, dout), dirty.stride, dirty.ld, heads).cpu()
+        assert torch.equal(others(grad, see, 0, H // K)[:, :, :H], others(d, see, 0, H // K)[:, :, :H])
+        view[0, at, part, 5] = clean.x[0, at, part, 5].to(view.dtype)
+    view[0, at, 0, 9] = math.inf
+    bad_dout = dout.clone()
+    dirty.view(bad_dout, dirty.out_stride, dirty.ld_out, H)[0, at, 0, 3] = math.nan
+    d = dirty.view(dirty.backward(out, lse, bad_dout), dirty.stride, dirty.ld, heads).cpu()
+    one = torch.arange(T) == at
+    x, y = others(grad, one, 0, 1), others(d, one, 0, 1)
+    for first in (H, H + K):
+        x, y = others(x, keys, first, 1), others(y, keys, first, 1)
+    assert torch.equal(x, y) and not torch.isfinite(d[0, keys, H].float()).all()
 
 
 def test_gradient_by_differences(gpu):
