@@ -12,9 +12,9 @@
 //
 // A row of bf16 is counted by value first (by_values), so that 4096 weights are formed in 64 bits and not one for each class.
 //
-// What bounds it: 4 rows of 128000 bf16 with top-k 50 (21 us) are latency, two passes of a row by one workgroup and a chain of scans and a sort; 1024 rows of 50001
-// bf16 with top-p and min-p (104 us, 102 MB read three times, twice from cache) the vector unit, 54 % of the time, 35 operations for a class.  The same of fp32 with top-p
-// takes 224, in weights of 64 bits for every class.
+// What bounds it: 4 rows of 128000 bf16 with top-k 50 (20 us) are latency, two passes of a row by one workgroup and a chain of scans and a sort; 1024 rows of 50001
+// bf16 with top-p and min-p (92 us, 102 MB read three times, twice from cache) the vector unit, about 35 operations for a class.  The same of fp32 with top-p
+// takes 211, in weights of 64 bits for every class.
 #include <type_traits>
 
 #include "tok.h"
@@ -28,7 +28,6 @@ constexpr int kBuckets = 2048;
 constexpr int kSteps = 32;    // steps of a power of two
 constexpr int kNear = 12 * kSteps;
 constexpr int kValues = 4096;  // values of a bf16 row that are counted: 32 octaves of 128
-constexpr int kBatch = 4;     // 16-byte loads of a thread on their way
 constexpr int kIdBits = 22;  // classes <= 2^22
 
 struct Args {
@@ -180,26 +179,20 @@ struct Sampler {
     float found_value;
   };
 
-  // f(x, class) for all classes of a row, eight neighbours x at a time, in no order; -inf where eight begin with classes that others have, and behind the
-  // last.  kBatch of a thread's loads are on their way.  The loop is not unrolled: a row takes few turns, and long code is fetched from memory for each.
+  // f(x, class) for all classes of a row from the begin-th on, eight neighbours x at a time, in no order; -inf where eight begin with classes that others
+  // have, and behind the last.  One load of a thread is on its way, which is enough beside fifteen other wavefronts: four, moved from register to register,
+  // took 104 us for 92 (1024 rows of 50001 bf16).  The loop is not unrolled: a row takes few turns, and long code is fetched from memory for each.
   template <typename T, typename F>
-  static __device__ __forceinline__ void for_raw(const T *row, int classes, F &&f) {
+  static __device__ __forceinline__ void for_raw(const T *row, int classes, F &&f, int begin = 0) {
     constexpr int kTurn = kThreads * kVec;
     const int last = max(classes - kVec, 0);
-    Raw8<T> r[kBatch];
-    int at = threadIdx.x * kVec;
-    if (classes >= kVec) {
-  #pragma unroll
-      for (int j = 0; j < kBatch; ++j) r[j].load(row + min(at + j * kTurn, last), kVec);
-    } else {
-      r[0].load(row, classes);
-    }
+    int at = begin + threadIdx.x * kVec;
+    Raw8<T> next;
+    next.load(row + min(at, last), classes);
   #pragma unroll 1
     for (; at < classes; at += kTurn) {
-      Raw8<T> x = r[0];
-  #pragma unroll
-      for (int j = 0; j + 1 < kBatch; ++j) r[j] = r[j + 1];
-      if (classes >= kVec) r[kBatch - 1].load(row + min(at + kBatch * kTurn, last), kVec);
+      Raw8<T> x = next;
+      if (classes >= kVec) next.load(row + min(at + kTurn, last), kVec);
       const int first = min(at, last);
       if (at != first || classes < kVec) {
   #pragma unroll
@@ -660,11 +653,23 @@ struct Sampler {
     us8 down, top;
   #pragma unroll
     for (int i = 0; i < kVec; ++i) up[i] = (short)0x8000, down[i] = 0xff80, top[i] = 0;
-    for_raw(row, classes, [&](const Raw8<bf16_t> &r, int) {
+    auto add = [&](const Raw8<bf16_t> &r, int) {
       const us8 v = r.v;
       up = __builtin_elementwise_max(up, __builtin_bit_cast(s8, v));
       down = __builtin_elementwise_min(down, v), top = __builtin_elementwise_max(top, v);
-    });
+    };
+    // the row comes from memory: several loads of a thread at a time
+    constexpr int kAtOnce = 4, kBlock = kAtOnce * kThreads * kVec;
+    const int whole = classes / kBlock * kBlock;
+  #pragma unroll 1
+    for (int at = threadIdx.x * kVec; at < whole; at += kBlock) {
+      Raw8<bf16_t> r[kAtOnce];
+  #pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) r[j].load(row + at + j * kThreads * kVec, kVec);
+  #pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) add(r[j], 0);
+    }
+    if (whole < classes) for_raw(row, classes, add, whole);
     int p = up[0];
     uint32_t n = down[0], t = top[0];
   #pragma unroll
@@ -895,7 +900,7 @@ hipError_t launch_sample(hipStream_t st, const parle_sample_desc &d, const void 
   Args g{logits, uniform, temperature, top_k, top_p, min_p, tokens, kept, logp, d.classes, bits, d.ld};
   const int rows = d.n * d.rows;
   // More rows than compute units: workgroups of 512 threads, two to a compute unit, where one's serial steps hide behind the other's passes.  1024 rows of
-  // 50001 classes, bf16 without top-k, take 103 us against 126 in workgroups of 1024, of 1000 classes 38 and 53; 4 rows of 128000 40 and 35.
+  // 50001 classes, bf16 without top-k, take 91 us against 110 in workgroups of 1024, 300 rows 41 and 52; 256 rows 31 and 29, 4 rows of 128000 36 and 32.
   const bool many = rows > 256;
   auto go = [&](auto *kernel, int threads) {
     kernel<<<rows, threads, 0, st>>>(g);
