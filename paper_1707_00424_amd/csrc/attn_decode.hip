@@ -3,7 +3,7 @@
 // A cache is read once and nothing else matters, so its tokens are shared out over enough workgroups to keep memory busy, and their maxima, sums
 // and partial results are joined behind.  The query heads of a key head, up to sixteen at a time, are the sixteen columns of a matrix instruction:
 // S^T = K Q^T and O^T = V^T P^T as in the forward pass, in tiles of 16 keys.  A wavefront has the next 32 keys and values on their way in registers while
-// it multiplies: 64 sequences of up to 8192 tokens, 32 heads on 8 of keys of 128 elements, bf16: 1.63 GB in 297 us, 5.5 TB/s; 4 sequences of 1028
+// it multiplies: 64 sequences of up to 8192 tokens, 32 heads on 8 of keys of 128 elements, bf16: 1.63 GB in 297 us, 5.5 TB/s (a plain read of as much 5.9); 4 sequences of 1028
 // tokens 11.5 us, of which 8.3 are the shares and 3 to join them.
 #include "attn.h"
 
@@ -366,16 +366,18 @@ hipError_t launch_attention_decode(hipStream_t st, const parle_cache_desc &d, co
   const int groups = tok::ceil_div(d.heads / d.kv_heads, kCols), splits = splits_of(d);
   DecodeArgs g{q,         k,       v,       lengths, k_cache, v_cache, out,    (float *)scratch, (float *)scratch + (int64_t)d.sequences * d.heads * splits * d.dim, d.sequences, d.capacity, d.heads, d.kv_heads, d.dim,
                d.window, d.sinks, splits, groups,  d.scale, d.ld_q,  d.ld_kv, d.ld_out};
+  // fp32 rows of 128 elements leave no registers for eight wavefronts: 32 sequences of 512 tokens, 8 key heads, 37 us with eight, 30 with four
+  const bool eight = in_one(d) && (d.dtype || d.dim <= 64);
   auto go = [&](auto *kernel, auto *join) {
-    kernel<<<dim3(splits, d.kv_heads * groups, d.sequences), in_one(d) ? 8 * PARLE_WAVE : 4 * PARLE_WAVE, 0, st>>>(g);
+    kernel<<<dim3(splits, d.kv_heads * groups, d.sequences), (eight ? 8 : 4) * PARLE_WAVE, 0, st>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     join<<<dim3(d.heads, d.sequences), kThreads, 0, st>>>(g);
     return hipGetLastError();
   };
-#define PARLE_GO(T, DP) (in_one(d) ? go(k_decode<T, DP, 8>, k_decode_join<T>) : go(k_decode<T, DP, 4>, k_decode_join<T>))
+#define PARLE_GO(T, DP) (eight ? go(k_decode<T, DP, 8>, k_decode_join<T>) : go(k_decode<T, DP, 4>, k_decode_join<T>))
   if (d.dtype) return d.dim <= 64 ? PARLE_GO(bf16_t, 64) : PARLE_GO(bf16_t, 128);
-  return d.dim <= 64 ? PARLE_GO(float, 64) : PARLE_GO(float, 128);
+  return d.dim <= 64 ? PARLE_GO(float, 64) : go(k_decode<float, 128, 4>, k_decode_join<float>);
 #undef PARLE_GO
 }
 
