@@ -729,8 +729,16 @@ struct Sampler {
       if (i < kList) sh.list[i] = rank_of(x, id);
     };
     bool done = false;
-    if constexpr (sizeof(T) == 2)
-      if (g.classes > kList && most < INFINITY && !(wanted > 0 && wanted <= kPick)) done = by_values(sh, row, sc, g.classes, most, Rules{u, p, least, wanted}, kept, mass, rank);
+    if constexpr (sizeof(T) == 2) {
+      if (g.classes > kList && most < INFINITY && !(wanted > 0 && wanted <= kPick)) {
+        done = by_values(sh, row, sc, g.classes, most, Rules{u, p, least, wanted}, kept, mass, rank);
+        if (!done) {  // the list begins anew
+          __syncthreads();
+          if (tid == 0) sh.listed = 0;
+          __syncthreads();
+        }
+      }
+    }
     const bool picks = wanted > 0 && wanted <= kPick, cuts = wanted <= 0 && least > 0.f && most < INFINITY;
     uint32_t size = kList + 1;
     if (done) {

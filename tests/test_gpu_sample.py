@@ -146,6 +146,22 @@ def test_zeros_of_both_signs_among_tiny_logits(gpu, dtype):
         check(torch, pb, x[None], [u] * 8, t=[3e-37] * 8, p=[0.7] * 8, k=[1500] * 8)
 
 
+@pytest.mark.parametrize("rows", [4, 260])
+def test_more_zeros_than_are_listed(gpu, rows):
+    """bf16 rows of zeros of both signs below a few larger logits, with every rule."""
+    torch, pb = gpu
+    C = 6000
+    g = torch.Generator().manual_seed(9)
+    x = torch.where(torch.rand(1, rows, C, generator=g) < 0.5, 0.0, -0.0)
+    x[:, :, ::40] = 4 * torch.rand(1, rows, C // 40, generator=g)
+    x = x.bfloat16()
+    rand = lambda: torch.rand(rows, generator=g).tolist()  # noqa: E731
+    check(torch, pb, x, rand())
+    check(torch, pb, x, rand(), m=[0.5] * rows)
+    check(torch, pb, x, rand(), m=[0.01] * rows, p=[0.9] * rows)
+    check(torch, pb, x, rand(), k=[2000] * rows, p=[0.5] * rows, t=[0.5] * rows)
+
+
 def test_special_rows(gpu):
     torch, pb = gpu
     inf, nan = math.inf, math.nan
