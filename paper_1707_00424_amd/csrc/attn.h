@@ -153,11 +153,12 @@ struct Loader {
   long long ld;
   int last, dim;
   u4 desc;
-  uint32_t off[DMA ? kLoads : 1];
+  uint32_t off[DMA ? kLoads : 1], mine;  // a lane's places in the matrix, its wavefront's in a tile
 
   __device__ __forceinline__ void init(long long ld_, int dim_) {
     ld = ld_, dim = dim_;
     if constexpr (DMA) {
+      mine = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * kLoads * 1024);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int at = ((int)(threadIdx.x >> 6) * kLoads + i) * PARLE_WAVE + (threadIdx.x & 63), r = at / kRowChunks;
@@ -171,12 +172,13 @@ struct Loader {
     base = p, last = last_;
     if constexpr (DMA) desc = igemm_dev::buffer_desc(p, (uint32_t)(last + 1) * (uint32_t)(ld * sizeof(T)));
   }
-  __device__ __forceinline__ void load(char *tile, int first) const {
+  // from row `first` and column `shift` on
+  __device__ __forceinline__ void load(char *tile, int first, int shift = 0) const {
     if constexpr (DMA) {
-      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile, row = (uint32_t)first * (uint32_t)(ld * sizeof(T));
+      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile + mine;
+      const uint32_t row = (uint32_t)first * (uint32_t)(ld * sizeof(T)) + (uint32_t)(shift * sizeof(T));
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        igemm_dev::dma16(__builtin_amdgcn_readfirstlane(lds + ((threadIdx.x >> 6) * kLoads + i) * 1024), desc, off[i] + row, 0);
+      for (int i = 0; i < kLoads; ++i) igemm_dev::dma16(__builtin_amdgcn_readfirstlane(lds + i * 1024), desc, off[i] + row, 0);
     } else {
       u4 v[kTurns];
 #pragma unroll
@@ -184,7 +186,7 @@ struct Loader {
         const int at = (int)threadIdx.x + i * kThreads, r = at / kChunks, c = at % kChunks;
         v[i] = u4{0u, 0u, 0u, 0u};
         if ((ROWS * kChunks % kThreads == 0 || r < ROWS) && c * Tl::kChunk < dim)
-          v[i] = *(const u4_any *)(base + (long long)min(first + r, last) * ld + c * Tl::kChunk);
+          v[i] = *(const u4_any *)(base + (long long)min(first + r, last) * ld + shift + c * Tl::kChunk);
       }
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {

@@ -298,6 +298,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
   f16v dk[ND], dv[ND];
   Loader<T, DP, BQ, DMA> ql, dl;
   ql.init(g.ld_q, g.dim), dl.init(g.ld_out, g.dim);
+  // the rows of all query heads that share the keys: a head is a column to begin at
+  ql.from((const T *)g.q + rep * g.q_stride + (long long)kvh * group * g.dim, qhi - 1);
+  dl.from((const T *)b.dout + rep * g.out_stride + (long long)kvh * group * g.dim, qhi - 1);
   constexpr int kLoads = PARTS * 2 * Loader<T, DP, BQ, DMA>::kLoads + 1;
   typename Tl::Places pl;
   pl.init(lane);
@@ -395,19 +398,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 && DP == 64) ? 2 : 1) voi
     for (int d = 0; d < ND; ++d) dk[d] = zero16(), dv[d] = zero16();
     // the tile that is fetched next: query head of the group, first query; and this part's that is added next
     int fetch_head = -1, fetch_at = qhi, at = qlo + part * BQ;
-    const float *sp = nullptr;
+    const float *sp = b.stats + (((long long)rep * g.heads + kvh * group) - 1) * 2 * g.tokens;
     auto fetch = [&](int buf) {
 #pragma unroll
       for (int i = 0; i < PARTS; ++i) {
         if (fetch_at >= qhi) {
-          if (fetch_head + 1 < group) ++fetch_head;  // behind the last tile, the last head's again, so that loads keep their count
-          const int head = kvh * group + fetch_head;
-          ql.from((const T *)g.q + rep * g.q_stride + (long long)head * g.dim, qhi - 1);
-          dl.from((const T *)b.dout + rep * g.out_stride + (long long)head * g.dim, qhi - 1);
-          sp = b.stats + ((long long)rep * g.heads + head) * 2 * g.tokens;
+          if (fetch_head + 1 < group) ++fetch_head, sp += 2LL * g.tokens;  // behind the last tile, the last head's again, so that loads keep their count
           fetch_at = qlo;
         }
-        ql.load(lds[buf][i][0], fetch_at), dl.load(lds[buf][i][1], fetch_at);
+        ql.load(lds[buf][i][0], fetch_at, fetch_head * g.dim), dl.load(lds[buf][i][1], fetch_at, fetch_head * g.dim);
         if (i == part) {
           if constexpr (DMA)
             igemm_dev::dma4(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&stats[buf][wave][0][0]),
