@@ -7,10 +7,11 @@
 // Sinks behind a window are seen by far more queries than other keys.  What the queries beyond the reach of a sink's tile add to it is summed in chunks by
 // workgroups of their own, into scratch, and joined behind.
 //
-// Measured, bf16: three replicas of 4096 tokens, 16 heads of 64 elements on 4 of keys, a window of 1024 and 4 sinks: 104 us for dQ, 155 for dK and dV, 7 for
-// the sinks, 0.45 PFLOP/s of the seven products; 4099 tokens of 16 heads of 128 elements without a window 182 and 257, 0.55 PFLOP/s.  What bounds them is that
-// matrix unit (30 and 26 to 42 % of the time), vector unit (24 to 46 %) and LDS (15 to 23 %) wait for one another: dK and dV of 128 elements leave room
-// for one wavefront on a SIMD, the others for two.
+// Measured, bf16: three replicas of 4096 tokens, 16 heads of 64 elements on 4 of keys, a window of 1024 and 4 sinks: 247 us, 0.51 PFLOP/s of the seven
+// products, of which dQ takes 42 %, dK and dV 55 %, the sinks 3; 4099 tokens of 16 heads of 128 elements without a window 383 us, 0.63 PFLOP/s, 39 and 61 %.
+// What bounds them is that matrix unit (30 and 27 to 47 % of the time), vector unit (24 to 45 %) and LDS (15 to 24 %) wait for one another: dK and dV of 128
+// elements leave room for one wavefront on a SIMD, the others for two.  With one, the scalar operations in front of a step's loads count as well (1000 of
+// 3900 cycles before all heads of a group shared a descriptor).
 #include "attn.h"
 
 namespace {
