@@ -410,10 +410,11 @@ struct Sampler {
     // magnitudes as bf16 codes: those of positive values go from the largest logit's down to c0, of negative ones from c0 up to what has no weight
     const float none = (float)(sc.most - (double)(sc.bits + 2) / sc.per);
     const int top_p = largest > 0.f ? (int)(__float_as_uint(largest) >> 16) : -1, top_n = none < 0.f ? (int)min(__float_as_uint(-none) >> 16, 0x7f7fu) : -1;
-    // octaves of both sides, 32 together; a whole number of them below the larger side where the other has none
+    // Octaves of both sides, 32 together at most, so that places are kValues at most: as deep on one as on the other, but 32 of the larger side where the
+    // other has none or none as large, a largest logit just above zero for one, which is of the band then.
     const int op = top_p >> 7, on = top_n >> 7;
     // (zeros are of the band: both are one value)
-    const int c0 = max(top_n < 0 ? (op - 31) << 7 : top_p < 0 ? (on - 31) << 7 : ((op + on - 30 + 1) >> 1) << 7, 1);
+    const int c0 = max(max((op + on - 30 + 1) >> 1, max(op, on) - 31) * 128, 1);
     const int count_p = top_p >= c0 ? top_p - c0 + 1 : 0, count_n = top_n >= c0 ? top_n - c0 + 1 : 0, shift_n = count_p - c0;
     // Places: the positive values', two for the band, the negative values', and those of what has no weight, a lane's own.  As whole numbers positive
     // values go down to count_p, negative ones, which are their magnitude less 2^15, up.

@@ -162,6 +162,44 @@ def test_more_zeros_than_are_listed(gpu, rows):
     check(torch, pb, x, rand(), k=[2000] * rows, p=[0.5] * rows, t=[0.5] * rows)
 
 
+@pytest.mark.parametrize("rows", [5, 260])
+def test_a_largest_logit_just_above_zero(gpu, rows):
+    """bf16 rows whose largest logit is tiny and whose others are not: far more octaves lie below zero than above."""
+    torch, pb = gpu
+    C = 5000
+    g = torch.Generator().manual_seed(10)
+    x = -3 * torch.randn(1, rows, C, generator=g).abs()
+    x[:, :, ::7] *= 1e-3
+    x[:, ::2, 3::5] = -math.inf
+    x[:, 1::4, 500:] = -2.0                                                   # thousands of one value
+    tiny = torch.tensor([1e-9, 1e-12, 1e-20, 1e-30, 1e-40])[torch.arange(rows) % 5]
+    x[0, torch.arange(rows), torch.randint(0, C, (rows,), generator=g)] = tiny
+    x = x.bfloat16()
+    rand = lambda: torch.rand(rows, generator=g).tolist()  # noqa: E731
+    check(torch, pb, x, rand())
+    check(torch, pb, x, rand(), t=[1.0, 0.1, 5.0, 0.01] * (rows // 4) + [1.0] * (rows % 4))
+    check(torch, pb, x, rand(), p=[0.9] * rows)
+    check(torch, pb, x, rand(), m=[0.2] * rows)
+    check(torch, pb, x, rand(), p=[0.5] * rows, m=[0.05] * rows, k=[2000] * rows)
+
+
+@pytest.mark.parametrize("C,most,t", [(20000, 7.15625, 0.21069972217082977), (10000, 7.90625, 0.2281261533498764)])
+def test_weights_that_end_just_below_zero(gpu, C, most, t):
+    """bf16 rows whose last weight is that of a logit just below zero: far more octaves lie above zero than below."""
+    torch, pb = gpu
+    g = torch.Generator().manual_seed(11)
+    x = most * torch.rand(4, C, generator=g)
+    x[1] = most * 2.0 ** (-34 * torch.rand(C, generator=g))                   # all octaves alike
+    x[2, ::3] *= -1.0
+    x[3, ::2] = -math.inf
+    x[:, 17] = most
+    x = x.bfloat16()[None]
+    for u in (0.0, 0.3, 0.999999):
+        check(torch, pb, x, [u] * 4, t=[t] * 4)
+        check(torch, pb, x, [u] * 4, t=[t] * 4, p=[0.9, 0.999999, 0.5, 0.99] * 1)
+        check(torch, pb, x, [u] * 4, t=[t] * 4, m=[1e-3] * 4, k=[1500] * 4)
+
+
 def test_special_rows(gpu):
     torch, pb = gpu
     inf, nan = math.inf, math.nan
