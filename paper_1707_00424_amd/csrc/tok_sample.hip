@@ -586,13 +586,15 @@ struct Sampler {
     ask_for(kMore, 0, target);
     rank = sh.found_rank;
     if (rank != ~0ull) return true;
-    // the class of that occurrence, in the order of classes: counted by ranges of them where there are many
+    // The class of that occurrence, in the order of classes.  Where more have the value than are listed, it is looked for in one of kValues ranges of
+    // them, known by counts, and again in a part of that, until the list holds what is left.
     uint32_t r = occurrences(kMore, target);
     const float v = sh.found_value;
     const bf16_t code = (bf16_t)(__float_as_uint(v) >> 16);
     int from = 0, to = classes;
     __syncthreads();
-    for (int again = 0; again < 2; ++again) {
+  #pragma unroll 1
+    while (true) {
       if (tid == 0) sh.listed = 0;
       __syncthreads();
       for_raw(row, classes, [&](const Raw8<bf16_t> &x, int id) {
@@ -610,9 +612,9 @@ struct Sampler {
       if (sh.listed <= kList) break;
       for (int i = tid; i < kValues; i += kThreads) sh.times[i] = 0;
       __syncthreads();
-      const int range = (classes + kValues - 1) / kValues;  // 1024 at most
+      const int range = (to - from + kValues - 1) / kValues;
       for_row(row, classes, [&](float x, int id) {
-        if (x == v) atomicAdd(&sh.times[id / range], 1u);
+        if (x == v && id >= from && id < to) atomicAdd(&sh.times[(id - from) / range], 1u);
       });
       __syncthreads();
       uint32_t c = 0, each[kEach];
@@ -628,7 +630,7 @@ struct Sampler {
         upto += each[i];
       }
       __syncthreads();
-      from = sh.found_bucket * range, to = min(from + range, classes), r -= sh.found_first;
+      from += sh.found_bucket * range, to = min(from + range, to), r -= sh.found_first;
       __syncthreads();
     }
     const u64 x = sorted(sh, sh.listed);

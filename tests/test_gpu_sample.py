@@ -200,6 +200,28 @@ def test_weights_that_end_just_below_zero(gpu, C, most, t):
         check(torch, pb, x, [u] * 4, t=[t] * 4, m=[1e-3] * 4, k=[1500] * 4)
 
 
+@pytest.mark.parametrize("rows,C", [(257, 2200000), (257, 1 << 22), (3, 1 << 22)])
+def test_millions_of_equal_logits(gpu, rows, C):
+    """bf16: each row's classes are equal or -inf, so the token is known: weights are one, and u times their number has 46 bits at most."""
+    torch, pb = gpu
+    ids = torch.arange(C, device="cuda")
+    patterns = [ids >= 0, ids % 3 == 1, (ids >= C // 2) | (ids == 5), ids < 700]
+    x = torch.empty(1, rows, C, dtype=torch.bfloat16, device="cuda")
+    left = [p.nonzero()[:, 0] for p in patterns]
+    for i, p in enumerate(patterns):
+        x[0, i::4] = torch.where(p, 1.5, -math.inf).to(x.dtype)
+    u = torch.rand(1, rows, generator=torch.Generator().manual_seed(12))
+    u[0, :8] = torch.tensor([0.0, 0.5, 0.25, 0.75, 0.99999994, 0.99999994, 0.0, 0.99999994][:rows])
+    tokens, kept = (torch.full((1, rows), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    desc = pb.parle_sample_desc(1, 1, rows, C, C)
+    sc = torch.empty(max(16, pb.parle_k_sample_scratch_bytes(desc)), dtype=torch.uint8, device="cuda")
+    pb.parle_k_sample(desc, x, u.cuda(), None, None, None, None, sc, tokens, kept, None)
+    for i in range(rows):
+        of = left[i % 4]
+        assert int(kept[0, i]) == len(of)
+        assert int(tokens[0, i]) == int(of[math.floor(float(u[0, i]) * len(of))]), i
+
+
 def test_special_rows(gpu):
     torch, pb = gpu
     inf, nan = math.inf, math.nan
