@@ -141,14 +141,14 @@ struct Tile {
 
 // Rows of a matrix that go into tiles of ROWS rows, by all threads of a workgroup.  With DMA they go straight into LDS, arrive some time later
 // (kLoads loads of each wavefront a tile) and are zeros behind the last row; without, they have arrived in front of the next barrier, and the last row
-// stands for those behind it.  Columns from `dim` on are zeros.  DMA needs rows of whole 16 bytes and a matrix of less than 2^31 of them (`direct`).
+// stands for those behind it.  Columns from `dim` on are zeros.  DMA needs rows of whole 16 bytes, less than 2^31 bytes with those behind the last (`direct`).
 template <typename T, int DP, int ROWS, bool DMA>
 struct Loader {
   using Tl = Tile<T, DP>;
   static constexpr int kChunks = DP / Tl::kChunk, kTurns = (ROWS * kChunks + kThreads - 1) / kThreads;
   static constexpr int kRowChunks = Tl::kPitch / Tl::kChunk, kLoads = ROWS * Tl::kRowBytes / (kWaves * PARLE_WAVE * 16);
   static_assert(ROWS * Tl::kRowBytes == kLoads * kWaves * PARLE_WAVE * 16, "a tile is whole loads of all wavefronts");
-  static constexpr uint32_t kFar = 0x80000000u;  // beyond any buffer, also with a row's offset added
+  static constexpr uint32_t kFar = 0x80000000u;  // beyond any buffer, also with a row's offset, less than 2^31, added
   const T *base;
   long long ld;
   int last, dim;
@@ -196,9 +196,11 @@ struct Loader {
     }
   }
 };
-// Whether a matrix can go straight into LDS.
+// Whether a matrix can go straight into LDS.  Tiles begin at a row that is there and end up to 126 rows behind the last, by places of less than 2^31 bytes
+// as well: beyond that they would come round to the first ones.
+constexpr int kRowsBehind = 128;
 inline bool direct(int tokens, int64_t ld, int64_t stride, int n, int size) {
-  return ld * size % 16 == 0 && (n == 1 || stride * size % 16 == 0) && (long long)tokens * ld * size < 1LL << 31;
+  return ld * size % 16 == 0 && (n == 1 || stride * size % 16 == 0) && (tokens + (long long)kRowsBehind) * ld * size < 1LL << 31;
 }
 // What was loaded into registers is there.  In front of a loop whose loads go to LDS: the compiler, which does not count those, would wait for registers
 // loaded before the loop at their first use in it, and so for all that is on its way.

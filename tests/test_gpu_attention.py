@@ -326,6 +326,32 @@ def test_offsets_beyond_32_bits(gpu):
     assert torch.equal(torch.as_strided(far, (T, 3, D), (ld, D, 1)), d.reshape(T, 3, D))
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T,row_bytes", [(1, 805306368), (1, (1 << 31) - 16), (3, 1 << 29), (16, 100663296), (16, (1 << 31) // 143 // 16 * 16), (16, (1 << 31) // 144 // 16 * 16)])
+def test_few_rows_far_apart(gpu, dtype, T, row_bytes):
+    """Tensors that end with their last row's heads: the tiles' rows behind the last lie far beyond, and beyond 2^32 bytes."""
+    torch, pb = gpu
+    t, D = dt(torch, dtype), 64
+    ld = row_bytes // (2 if dtype else 4)
+    x = torch.randn(T, 3 * D, generator=torch.Generator().manual_seed(6)).to(t).cuda()
+    far = torch.empty((T - 1) * ld + 3 * D, dtype=t, device="cuda")
+    rows = torch.as_strided(far, (T, 3 * D), (ld, 1))
+    rows.copy_(x)
+    results = []
+    for r, step in ((far, ld), (x, 3 * D)):
+        flat = r.reshape(-1)
+        desc = pb.parle_attention_desc(dtype, 1, T, 1, 1, 1, D, 0, 0, D ** -0.5, step, 0, step, 0, step, 0)
+        out, d = torch.empty_like(flat), torch.empty_like(flat)
+        lse = torch.empty(1, 1, T, device="cuda")
+        pb.parle_k_attention_forward(desc, flat, flat[D:], flat[2 * D:], None, out, lse)
+        sc = torch.empty(pb.parle_k_attention_scratch_bytes(desc), dtype=torch.uint8, device="cuda")
+        pb.parle_k_attention_backward(desc, flat, flat[D:], flat[2 * D:], None, out, lse, flat[2 * D:], sc, d, d[D:], d[2 * D:])
+        view = lambda v, c: torch.as_strided(v, (T, c), (step, 1)).clone()  # noqa: E731
+        results.append((view(out, D), lse, view(d, 3 * D)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and torch.isfinite(a.float()).all()
+
+
 def test_graph_and_stream(gpu):
     """Captured once and replayed between eager runs on other data, and run on a stream of its own: every result is the eager one."""
     torch, pb = gpu
