@@ -91,6 +91,11 @@ struct Scale {
   }
   __device__ __forceinline__ u64 raw_units(double t) const { return (u64)__double_as_longlong(power(t, bits) + kWhole); }  // as kWhole and that
   __device__ __forceinline__ u64 units(double t) const { return t > -(double)(bits + 1) ? raw_units(t) - (u64)__double_as_longlong(kWhole) : 0; }
+  // whether a class' weight is at least `least` > 0, fp32's smallest included: also of one too small to be counted
+  __device__ __forceinline__ bool at_least(float x, float least) const {
+    const float y = infinite ? (x == INFINITY ? 0.f : -1e30f) : x;
+    return power(fmax(((double)y - most) * per, -160.0), 0) >= (double)least;
+  }
 };
 
 __device__ __forceinline__ void hide(Raw8<bf16_t> &r, int i) { r.v[i] = 0xff80; }
@@ -407,8 +412,9 @@ struct Sampler {
                                             u64 &rank) {
     constexpr int kEach = kValues / kThreads;
     const int tid = threadIdx.x;
-    // magnitudes as bf16 codes: those of positive values go from the largest logit's down to c0, of negative ones from c0 up to what has no weight
-    const float none = (float)(sc.most - (double)(sc.bits + 2) / sc.per);
+    // magnitudes as bf16 codes: those of positive values go from the largest logit's down to c0, of negative ones from c0 up to what has no weight and does
+    // not reach min-p
+    const float none = (float)(sc.most - fmax((double)(sc.bits + 2), rules.least > 0.f ? 1.0 - log2((double)rules.least) : 0.0) / sc.per);
     const int top_p = largest > 0.f ? (int)(__float_as_uint(largest) >> 16) : -1, top_n = none < 0.f ? (int)min(__float_as_uint(-none) >> 16, 0x7f7fu) : -1;
     // Octaves of both sides, 32 together at most, so that places are kValues at most: as deep on one as on the other, but 32 of the larger side where the
     // other has none or none as large, a largest logit just above zero for one, which is of the band then.
@@ -447,8 +453,7 @@ struct Sampler {
     const u64 band_rank = sorted(sh, in_band);
     const float band_value = value_of(band_rank);
     const bool banded = tid < (int)in_band;
-    const double band_t = banded ? sc.log_of(band_value) : 0.0;
-    const u64 band_w = banded ? sc.units(band_t) : 0;
+    const u64 band_w = banded ? sc.units(sc.log_of(band_value)) : 0;
     u64 band_m = band_w;
     uint32_t band_c = banded;
     __syncthreads();
@@ -469,9 +474,8 @@ struct Sampler {
       times[i] = at < count_p ? sh.times[at] : at < count_p + count_n ? sh.times[at + 2] : 0;
       weight[i] = 0;
       if (times[i]) {
-        const double t = sc.log_of(value(i));
-        weight[i] = sc.units(t);
-        stays |= (uint32_t)(rules.least > 0.f && sc.power(t, 0) >= (double)rules.least) << i;
+        weight[i] = sc.units(sc.log_of(value(i)));
+        stays |= (uint32_t)(rules.least > 0.f && sc.at_least(value(i), rules.least)) << i;
       }
       before_m += times[i] * weight[i], before_c += times[i];
     }
@@ -571,7 +575,7 @@ struct Sampler {
           in_front(i, most_c, most_m);
           most_c += times[i], most_m += times[i] * weight[i];
         }
-      if (banded && sc.power(band_t, 0) >= (double)rules.least && positive_c + band_c > most_c) most_c = positive_c + band_c, most_m = positive_m + band_m;
+      if (banded && sc.at_least(band_value, rules.least) && positive_c + band_c > most_c) most_c = positive_c + band_c, most_m = positive_m + band_m;
       if (tid == 0) sh.found_count = 1, sh.found_mass = sc.units(0.0);
       __syncthreads();
       const uint32_t c = wave_most(most_c);
@@ -780,8 +784,7 @@ struct Sampler {
     if (done) {
     } else if (size <= kList) {
       const u64 r = sorted(sh, size);
-      const double t = tid < (int)size ? sc.log_of(value_of(r)) : 0.0;
-      const u64 w = tid < (int)size ? sc.units(t) : 0;
+      const u64 w = tid < (int)size ? sc.units(sc.log_of(value_of(r))) : 0;
       u64 m = w;
       uint32_t c = tid < (int)size;
       __syncthreads();
@@ -797,7 +800,7 @@ struct Sampler {
       __syncthreads();
       kept = min(kept, sh.found_count);
       if (least > 0.f) {
-        const int stay = __syncthreads_count(tid < (int)size && sc.power(t, 0) >= (double)least);
+        const int stay = __syncthreads_count(tid < (int)size && sc.at_least(value_of(r), least));
         kept = min(kept, (uint32_t)max(stay, 1));
       }
       if (tid == (int)kept - 1) sh.found_mass = m;
@@ -858,7 +861,7 @@ struct Sampler {
                 u64 m = 0;
                 for_row(row, g.classes, [&](float x, int) {
                   const double t = sc.log_of(x);
-                  if (x > -INFINITY && sc.bucket(t) == b && sc.power(t, 0) >= (double)least) ++c, m += sc.units(t);
+                  if (x > -INFINITY && sc.bucket(t) == b && sc.at_least(x, least)) ++c, m += sc.units(t);
                 });
                 block_scan(sh, m, c);
                 if (tid == kThreads - 1) sh.found_count = c0 + c, sh.found_mass = (b ? sh.mass[b - 1] : 0) + m;

@@ -222,6 +222,23 @@ def test_millions_of_equal_logits(gpu, rows, C):
         assert int(tokens[0, i]) == int(of[math.floor(float(u[0, i]) * len(of))]), i
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,C", [(6, 300), (6, 5000), (300, 2000)])
+def test_a_min_p_below_what_is_counted(gpu, dtype, rows, C):
+    """Weights under 2^-52 of the largest are nothing to a sum, but min-p still says which of their classes stay."""
+    torch, pb = gpu
+    g = torch.Generator().manual_seed(13)
+    x = (3 * torch.randn(1, rows, C, generator=g)).to(torch.bfloat16 if dtype else torch.float32)
+    x[:, 1::3, ::2] = -math.inf
+    x[:, 2::3, 7:9] = math.inf
+    u = torch.rand(rows, generator=g).tolist()
+    for t in (0.05, 0.2):
+        for m in (1e-15, 1e-17, 1e-25, 1e-38, 1e-44):
+            check(torch, pb, x, u, t=[t] * rows, m=[m] * rows)
+        check(torch, pb, x, u, t=[t] * rows, m=[1e-25] * rows, k=[C - 100] * rows, p=[0.99] * rows)
+        check(torch, pb, x, u, t=[t] * rows, m=[1e-30] * rows, k=[C - 100] * rows)
+
+
 def test_special_rows(gpu):
     torch, pb = gpu
     inf, nan = math.inf, math.nan
