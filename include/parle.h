@@ -567,7 +567,7 @@ typedef struct {
 /* out = softmax(scale * q k^T over the tokens seen) v, lse [n][heads][tokens] fp32 its log sum of exponentials (may be NULL).  Sequence b of
  * replica a has rows offsets[a][b] .. offsets[a][b + 1] - 1, offsets [n][sequences + 1] ascending from 0 at least to `tokens` at most; NULL, with
  * one sequence, is all rows.  Rows outside get out 0 and lse -inf.  A token that is not seen has no influence, whatever it holds; a NaN or an infinity in a
- * value that is seen makes NaN (or that infinity) of its column of out.  Of the probabilities, bf16 tensors have their products with v in bf16, sums are fp32. */
+ * value that is seen makes NaN (or that infinity) of its column of out, and a row whose scores are all -inf has a softmax of NaN and an lse of -inf.  Of the probabilities, bf16 tensors have their products with v in bf16, sums are fp32. */
 parle_status parle_k_attention_forward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
                                        const int32_t *offsets, void *out, float *lse);
 /* With P = e^(scale * q k^T - lse) of the forward pass, delta = sum_d dout * out and dS = P * (dout v^T - delta):

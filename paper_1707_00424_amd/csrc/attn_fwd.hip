@@ -223,7 +223,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 4 && DP == 128) || (PARTS >
     if (part) return;
   }
   if (row >= g.tokens) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  // no sum: a row outside of every sequence, or one that sees scores of -inf only, whose softmax is not a number
+  const float inv = l == 0.f ? (s.count ? NAN : 0.f) : 1.f / l;
   T *out = (T *)g.out + rep * g.out_stride + (long long)row * g.ld_out + (long long)head * g.dim;
 #pragma unroll
   for (int d = 0; d < ND; ++d)

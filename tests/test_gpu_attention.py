@@ -264,6 +264,41 @@ def test_what_is_not_seen_among_many_heads(gpu, dtype, H, K, D):
     assert torch.equal(x, y) and not torch.isfinite(d[0, keys, H].float()).all()
 
 
+@pytest.mark.parametrize("dtype,n,H,K,D", [(0, 1, 2, 1, 64), (1, 1, 2, 1, 64), (1, 1, 4, 2, 96), (0, 4, 40, 40, 64), (1, 4, 40, 20, 64), (1, 4, 24, 24, 128)])
+def test_scores_of_minus_infinity(gpu, dtype, n, H, K, D):
+    """A softmax over scores of -inf only is NaN, here as for a token over its cache; where a row sees another score as well, such a key counts for nothing."""
+    torch, pb = gpu
+    T = 140
+    P = Problem(torch, pb, dtype, n, T, [[3, 60, T - 1]] * n, H, K, D, 0, 0)
+    P.x[:, :, :H, 0] = 1.0
+    P.x[:, 3, H:H + K, 0] = -math.inf                          # the first sequence's first two tokens
+    P.x[:, 4, H:H + K, 0] = -math.inf
+    P.view(P.rows, P.stride, P.ld, H + 2 * K).copy_(P.x)
+    out, lse = P.forward()
+    o, lse = P.view(out, P.out_stride, P.ld_out, H).cpu().double(), lse.cpu()
+    assert o[:, 3:5].isnan().all() and (lse[:, :, 3:5] == -math.inf).all()
+    assert (o[:, :3] == 0).all() and (o[:, T - 1:] == 0).all() and (lse[:, :, :3] == -math.inf).all()
+    assert o[:, 5:T - 1].isfinite().all() and lse[:, :, 5:T - 1].isfinite().all()
+    see = visible(T, [0, T], 0, 0)
+    for head in range(H):
+        q, k, v = P.heads(0, head)
+        # without those two, from token 5 on
+        R = Head(q[5:60], k[5:60], v[5:60], see[:55, :55], P.scale, dtype)
+        tol, tol_lse = R.forward_bounds()
+        within(o[0, 5:60, head], R.out, tol, f"out of head {head}")
+        within(lse[0, head, 5:60], R.lse, tol_lse, f"lse of head {head}")
+    # the same of caches
+    rows = P.x[:, :, :].to(dt(torch, dtype))
+    caches = [rows[:, 3:6, H + i * K:H + (i + 1) * K].transpose(1, 2).contiguous().cuda() for i in (0, 1)]
+    desc = pb.parle_cache_desc(dtype, n, 3, H, K, D, 0, 0, P.scale, H * D, K * D, H * D)
+    got = torch.empty(n, H * D, dtype=dt(torch, dtype), device="cuda")
+    sc = torch.empty(max(16, pb.parle_k_decode_scratch_bytes(desc)), dtype=torch.uint8, device="cuda")
+    for length in (2, 3):
+        q = rows[:, 2 + length, :H].reshape(n, H * D).contiguous().cuda()
+        pb.parle_k_attention_decode(desc, q, None, None, torch.full((n,), length, dtype=torch.int32, device="cuda"), sc, *caches, got)
+        assert got.isnan().all() if length == 2 else torch.isfinite(got).all()
+
+
 def test_gradient_by_differences(gpu):
     """fp32: the derivative of <out, dout> along a direction of q, k and v, by central differences at two widths."""
     torch, pb = gpu
