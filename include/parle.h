@@ -547,8 +547,8 @@ typedef struct {
   int64_t ld_out, out_stride;         /* of out */
 } parle_rope_desc;
 /* Rotary positions: each pair (a, b) of a head turns by t = position * freqs[p], its axis' position in positions [n][tokens][axes], freqs [P] fp32:
- * (a cos t - b sin t, a sin t + b cos t).  The angle is formed and reduced in 64 bits, so far positions are as exact as near ones.  Elements
- * from 2 P on are copied.  out may be x, in the same layout. */
+ * (a cos t - b sin t, a sin t + b cos t).  Nothing of the angle is lost before it is reduced to a turn, so far positions are as exact as near ones,
+ * for frequencies up to 2^16.  Elements from 2 P on are copied.  out may be x, in the same layout. */
 parle_status parle_k_rope(void *hip_stream, const parle_rope_desc *desc, const void *x, const int32_t *positions, const float *freqs, void *out);
 
 #define PARLE_ATTENTION_MAX_DIM 128

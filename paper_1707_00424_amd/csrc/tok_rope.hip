@@ -1,8 +1,10 @@
 // Rotary positions: pairs of a head's elements turned by position * frequency.  All memory: each element is read and written once.
 //
 // The sines and cosines of a token are the same for its heads, so a workgroup makes those of its tokens once, in LDS, and then streams the
-// heads.  An angle is formed and reduced to a turn in 64 bits, where position * frequency is exact; sine and cosine of the rest, half a turn at most
-// either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the rest's rounding and two steps of the function.
+// heads.  An angle is reduced to a turn in 64 bits: position * frequency as its rounded value and what that left out, times 1 / (2 pi) in two parts as well, so
+// that what is lost does not grow with the position (a product rounded in between is off by 2^-21 of angles at positions near 2^31, and by as often more as
+// the frequency is above 1).  Sine and cosine of the rest, half a turn at most either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the
+// rest's rounding and two steps of the function; for frequencies up to 2^16.
 //
 // Three replicas of 4099 tokens, 20 heads of 80 elements of which 64 turn, fp32: 40 us, 3.9 TB/s for reads and writes; 8192 tokens of 40 heads of 128 elements in bf16
 // 36 us, 4.7 TB/s; 16 tokens 6 us, a start, sines and a load.
@@ -67,8 +69,10 @@ __global__ __launch_bounds__(kThreads) void k_rope(Args g) {
     const int t = i / g.pairs, p = i - t * g.pairs;
     int axis = 0;
     while (axis < g.axes - 1 && p >= g.ends[axis]) ++axis;
-    const double turns = (double)pos[t * g.axes + axis] * (double)g.freqs[p] * 0.15915494309189533577;
-    const float half = (float)(2.0 * (turns - rint(turns)));
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -9.839338337591243e-18;  // 1 / (2 pi)
+    const double at = pos[t * g.axes + axis], freq = g.freqs[p], angle = at * freq, rest = __builtin_fma(at, freq, -angle);
+    const double turns = __builtin_fma(angle, kTurn, -rint(angle * kTurn));
+    const float half = (float)(2.0 * __builtin_fma(rest, kTurn, __builtin_fma(angle, kTurnRest, turns)));
     float s, c;
     sincospif(half, &s, &c);
     turn[i] = f2{c, s * g.sign};

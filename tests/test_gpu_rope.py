@@ -80,6 +80,33 @@ def test_rope(gpu, dtype, interleaved, n, tokens, heads, dim, pairs, pad):
     assert ((got - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("most", [1.0, 64.0, 65536.0])
+def test_far_positions_are_as_exact_as_near_ones(gpu, most):
+    """Sines and cosines of angles up to 2^47, against products and reductions of sixty digits."""
+    from decimal import Decimal, getcontext
+    torch, pb = gpu
+    getcontext().prec = 60
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+    T, P = 60, 16
+    g = torch.Generator().manual_seed(7)
+    positions = torch.randint(1 << 30, (1 << 31) - 1, (1, T, 1), generator=g, dtype=torch.int64)
+    positions[0, ::2] *= -1
+    positions[0, :2, 0] = torch.tensor([(1 << 31) - 1, -(1 << 31)])
+    freqs = most * torch.rand(P, generator=g)
+    freqs[0] = most
+    x = torch.zeros(1, T, 1, 2 * P)
+    x[..., :P] = 1.0
+    out = torch.empty(1, T, 1, 2 * P, device="cuda")
+    pb.parle_k_rope(pb.make_rope_desc(0, 1, T, 1, 2 * P, [P], 0, 0, 2 * P, 2 * P * T, 2 * P, 2 * P * T), x.cuda(), positions.int().cuda(), freqs.cuda(), out)
+    got = out.cpu().double()[0, :, 0]
+    for t in range(T):
+        for p in range(P):
+            turns = Decimal(int(positions[0, t, 0])) * Decimal(float(freqs[p])) / turn
+            angle = float((turns - turns.to_integral_value()) * turn)
+            # within 2^-22 as stated, and the product with one of this pair is exact
+            assert abs(float(got[t, p]) - math.cos(angle)) <= 2.0 ** -22 and abs(float(got[t, P + p]) - math.sin(angle)) <= 2.0 ** -22, (t, p)
+
+
 def test_the_inverse_is_the_gradient(gpu):
     """<rope(x), dy> = <x, inverse(dy)> for any x and dy: the map is linear."""
     torch, pb = gpu
