@@ -296,7 +296,8 @@ class TokenModel:
         positions = (torch.arange(total, dtype=torch.int32, device=dev) - offsets[:-1].repeat_interleave(lengths)).reshape(1, -1, 1)
         if A:
             W, H = (A.heads + 2 * A.kv_heads) * A.dim, A.heads * A.dim
-            capacity = A.sinks + A.window if A.window else max(len(p) for p in prompts) + count
+            # (a cache has a slot behind its sinks, also where a whole answer is no longer than they are)
+            capacity = A.sinks + A.window if A.window else max(max(len(p) for p in prompts) + count, A.sinks + 1)
             caches = [[torch.zeros((B, A.kv_heads, capacity, A.dim), dtype=torch.bfloat16, device=dev) for _ in range(2)] for _ in range(self.L)]
             cache = pb.parle_cache_desc(1, B, capacity, A.heads, A.kv_heads, A.dim, A.window, A.sinks, A.dim ** -0.5, W, W, H)
             attention = pb.parle_attention_desc(1, 1, total, B, A.heads, A.kv_heads, A.dim, A.window, A.sinks, A.dim ** -0.5, W, total * W, W, total * W, H, total * H)

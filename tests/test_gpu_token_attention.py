@@ -105,6 +105,16 @@ def test_answers_are_those_of_whole_sequences(gpu, window, sinks):
     assert ((drawn >= 0) & (drawn < V)).all() and drawn.shape == (3, count)
 
 
+@pytest.mark.parametrize("sinks", [4, 5, 128])
+def test_answers_no_longer_than_the_sinks(gpu, sinks):
+    """Without a window all tokens are seen, sinks or not: the answers are those of the same model without sinks."""
+    torch, tm = gpu
+    prompts = [torch.tensor([3], dtype=torch.int32), torch.tensor([5, 6], dtype=torch.int32)]
+    uniform = torch.rand((2, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    make = lambda s: tm.TokenModel(1, 32, 100, 32, layers=1, seed=4, attention=tm.Heads(heads=2, kv_heads=1, dim=16, sinks=s))  # noqa: E731
+    assert torch.equal(make(sinks).answer(prompts, uniform), make(0).answer(prompts, uniform))
+
+
 def test_a_model_without_attention_answers_too(gpu):
     torch, tm = gpu
     model = tm.TokenModel(1, 32, 100, 32, layers=1)
