@@ -282,13 +282,23 @@ class TokenModel:
 
     def answer(self, prompts, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
         """Tokens behind ``prompts``, a list of int32 tensors: one for each of the numbers ``uniform`` [prompts, count] out of [0, 1), by
-        the reference x_ref: int32 [prompts, count].  temperature, top_k, top_p, min_p: [prompts] each, or None.  A model with attention keeps
-        rolling caches of sinks + window tokens (all of them without a window); one without sees the last token only."""
+        the reference x_ref: int32 [prompts, count].  temperature, top_k, top_p, min_p: [prompts] each, or None.  All may be of any type and on any
+        device.  A model with attention keeps rolling caches of sinks + window tokens (all of them without a window); one without sees the last token only."""
         torch, A, V = self.torch, self.A, self.V
-        count, B = uniform.shape[1], len(prompts)
-        if B != uniform.shape[0] or not all(len(p) for p in prompts):
+        count, B, dev = uniform.shape[1], len(prompts), self.x.device
+        if not B or B != uniform.shape[0] or not all(len(p) for p in prompts):
             raise ValueError("answer needs a row of numbers for each prompt, and prompts of one token at least")
-        dev = uniform.device
+
+        def rule(name, value, dtype):
+            if value is None:
+                return None
+            value = torch.as_tensor(value)
+            if value.numel() != B:
+                raise ValueError(f"answer needs one {name} for each prompt")
+            return value.reshape(B).to(device=dev, dtype=dtype, copy=True).contiguous()  # a tensor of its own is aligned
+
+        temperature, top_p, min_p = (rule(k, v, torch.float32) for k, v in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p)))
+        top_k = rule("top_k", top_k if top_k is None else torch.as_tensor(top_k).clamp(-1, V), torch.int32)
         lengths = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device=dev)
         offsets = torch.nn.functional.pad(torch.cumsum(lengths, 0, dtype=torch.int32), (1, 0))
         packed = torch.cat(list(prompts)).to(device=dev, dtype=torch.int32)
@@ -314,7 +324,7 @@ class TokenModel:
         desc = pb.parle_sample_desc(1, 1, B, V, V)
         sampling = torch.empty(max(16, pb.parle_k_sample_scratch_bytes(desc)), dtype=torch.uint8, device=dev)
         chosen = torch.empty((count, B), dtype=torch.int32, device=dev)
-        numbers = uniform.t().contiguous()
+        numbers = uniform.to(device=dev, dtype=torch.float32).t().contiguous()
         logits = self._reference_logits(packed, positions, prompt)[:, (offsets[1:] - 1).long()].contiguous()
         for step in range(count):
             # each step's row of numbers and tokens is copied: rows of B begin anywhere, and a tensor of its own is aligned

@@ -115,6 +115,28 @@ def test_answers_no_longer_than_the_sinks(gpu, sinks):
     assert torch.equal(make(sinks).answer(prompts, uniform), make(0).answer(prompts, uniform))
 
 
+def test_rules_of_any_type_and_place(gpu):
+    """Numbers and rules are converted, not read as what they are not; every second row of a 64-bit top_k had none."""
+    torch, tm = gpu
+    model = tm.TokenModel(1, 32, 100, 32, layers=1, seed=4, attention=tm.Heads(heads=2, kv_heads=1, dim=16))
+    B = 4
+    prompts = [torch.tensor([3 + i], dtype=torch.int32) for i in range(B)]
+    uniform = torch.rand((B, 6), generator=torch.Generator().manual_seed(1))
+    rules = dict(temperature=torch.tensor([2.0, 1.0, 3.0, 0.5]), top_k=torch.tensor([1, 2, 1, 3]), top_p=torch.tensor([0.9, 0.8, 1.0, 0.7]), min_p=torch.tensor([0.0, 0.1, 0.0, 0.2]))
+    want = model.answer(prompts, uniform.cuda(), **{k: v.to(torch.int32 if k == "top_k" else torch.float32).cuda() for k, v in rules.items()})
+    assert torch.equal(want, model.answer(prompts, uniform, **rules))
+    assert torch.equal(want, model.answer([p.cuda().long() for p in prompts], uniform.double().cuda(), **{k: (v if k == "top_k" else v.double()).cuda() for k, v in rules.items()}))
+    assert torch.equal(want, model.answer(prompts, uniform, **{k: torch.stack((v, v), 1)[:, 0] for k, v in rules.items()}))
+    # more classes than 32 bits count are all of them
+    assert torch.equal(model.answer(prompts, uniform), model.answer(prompts, uniform, top_k=torch.full((B,), 1 << 40)))
+    for k, v in rules.items():
+        for bad in (v[:3], v[0]):
+            with pytest.raises(ValueError, match=k):
+                model.answer(prompts, uniform, **{k: bad})
+    with pytest.raises(ValueError, match="answer needs"):
+        model.answer([], uniform[:0])
+
+
 def test_a_model_without_attention_answers_too(gpu):
     torch, tm = gpu
     model = tm.TokenModel(1, 32, 100, 32, layers=1)
