@@ -526,7 +526,15 @@ int parts_of(const parle_attention_desc &d) {
   return wgs >= places || (!d.dtype && d.dim > 64) ? 2 : 4;
 }
 
+// Workgroups of k_attn_dkv, of a replica: of keys, and of the sinks' chunks.
+int64_t dkv_workgroups(const parle_attention_desc &d) {
+  const int keys = kRows / parts_of(d);
+  return ((int64_t)tok::ceil_div(d.tokens, keys) + (has_far(d) ? (int64_t)tok::ceil_div(d.tokens, chunk_of(d)) * tok::ceil_div(d.sinks, keys) : 0)) * d.kv_heads;
+}
+
 }  // namespace
+
+bool attention_bwd_fits(const parle_attention_desc &d) { return d.tokens == 0 || dkv_workgroups(d) * kThreads < 1LL << 32; }
 
 int64_t attention_scratch_bytes(const parle_attention_desc &d) { return d.tokens == 0 ? 0 : stats_bytes(d) + 2 * far_elems(d) * 4; }
 
@@ -548,9 +556,8 @@ hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, c
     of_queries<<<dim3(b.a.tiles * d.heads, d.n), kThreads, 0, st>>>(b);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int keys = kRows / parts;
-    b.a.tiles = tok::ceil_div(d.tokens, keys);
-    of_keys<<<dim3((b.a.tiles + (far ? chunks * tok::ceil_div(d.sinks, keys) : 0)) * d.kv_heads, d.n), kThreads, 0, st>>>(b);
+    b.a.tiles = tok::ceil_div(d.tokens, kRows / parts);
+    of_keys<<<dim3((uint32_t)dkv_workgroups(d), d.n), kThreads, 0, st>>>(b);
     e = hipGetLastError();
     if (e != hipSuccess || !far) return e;
     of_sinks<<<dim3(chunks * d.kv_heads, d.n), 256, 0, st>>>(b);

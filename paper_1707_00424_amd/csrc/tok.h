@@ -212,6 +212,7 @@ hipError_t launch_rope(hipStream_t st, const parle_rope_desc &d, const void *x, 
 
 hipError_t launch_attention_fwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
                                 const int32_t *offsets, void *out, float *lse);
+bool attention_bwd_fits(const parle_attention_desc &d);  // one launch holds the workgroups of the gradient
 int64_t attention_scratch_bytes(const parle_attention_desc &d);
 hipError_t launch_attention_bwd(hipStream_t st, const parle_attention_desc &d, const void *q, const void *k, const void *v,
                                 const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch, void *dq, void *dk,

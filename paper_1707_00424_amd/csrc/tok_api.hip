@@ -172,6 +172,12 @@ bool good(Check &c, const parle_attention_desc *d) {
          good_rows(c, d->n, d->tokens, (long long)d->heads * d->dim, d->ld_out, d->out_stride, "ld_out is less than heads * dim",
                    "out_stride is less than a replica's rows");
 }
+// The gradient's workgroups of keys are more than the forward pass', and those of the sinks' queries are added.
+bool good_bwd(Check &c, const parle_attention_desc *d) {
+  if (!good(c, d)) return false;
+  c.that(attention_bwd_fits(*d), PARLE_ESIZE, "the gradient of these tokens, heads and sinks takes more than 2^32 threads of a replica");
+  return c.status == PARLE_OK;
+}
 bool good(Check &c, const parle_cache_desc *d) {
   c.field(d, "desc is NULL");
   if (c.status || !good_heads(c, d->dtype, d->heads, d->kv_heads, d->dim, d->window, d->sinks, d->scale)) return false;
@@ -330,7 +336,7 @@ parle_status parle_k_rope(void *hip_stream, const parle_rope_desc *desc, const v
 
 int64_t parle_k_attention_scratch_bytes(const parle_attention_desc *desc) {
   Check c{"parle_k_attention_scratch_bytes"};
-  return good(c, desc) ? attention_scratch_bytes(*desc) : -1;
+  return good_bwd(c, desc) ? attention_scratch_bytes(*desc) : -1;
 }
 
 parle_status parle_k_attention_forward(void *hip_stream, const parle_attention_desc *desc, const void *q, const void *k, const void *v,
@@ -349,7 +355,7 @@ parle_status parle_k_attention_backward(void *hip_stream, const parle_attention_
                                         const int32_t *offsets, const void *out, const float *lse, const void *dout, void *scratch,
                                         int64_t scratch_bytes, void *dq, void *dk, void *dv) {
   Check c{"parle_k_attention_backward"};
-  if (!good(c, desc)) return c.status;
+  if (!good_bwd(c, desc)) return c.status;
   if (desc->tokens == 0) return PARLE_OK;
   c.given(q, "q is NULL").given(k, "k is NULL").given(v, "v is NULL").given(out, "out is NULL").given(lse, "lse is NULL").given(dout, "dout is NULL");
   c.given(dq, "dq is NULL").given(dk, "dk is NULL").given(dv, "dv is NULL").maybe(offsets);

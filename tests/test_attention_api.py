@@ -115,6 +115,20 @@ def test_buffers_that_meet():
     assert _call("parle_k_attention_decode", cache(), s[0], None, *s[2:])[0] == E     # k without v
 
 
+def test_a_gradient_of_more_threads_than_a_launch_has():
+    """Refused in front of its first launch; the forward pass of the same descriptor has half as many and asks for its pointers."""
+    most = dict(n=1, tokens=16384, sequences=1, heads=65535, kv_heads=65535, dim=8, q_stride=0, kv_stride=0, out_stride=0, ld_q=65535 * 8, ld_kv=65535 * 8, ld_out=65535 * 8)
+    others = most | dict(tokens=26843, heads=40000, kv_heads=40000)               # 420 workgroups for each of 40000 heads
+    fits = most | dict(heads=65534, kv_heads=32767)
+    for kw, ok in ((most | dict(window=1, sinks=128), False), (others, False), (most, True), (fits | dict(window=1, sinks=128), True)):
+        d = attention(**kw)
+        assert (pb.parle_k_attention_scratch_bytes(d) > 0) == ok
+        status, text = _call("parle_k_attention_backward", d, None, *CALLS["parle_k_attention_backward"][1][1:])
+        assert (status, "threads" in text) == ((E, False) if ok else (S, True)), (kw, status, text)
+        status, text = _call("parle_k_attention_forward", d, None, *CALLS["parle_k_attention_forward"][1][1:])
+        assert status == E and "q is NULL" in text
+
+
 def test_scratch():
     for make, query, name, at in [(attention, "parle_k_attention_scratch_bytes", "parle_k_attention_backward", 8), (cache, "parle_k_decode_scratch_bytes", "parle_k_attention_decode", 5),
                                   (sample, "parle_k_sample_scratch_bytes", "parle_k_sample", 7)]:
