@@ -96,6 +96,23 @@ def test_decode(gpu, case, fused):
         assert same.all(), "the caches hold something else"
 
 
+SPREAD = [1, 0, 31, 513, 600, 1024, 1099, 700]
+# 128 workgroups of sequences, key heads and sixteens of query heads, or more: up to 1536 visible tokens go through one workgroup, more are shared
+MANY = [
+    (1, SPREAD + [1100] * 8, 16, 8, 64, 0, 0, 1100),
+    (0, SPREAD * 4, 4, 4, 64, 700, 3, 703),
+    (0, SPREAD + [1536] * 8, 8, 8, 128, 0, 0, 1536),
+    (1, SPREAD + [2000, 513, 514], 160, 4, 128, 0, 100, 613),
+    (1, SPREAD + [1537] * 8, 8, 8, 72, 0, 0, 1537),
+]
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(str(v) for v in c[2:]) + f"-{c[0]}-{len(c[1])}")
+def test_decode_of_many_sequences(gpu, case, fused):
+    test_decode(gpu, case, fused)
+
+
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("sinks,capacity", [(0, 7), (3, 10), (0, 64), (5, 300), (128, 129)])
 def test_store(gpu, dtype, sinks, capacity):
