@@ -608,8 +608,9 @@ typedef struct {
  * falling logit, the lower class first where two are equal: the first top_k stay (top_k <= 0: all); of those the shortest beginning whose sum of w is at
  * least top_p times that of all that stayed (top_p >= 1: all of them); of those the ones with w >= min_p.  At least one stays.  The token is the first whose sum of w
  * with those before it exceeds uniform times the whole sum.  temperature <= 0 takes the first class.  kept: how many stayed; logp: the logarithm of the
- * token's share of their sum; both may be NULL.  In sums w is counted in whole multiples of 2^-s, s the largest up to 50 with
- * classes * 2^s <= 2^62; min_p is held against w itself, however small.
+ * token's share of their sum; both may be NULL.  In sums w is counted in whole multiples of 2^-s, s the largest up to 50 with classes * 2^s <= 2^62;
+ * min_p is held against w itself, however small.  w is formed to 3e-14 of itself: a border that near may lie on either side.
+ * The scratch query says 0 as yet, and scratch may be NULL.
  * A row of -inf only gives token -1, kept 0 and logp -inf; a row with a NaN token -1, kept 0 and logp NaN; +inf leaves the classes that have it, evenly. */
 parle_status parle_k_sample(void *hip_stream, const parle_sample_desc *desc, const void *logits, const float *uniform, const float *temperature,
                             const int32_t *top_k, const float *top_p, const float *min_p, void *scratch, int64_t scratch_bytes, int32_t *tokens,

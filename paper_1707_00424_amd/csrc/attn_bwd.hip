@@ -8,7 +8,7 @@
 // workgroups of their own, into scratch, and joined behind.
 //
 // Measured, bf16: three replicas of 4096 tokens, 16 heads of 64 elements on 4 of keys, a window of 1024 and 4 sinks: 247 us, 0.51 PFLOP/s of the seven
-// products, of which dQ takes 42 %, dK and dV 55 %, the sinks 3; 4099 tokens of 16 heads of 128 elements without a window 383 us, 0.63 PFLOP/s, 39 and 61 %.
+// products, of which dQ takes 42 %, dK and dV 55 %, the sinks 3; 4099 tokens of 16 heads of 128 elements without a window 386 us, 0.63 PFLOP/s, 41 and 59 %.
 // What bounds them is that matrix unit (30 and 27 to 47 % of the time), vector unit (24 to 45 %) and LDS (15 to 24 %) wait for one another: dK and dV of 128
 // elements leave room for one wavefront on a SIMD, the others for two.  With one, the scalar operations in front of a step's loads count as well (1000 of
 // 3900 cycles before all heads of a group shared a descriptor).

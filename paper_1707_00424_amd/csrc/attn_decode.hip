@@ -3,7 +3,7 @@
 // A cache is read once and nothing else matters, so its tokens are shared out over enough workgroups to keep memory busy, and their maxima, sums
 // and partial results are joined behind.  The query heads of a key head, up to sixteen at a time, are the sixteen columns of a matrix instruction:
 // S^T = K Q^T and O^T = V^T P^T as in the forward pass, in tiles of 16 keys.  A wavefront has the next 32 keys and values on their way in registers while
-// it multiplies: 64 sequences of up to 8192 tokens, 32 heads on 8 of keys of 128 elements, bf16: 1.63 GB in 297 us, 5.5 TB/s (a plain read of as much 5.9); 4 sequences of 1028
+// it multiplies: 64 sequences of up to 8192 tokens, 32 heads on 8 of keys of 128 elements, bf16: 1.63 GB in 299 us, 5.4 TB/s (a plain read of as much 5.9); 4 sequences of 1028
 // tokens 11.5 us, of which 8.3 are the shares and 3 to join them.
 #include "attn.h"
 

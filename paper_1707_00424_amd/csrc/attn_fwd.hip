@@ -4,8 +4,8 @@
 // A wavefront has 32 queries, whose Q stays in registers; tiles of 64 keys and values go from memory straight into LDS, the next one while one is
 // multiplied.  Per tile that is as much work for the matrix unit (of 128 elements: 32 instructions of 32 cycles) as for the vector unit (exponentials, maxima
 // and conversions), and half of that for LDS, where the values' transposing reads go at a quarter of the rate of rows.  Two wavefronts of a SIMD overlap
-// them in part: 8192 tokens of 32 heads of 128 elements in bf16, 524 us, are 1.05 PFLOP/s, the units 55 and 51 % of the time busy.  With a window of 1024 (16
-// heads) it is 0.66 PFLOP/s, 82 us: a third of what a wavefront multiplies lies outside of its window's edges, and starts are a larger part.
+// them in part: 8192 tokens of 32 heads of 128 elements in bf16, 534 us, are 1.03 PFLOP/s, the units 55 and 51 % of the time busy.  With a window of 1024 (16
+// heads) it is 0.66 PFLOP/s, 83 us: a third of what a wavefront multiplies lies outside of its window's edges, and starts are a larger part.
 // 64 queries to a wavefront, which would halve the reads of LDS, need more registers than there are.
 #include "attn.h"
 

@@ -7,7 +7,7 @@
 // rest's rounding and two steps of the function; for frequencies up to 2^16.
 //
 // Three replicas of 4099 tokens, 20 heads of 80 elements of which 64 turn, fp32: 40 us, 3.9 TB/s for reads and writes; 8192 tokens of 40 heads of 128 elements in bf16
-// 36 us, 4.7 TB/s; 16 tokens 6 us, a start, sines and a load.
+// 37 us, 4.5 TB/s; 16 tokens 6 us, a start, sines and a load.
 #include "tok.h"
 
 namespace {

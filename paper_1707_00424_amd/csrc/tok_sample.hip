@@ -13,8 +13,8 @@
 // A row of bf16 is counted by value first (by_values), so that 4096 weights are formed in 64 bits and not one for each class.
 //
 // What bounds it: 4 rows of 128000 bf16 with top-k 50 (20 us) are latency, two passes of a row by one workgroup and a chain of scans and a sort; 1024 rows of 50001
-// bf16 with top-p and min-p (92 us, 102 MB read three times, twice from cache) the vector unit, about 35 operations for a class.  The same of fp32 with top-p
-// takes 211, in weights of 64 bits for every class.
+// bf16 with top-p and min-p (93 us, 102 MB read three times, twice from cache) the vector unit, about 35 operations for a class.  The same of fp32 with top-p
+// takes 212, with min-p too 169, in weights of 64 bits for every class.
 #include <type_traits>
 
 #include "tok.h"
@@ -913,8 +913,11 @@ hipError_t launch_sample(hipStream_t st, const parle_sample_desc &d, const void 
   while (d.classes > 1LL << (62 - bits)) --bits;
   Args g{logits, uniform, temperature, top_k, top_p, min_p, tokens, kept, logp, d.classes, bits, d.ld};
   const int rows = d.n * d.rows;
-  // More rows than compute units: workgroups of 512 threads, two to a compute unit, where one's serial steps hide behind the other's passes.  1024 rows of
-  // 50001 classes, bf16 without top-k, take 91 us against 110 in workgroups of 1024, 300 rows 41 and 52; 256 rows 31 and 29, 4 rows of 128000 36 and 32.
+  // More rows than compute units: workgroups of 512 threads, two to a compute unit, where one's serial steps hide behind the other's passes.  In us, against
+  // workgroups of 1024, top-p and min-p without top-k: bf16, 1024 rows of 50001 classes 87 and 104, of 5001 47 and 64, of 1000 41 and 46, 300 of 50001 42 and 52,
+  // 257 of 1000 18 and 15; 256 of 50001 32 and 28, 64 of 128000 40 and 34.  fp32, 1024 of 50001 168 and 170, of 1000 24 and 45, 257 of 1000 12 and 15; 256 of
+  // 50001 91 and 59; but 300 of 50001 114 and 93, 512 132 and 109, as one long row's passes are most of the time.  With a top-k of 50 the smaller ones win
+  // wherever they are taken: 1024 of 50001 46 and 54, 257 of 1000 11 and 14 (fp32 9 and 14), and lose below: 64 of 128000 29 and 22.
   const bool many = rows > 256;
   auto go = [&](auto *kernel, int threads) {
     kernel<<<rows, threads, 0, st>>>(g);
