@@ -2,9 +2,9 @@
 //
 // The sines and cosines of a token are the same for its heads, so a workgroup makes those of its tokens once, in LDS, and then streams the
 // heads.  An angle is reduced to a turn in 64 bits: position * frequency as its rounded value and what that left out, times 1 / (2 pi) in two parts as well, so
-// that what is lost does not grow with the position (a product rounded in between is off by 2^-21 of angles at positions near 2^31, and by as often more as
-// the frequency is above 1).  Sine and cosine of the rest, half a turn at most either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the
-// rest's rounding and two steps of the function; for frequencies up to 2^16.
+// that what is lost does not grow with the position (a product rounded in between is off by 2^-21 of an angle near position 2^31 at a frequency of 1, by
+// 2^-15 at 64).  Sine and cosine of the rest, half a turn at most either way, are fp32's, within 2^-22 of the true ones: 2^-25 * pi from the rest's
+// rounding and two steps of the function; for frequencies up to 2^16.
 //
 // Three replicas of 4099 tokens, 20 heads of 80 elements of which 64 turn, fp32: 40 us, 3.9 TB/s for reads and writes; 8192 tokens of 40 heads of 128 elements in bf16
 // 37 us, 4.5 TB/s; 16 tokens 6 us, a start, sines and a load.
